@@ -300,6 +300,152 @@ int fl_lm_head_backward(fl_client* client, const void* h, const void* ln_g, cons
                         float grad_scale, void* dh, float* dln_g, float* dln_b, float* dw, void* workspace,
                         size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Preference loss on pairs of answers, beside the cross-entropy of the final
+ * linear layer.  The sequences of a batch come in pairs, every client's own:
+ * sequence 2p is the preferred answer of pair p, sequence 2p + 1 the rejected
+ * one.  Over the labelled rows t of sequence s
+ *     l_s = sum_t (y'_t[label_t] - logsumexp(y'_t)),
+ *     z_p = beta ((l_2p - ref_2p) - (l_2p+1 - ref_2p+1)),
+ *     L_p = (1 - eps) softplus(-z_p) + eps softplus(z_p),
+ * with the sequences' log-probabilities under a frozen reference model, ref
+ * (none: 0).  A label outside [0, vocab) marks a row without one (a prompt's,
+ * a sequence's last); its logits are not read and its gradient is zero.  A
+ * sequence without labels has l_s = 0.  Sums over a row are fp32, sums over a
+ * sequence 64 bits.  -infinity marks a masked id (probability and gradient 0).
+ *
+ * These entry points take the labels in device memory (read on the stream;
+ * nothing is uploaded, so calls can be captured into a graph). */
+typedef struct fl_preference_desc {
+  int64_t vocab;          /* multiple of 8, <= 2^24 */
+  int32_t dtype;          /* FL_BF16 | FL_F32: element type of the logits */
+  float beta;             /* > 0 */
+  float label_smoothing;  /* eps in [0, 0.5]: probability that a pair is labelled the wrong way round */
+} fl_preference_desc;
+
+/* Device workspace of the forward and backward for this batch; it holds what
+ * the backward needs of the forward. */
+int fl_preference_workspace_bytes(const fl_preference_desc* desc, const fl_batch_desc* batch, size_t* bytes);
+/* logits device [T, ld] (ld >= vocab, a multiple of 8; columns past vocab are
+ * not read); labels device [T]; ref_logp device [S] or NULL; logp device [S]
+ * receives l_s, loss device [S / 2] L_p and loss_sum device [1] their sum in
+ * pair order.  With ref_logp NULL logp is what a reference model's pass
+ * gives.  Outputs overlap neither inputs nor the workspace. */
+int fl_preference_forward(const fl_preference_desc* desc, const fl_batch_desc* batch, const void* logits, int64_t ld,
+                          const int32_t* labels, const float* ref_logp, float* logp, float* loss, float* loss_sum,
+                          void* workspace, size_t workspace_bytes, void* stream);
+/* Gradient of grad_scale * loss_sum by the logits, after a forward with the
+ * same descriptor, batch, logits, labels and workspace: dlogits [T, ld_d]
+ * (ld_d as ld), of which the first width_d columns are written (vocab <=
+ * width_d <= ld_d, a multiple of 8), 0 past vocab; may be the logits
+ * themselves when ld_d = ld. */
+int fl_preference_backward(const fl_preference_desc* desc, const fl_batch_desc* batch, const void* logits, int64_t ld,
+                           const int32_t* labels, float grad_scale, void* dlogits, int64_t ld_d, int64_t width_d,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* fl_lm_head_forward / fl_lm_head_backward with the preference loss in the
+ * cross-entropy's place: the logits stay in the client's workspace, where the
+ * backward replaces them by their gradient.  desc's vocab and dtype are the
+ * client's; labels host [T] (a negative one marks a row without label, one >=
+ * vocab gives FL_ERR_ARG); the other arguments as in the four calls above. */
+int fl_lm_head_preference_forward(fl_client* client, const fl_preference_desc* desc, const fl_batch_desc* batch,
+                                  const void* h, const void* ln_g, const void* ln_b, const void* w,
+                                  const int32_t* labels, const float* ref_logp, float* logp, float* loss,
+                                  float* loss_sum, void* workspace, size_t workspace_bytes, void* pref_workspace,
+                                  size_t pref_workspace_bytes, void* stream);
+int fl_lm_head_preference_backward(fl_client* client, const fl_preference_desc* desc, const fl_batch_desc* batch,
+                                   const void* h, const void* ln_g, const void* w, float grad_scale, void* dh,
+                                   float* dln_g, float* dln_b, float* dw, void* workspace, size_t workspace_bytes,
+                                   void* pref_workspace, size_t pref_workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Low-rank adapters: every client's own trained pair beside a projection that
+ * all clients share, over one packed client batch.  With s the slot of row
+ * t's client
+ *     v_t = A_s x_t,    y_t = base_t + scale B_s v_t;
+ * a client without a slot has v_t = 0 and y_t = base_t.  Backward:
+ *     dv_t = scale B_s^T dy_t,   dx_t = dres_t + A_s^T dv_t,
+ *     dA_s += sum_t dv_t x_t^T,  dB_s += scale sum_t dy_t v_t^T
+ * over all rows of all clients that share slot s.  v stays in fp32 between
+ * the two products, and products with it keep its digits (bf16 inputs give
+ * the results of an fp32 computation rounded once).
+ * Row strides are in elements, multiples of 8, at least the row's width. */
+typedef struct fl_adapter_desc {
+  int32_t num_adapters;  /* slots n, 1 .. 2^16 */
+  int32_t rank;          /* r: a multiple of 8 in [8, 64] */
+  int32_t in_features;   /* multiples of 8 in [8, 65536] */
+  int32_t out_features;
+  float scale;           /* finite */
+  int32_t dtype;         /* FL_BF16 | FL_F32: x, y, A, B and their gradients dx; v, dA, dB are fp32 */
+} fl_adapter_desc;
+
+/* Device workspace of the forward and of the backward for this batch; nothing
+ * is kept in it between calls. */
+int fl_adapter_workspace_bytes(const fl_adapter_desc* desc, const fl_batch_desc* batch, size_t* bytes);
+/* client_adapter host [C]: each client's slot in [0, n), or -1; several
+ * clients may share a slot.  x [T, ldx]; a [n, r, in]; b [n, out, r]; base [T,
+ * ld_base] or NULL (0), may be y itself; y [T, ldy]; v [T, r] fp32, which the
+ * backward reads. */
+int fl_adapter_forward(const fl_adapter_desc* desc, const fl_batch_desc* batch, const int32_t* client_adapter,
+                       const void* x, int64_t ldx, const void* a, const void* b, const void* base, int64_t ld_base,
+                       void* y, int64_t ldy, float* v, void* workspace, size_t workspace_bytes, void* stream);
+/* dy [T, ld_dy]; x, a, b, client_adapter as in the forward; v as it left it;
+ * dres [T, ld_dres] or NULL (0), may be dx itself; dx [T, ld_dx], or NULL: not
+ * formed; da, db fp32 in A's and B's shapes, accumulated (+=), never zeroed. */
+int fl_adapter_backward(const fl_adapter_desc* desc, const fl_batch_desc* batch, const int32_t* client_adapter,
+                        const void* dy, int64_t ld_dy, const void* x, int64_t ldx, const void* a, const void* b,
+                        const float* v, const void* dres, int64_t ld_dres, void* dx, int64_t ld_dx, float* da,
+                        float* db, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The server stack with adapters on every block's fused query / key / value
+ * projection (in = H, out = 3H; rotary follows, as for the projection
+ * itself).  The block weights may be trained or frozen, the P-tuning prefix
+ * present or not, as without adapters. */
+typedef struct fl_layer_adapters {
+  const void *a, *b; /* device [n, r, H] and [n, 3H, r], handle dtype */
+} fl_layer_adapters;
+typedef struct fl_layer_adapter_grads {
+  float *a, *b; /* device fp32 accumulators (+=), same shapes */
+} fl_layer_adapter_grads;
+typedef struct fl_stack_adapters {
+  int32_t num_adapters, rank;           /* as in fl_adapter_desc */
+  float scale;
+  const int32_t* client_adapter;        /* host [C] */
+  const fl_layer_adapters* layers;      /* host [N] */
+  const fl_layer_adapter_grads* grads;  /* host [N]; backward only */
+} fl_stack_adapters;
+/* Device memory beside the stack's workspace: every block's v, kept from the
+ * forward for the backward, and scratch. */
+int fl_stack_adapter_bytes(const fl_stack* stack, const fl_batch_desc* batch, const fl_stack_adapters* adapters,
+                           size_t* bytes);
+int fl_server_stack_forward_adapters(fl_stack* stack, const fl_batch_desc* batch, const fl_layer_params* layers,
+                                     const fl_stack_adapters* adapters, const void* x, void* y, void* saved,
+                                     int recompute, void* workspace, size_t workspace_bytes, void* adapter_workspace,
+                                     size_t adapter_workspace_bytes, void* stream);
+int fl_server_stack_backward_adapters(fl_stack* stack, const fl_batch_desc* batch, const fl_layer_params* layers,
+                                      const fl_layer_grads* grads, const fl_stack_adapters* adapters, const void* x,
+                                      const void* saved, const void* dy, void* dx, int recompute, void* workspace,
+                                      size_t workspace_bytes, void* adapter_workspace,
+                                      size_t adapter_workspace_bytes, void* stream);
+
+/* Global gradient norm and clipping, before the update:
+ *     norm = sqrt(sum of g^2 over all elements of all tensors),
+ *     coef = min(1, max_norm / (norm + 1e-6)),   out_i = coef g_i.
+ * grads / out: host arrays of num_tensors (1 .. 2^20) device pointers, 16-byte
+ * aligned (one of a tensor without elements is not read); sizes host [num]
+ * elements; dtype (FL_F32 or FL_BF16) is the one of all tensors.  The squares
+ * are summed in 64 bits in a fixed order.  norm_coef device fp32 [2], 8-byte
+ * aligned, receives norm and coef; nothing waits for them on the host.
+ * max_norm >= 0; infinity: coef = 1.  An infinite norm gives coef = 0, a NaN
+ * one NaN.  The workspace holds one call's partial sums. */
+int fl_grad_norm_workspace_bytes(int32_t num_tensors, const int64_t* sizes, size_t* bytes);
+int fl_grad_norm(int32_t dtype, int32_t num_tensors, const void* const* grads, const int64_t* sizes, double max_norm,
+                 float* norm_coef, void* workspace, size_t workspace_bytes, void* stream);
+/* out[i] (may be grads[i] itself: clipped in place) = norm_coef[1] * grads[i].
+ * No output may overlap another one or another tensor's gradient. */
+int fl_clip_grads(int32_t dtype, int32_t num_tensors, const void* const* grads, void* const* out,
+                  const int64_t* sizes, const float* norm_coef, void* stream);
+
 /* Server update (Section 4.1.4, Parameter Settings: Adam, learning rate
  * 2e-2, batch size 1, no warmup, no weight decay).  One step of Algorithm 1
  * of the Adam paper (Kingma & Ba) over n fp32 elements, elementwise in

@@ -8,5 +8,7 @@ no CPU path.
 from . import flglm  # noqa: F401
 from .flglm import BatchDesc, FlglmError, load  # noqa: F401
 from .stack import ServerStack  # noqa: F401
-from .optim import ParamArena, average  # noqa: F401
+from .optim import GradNorm, ParamArena, average  # noqa: F401
 from .client import ClientHead, SplitModel  # noqa: F401
+from .preference import PreferenceLoss  # noqa: F401
+from .adapters import ClientAdapters, StackAdapters  # noqa: F401

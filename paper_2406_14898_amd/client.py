@@ -47,6 +47,19 @@ class ClientHead:
                       dln_b=None) -> None:
         F.fl_lm_head_backward(self.handle, h, w, T, grad_scale, dh, dw, ws, stream, ln_g, dln_g, dln_b)
 
+    def preference_forward(self, pref, batch: F.BatchDesc, h, w, labels, ref_logp, logp, loss, loss_sum, ws, pref_ws,
+                           stream=None, ln_g=None, ln_b=None) -> None:
+        """head_forward with the PreferenceLoss `pref` in the cross-entropy's
+        place; labels host [T] (negative: none), outputs as pref.forward's."""
+        pref._outputs(batch, ref_logp, logp, loss, loss_sum)
+        F.fl_lm_head_preference_forward(self.handle, pref.desc, batch, h, w, labels, ref_logp, logp, loss, loss_sum, ws,
+                                        pref_ws, stream, ln_g, ln_b)
+
+    def preference_backward(self, pref, batch: F.BatchDesc, h, w, grad_scale: float, dh, dw, ws, pref_ws, stream=None,
+                            ln_g=None, dln_g=None, dln_b=None) -> None:
+        F.fl_lm_head_preference_backward(self.handle, pref.desc, batch, h, w, grad_scale, dh, dw, ws, pref_ws, stream,
+                                         ln_g, dln_g, dln_b)
+
 
 class SplitModel:
     """The whole split model on one GPU: the client's embedding, block 0,

@@ -1,0 +1,885 @@
+// Low-rank adapters of many clients beside a shared projection (C ABI entry
+// points), forward and backward over one packed client batch.
+//
+//   v = x A^T,  y = base + scale v B^T                        (rows' own A, B)
+//   dv = scale dy B,  dx = dres + dv A,  dA += dv^T x,  dB += scale dy^T v
+//
+// With a rank of at most 64 every one of these is bound by the wide operands
+// (x, y, dy, dx): each is read or written once, in four kernels.
+//
+//  * down: v from x.  64-row tiles, the reduction over a workgroup's waves,
+//    and over workgroups too when rows are few.
+//  * up: y from base and v.  A workgroup covers 64 rows x 256 columns.
+//  * bwd_out: one pass over dy gives dv (summed over column blocks) and dB
+//    (summed over slabs of rows).
+//  * bwd_in: one pass over x and dres gives dx and dA.
+//
+// v and dv are fp32.  In bf16 mode a matrix product with them runs on the bf16
+// matrix cores in parts: v = v0 + v1 (+ v2), each part the bf16 nearest to
+// what the parts before it leave.  Two parts hold 16 digits, enough under an
+// output that is rounded to bf16; three hold all 24, for dA and dB.
+//
+// Rows reach their adapters through a table of segments (runs of rows with
+// one slot) in kernel arguments: nothing is uploaded, and a call can be
+// captured.  Sums over rows and slabs have a fixed order: no atomics.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <new>
+#include <vector>
+
+#include "../../include/flglm.h"
+#include "common.h"
+#include "kernels.h"
+
+using namespace flglm;
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kSegs = 128;     // segments a launch (2 KB of kernel arguments, 3.5 KB with the slabs)
+constexpr int kTile = 64;      // forward: rows of a tile
+constexpr int kUpCols = 256;   // forward: columns of a workgroup of `up`
+constexpr int kStep = 32;      // backward: rows of a step
+constexpr int kBwdCols = 128 * kWaves;  // backward: columns of a workgroup
+
+struct Segs {
+  int32_t row0[kSegs], rows[kSegs], slot[kSegs];
+  int32_t step0[kSegs + 1];  // first tile / step of each, within the launch
+  int count;
+};
+// Slabs: runs of `steps` steps of one slot, over its segments in row order.
+struct Slabs {
+  int32_t slot[kSegs], step0[kSegs + 1], slab0[kSegs + 1];
+  int32_t part0[kSegs];  // first partial sum of a slot of several slabs; -1: one slab, which adds to the output itself
+  int count, steps;
+};
+
+__device__ __forceinline__ int find(const int32_t* first, int count, int v) {
+  int lo = 0, hi = count;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first[mid] <= v) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// How many parts of T an fp32 factor is held in, under a T and an fp32 result.
+template <typename T> struct Parts;
+template <> struct Parts<bf16> { static constexpr int result = 2, exact = 3; };
+template <> struct Parts<float> { static constexpr int result = 1, exact = 1; };
+// The part of x that T holds; x becomes the rest (0 behind an infinity or NaN).
+__device__ __forceinline__ float split(float& x, float*) {
+  const float p = x;
+  x = 0.f;
+  return p;
+}
+__device__ __forceinline__ bf16 split(float& x, bf16*) {
+  const bf16 p = from_f32<bf16>(x);
+  const float f = to_f32(p);
+  x = fabsf(f) < INFINITY ? x - f : 0.f;
+  return p;
+}
+
+// A product over RP ranks with the fp32 factor in NP parts: its reduction runs
+// over NP * RP / 8 chunks of eight slots, part by part.  Step s of 32 slots,
+// lane group g: which part and which eight ranks.
+template <typename T, int RP> struct Up {
+  static constexpr int parts = Parts<T>::result;
+  static constexpr int steps = (parts * RP + 31) / 32;
+  static constexpr int weights = RP < 32 ? 1 : RP / 32;  // different weight fragments of one column
+  static constexpr int stride = parts * RP + 8;          // LDS row of one token
+  __device__ static __forceinline__ int chunk(int s, int g) { return 4 * s + g; }
+  __device__ static __forceinline__ bool live(int s, int g) { return chunk(s, g) < parts * RP / 8; }
+  __device__ static __forceinline__ int rank(int s, int g) { return chunk(s, g) % (RP / 8) * 8; }
+};
+
+template <typename T>
+__device__ __forceinline__ frag_t<T> zero_frag() {
+  Vec8<T> z;
+  z.zero();
+  return z.frag();
+}
+
+// ---------------------------------------------------------------------------
+// Forward
+// ---------------------------------------------------------------------------
+
+// v (or a part of its reduction, part[split][T][r]) of one 64-row tile.
+template <typename T, int RT>
+__global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long ldx, const T* a, int r, int in,
+                                                        float* v, long total_rows) {
+  constexpr int RP = 16 * RT;
+  __shared__ float sh[kWaves][kTile][RP + 1];
+  const int seg = find(t.step0, t.count, blockIdx.x);
+  const int first = (blockIdx.x - t.step0[seg]) * kTile;
+  const int rows = min(kTile, t.rows[seg] - first), slot = t.slot[seg];
+  const long row0 = t.row0[seg] + first;
+  float* out = v + ((long)blockIdx.y * total_rows + row0) * r;
+  if (slot < 0) {
+    for (int i = threadIdx.x; i < rows * r; i += kThreads) out[i] = 0.f;
+    return;
+  }
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  const int tiles = (rows + 15) / 16;
+  const T* as = a + (long)slot * r * in;
+  f32x4 acc[4][RT];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // 32-column steps, dealt to the splits and then to the waves in turn
+  const int nk = (in + 31) / 32, stride = gridDim.y * kWaves;
+  for (int k = blockIdx.y * kWaves + w; k < nk; k += stride) {
+    const int c = 32 * k + 8 * g;
+    Vec8<T> av[RT];
+#pragma unroll
+    for (int j = 0; j < RT; ++j) {
+      if (16 * j + m < r && c < in) av[j].load(as + (long)(16 * j + m) * in + c);
+      else av[j].zero();
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i >= tiles) break;
+      Vec8<T> xv;
+      if (16 * i + m < rows && c < in) xv.load(x + (row0 + 16 * i + m) * ldx + c);
+      else xv.zero();
+#pragma unroll
+      for (int j = 0; j < RT; ++j) acc[i][j] = mma16(xv.frag(), av[j].frag(), acc[i][j]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < RT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sh[w][16 * i + 4 * g + e][16 * j + m] = acc[i][j][e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * r; i += kThreads) {
+    const int row = i / r, c = i - row * r;
+    float s = sh[0][row][c];
+#pragma unroll
+    for (int q = 1; q < kWaves; ++q) s += sh[q][row][c];
+    out[i] = s;
+  }
+}
+
+// y = base + scale v B^T on one 64-row tile and 256 columns; v the sum of
+// `parts` partial reductions (parts > 1: also stored to v_out).
+template <typename T, int RP>
+__global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, int parts, long total_rows,
+                                                      float* v_out, const T* b, int r, int out_features, float scale,
+                                                      const T* base, long ldb, T* y, long ldy) {
+  using U = Up<T, RP>;
+  __shared__ __align__(16) T sh[kTile][U::stride];
+  const int cols = (out_features + kUpCols - 1) / kUpCols;
+  const int tile = blockIdx.x / cols, cb = blockIdx.x - tile * cols;
+  const int seg = find(t.step0, t.count, tile);
+  const int first = (tile - t.step0[seg]) * kTile;
+  const int rows = min(kTile, t.rows[seg] - first), slot = t.slot[seg];
+  const long row0 = t.row0[seg] + first;
+  if (slot < 0 && base == y) return;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  if (slot >= 0) {
+    for (int i = threadIdx.x; i < kTile * RP; i += kThreads) {
+      const int row = i / RP, c = i - row * RP;
+      float s = 0.f;
+      if (row < rows && c < r) {
+        const float* p = v + (row0 + row) * r + c;
+        s = p[0];
+        for (int q = 1; q < parts; ++q) s += p[(long)q * total_rows * r];
+        if (parts > 1 && cb == 0) v_out[(row0 + row) * r + c] = s;
+      }
+#pragma unroll
+      for (int q = 0; q < U::parts; ++q) sh[row][q * RP + c] = split(s, (T*)nullptr);
+    }
+  } else if (parts > 1 && cb == 0) {
+    for (int i = threadIdx.x; i < rows * r; i += kThreads) v_out[row0 * r + i] = 0.f;
+  }
+  __syncthreads();
+  // a wave's 64 columns: column tile q, first-operand row mm is column
+  // 16 (mm / 4) + 4 q + mm % 4, so that a lane's results are 16 neighbours
+  const int c0 = cb * kUpCols + 64 * w;
+  if (c0 >= out_features) return;
+  frag_t<T> wf[4][U::weights];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int col = c0 + 16 * (m >> 2) + 4 * q + (m & 3);
+#pragma unroll
+    for (int s = 0; s < U::weights; ++s) {
+      const int rk = U::rank(s, g);
+      Vec8<T> f;
+      if (slot >= 0 && col < out_features && rk < r) f.load(b + ((long)slot * out_features + col) * r + rk);
+      else f.zero();
+      wf[q][s] = f.frag();
+    }
+  }
+  const int col = c0 + 16 * g;
+#pragma unroll
+  for (int i = 0; i < kTile / 16; ++i) {
+    if (16 * i >= rows) break;
+    const long row = row0 + 16 * i + m;
+    const bool in_row = 16 * i + m < rows;
+    Vec8<T> bs[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (base && in_row && col + 8 * h < out_features) bs[h].load(base + row * ldb + col + 8 * h);
+      else bs[h].zero();
+    }
+    f32x4 acc[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (slot >= 0) {
+#pragma unroll
+      for (int s = 0; s < U::steps; ++s) {
+        Vec8<T> vv;
+        if (U::live(s, g)) vv.load(&sh[16 * i + m][8 * U::chunk(s, g)]);
+        else vv.zero();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[q] = mma16(wf[q][s % U::weights], vv.frag(), acc[q]);
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float o[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = bs[h].get(e) + scale * acc[2 * h + (e >> 2)][e & 3];
+      Vec8<T> ov;
+      ov.set(o);
+      if (in_row && col + 8 * h < out_features) ov.store(y + row * ldy + col + 8 * h);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Backward
+// ---------------------------------------------------------------------------
+
+// Walks the steps of a slab.
+struct Walk {
+  int slot, step, end, seg, part;
+  __device__ __forceinline__ Walk(const Segs& t, const Slabs& sl, int slab) {
+    const int k = find(sl.slab0, sl.count, slab);
+    slot = sl.slot[k];
+    const int i = slab - sl.slab0[k];
+    step = sl.step0[k] + i * sl.steps;
+    end = min(sl.step0[k + 1], step + sl.steps);
+    seg = find(t.step0, t.count, step);
+    part = sl.part0[k] < 0 ? -1 : sl.part0[k] + i;
+  }
+  // The current step's first row and its rows; moves on.
+  __device__ __forceinline__ int next(const Segs& t, long* row0) {
+    while (step >= t.step0[seg + 1]) ++seg;
+    const int first = (step - t.step0[seg]) * kStep;
+    *row0 = t.row0[seg] + first;
+    ++step;
+    return min(kStep, t.rows[seg] - first);
+  }
+};
+
+// LDS rows of a factor [32 tokens][RP] turned to [part][rank][token].
+constexpr int kTokStride = kStep + 8;
+
+// One 32-row x 128-column tile of X in a wave's registers: lane (m, g) holds
+// rows 8g .. 8g + 7 at columns 8m .. 8m + 7.
+template <typename T>
+__device__ __forceinline__ void load_tile(Vec8<T> (&xr)[8], const T* x, long ld, long row0, int rows, int c0, int width,
+                                          int m, int g) {
+  const int c = c0 + 8 * m;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (8 * g + i < rows && c < width) xr[i].load(x + (row0 + 8 * g + i) * ld + c);
+    else xr[i].zero();
+  }
+}
+
+// acc[j][q] += X^T W over the tile's 32 rows: columns 8 m + j, ranks 16 q + n.
+template <typename T, int RT>
+__device__ __forceinline__ void outer(f32x4 (&acc)[8][RT], const Vec8<T> (&xr)[8], const T* wt, int m, int g) {
+  constexpr int NP = Parts<T>::exact;
+  Vec8<T> xt[8];
+  transpose8x8(xr, xt);
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+#pragma unroll
+    for (int q = 0; q < RT; ++q) {
+      Vec8<T> f;
+      f.load(wt + ((long)p * 16 * RT + 16 * q + m) * kTokStride + 8 * g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j][q] = mma16(xt[j].frag(), f.frag(), acc[j][q]);
+    }
+}
+
+// dv parts (one for each column block) and dB (or its slab's part).
+template <typename T, int RT>
+__global__ void __launch_bounds__(kThreads) bwd_out_kernel(Segs t, Slabs sl, const T* dy, long lddy, const T* b,
+                                                           const float* v, int r, int out_features, float scale,
+                                                           float* dv_part, long total_rows, float* db,
+                                                           float* db_part) {
+  constexpr int RP = 16 * RT, NP = Parts<T>::exact;
+  constexpr int kRow = 128 + 16 / (int)sizeof(T);
+  __shared__ __align__(16) T wt[NP * RP * kTokStride];
+  __shared__ __align__(16) T tile[kWaves][kStep][kRow];
+  __shared__ float dvs[kWaves][kStep][RP + 1];
+  const int cols = (out_features + kBwdCols - 1) / kBwdCols;
+  const int slab = blockIdx.x / cols, cb = blockIdx.x - slab * cols;
+  Walk wk(t, sl, slab);
+  if (wk.slot < 0) return;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  const int c0 = cb * kBwdCols + 128 * w;
+  const T* bs = b + (long)wk.slot * out_features * r;
+  // B as the second operand of dv = dy B: rank 16 q + m, columns 32 k + 8 g ..
+  frag_t<T> bf[4][RT];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int q = 0; q < RT; ++q) {
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = c0 + 32 * k + 8 * g + e;
+        f[e] = (c < out_features && 16 * q + m < r) ? to_f32(bs[(long)c * r + 16 * q + m]) : 0.f;
+      }
+      bf[k][q] = pack8(f, (T*)nullptr);
+    }
+  f32x4 acc[8][RT];
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+#pragma unroll
+    for (int q = 0; q < RT; ++q) acc[j][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+  while (wk.step < wk.end) {
+    long row0;
+    const int rows = wk.next(t, &row0);
+    Vec8<T> xr[8];
+    load_tile(xr, dy, lddy, row0, rows, c0, out_features, m, g);
+    for (int i = threadIdx.x; i < kStep * RP; i += kThreads) {
+      const int row = i / RP, c = i - row * RP;
+      float f = row < rows && c < r ? v[(row0 + row) * r + c] : 0.f;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) wt[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) xr[i].store(&tile[w][8 * g + i][8 * m]);
+    __syncthreads();
+    outer<T, RT>(acc, xr, wt, m, g);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      f32x4 d[RT];
+#pragma unroll
+      for (int q = 0; q < RT; ++q) d[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        Vec8<T> f;
+        f.load(&tile[w][16 * h + m][32 * k + 8 * g]);
+#pragma unroll
+        for (int q = 0; q < RT; ++q) d[q] = mma16(f.frag(), bf[k][q], d[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < RT; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dvs[w][16 * h + 4 * g + e][16 * q + m] = d[q][e];
+    }
+    __syncthreads();
+    float* dst = dv_part + ((long)cb * total_rows + row0) * r;
+    for (int i = threadIdx.x; i < rows * r; i += kThreads) {
+      const int row = i / r, c = i - row * r;
+      float s = dvs[0][row][c];
+#pragma unroll
+      for (int q = 1; q < kWaves; ++q) s += dvs[q][row][c];
+      dst[i] = scale * s;
+    }
+  }
+  const bool add = wk.part < 0;
+  float* dst = add ? db + (long)wk.slot * out_features * r : db_part + (long)wk.part * out_features * r;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int c = c0 + 8 * (4 * g + e) + j;
+      if (c >= out_features) continue;
+#pragma unroll
+      for (int q = 0; q < RT; ++q) {
+        const int k = 16 * q + m;
+        if (k >= r) continue;
+        float* p = dst + (long)c * r + k;
+        *p = (add ? *p : 0.f) + scale * acc[j][q][e];
+      }
+    }
+}
+
+// dx and dA (or its slab's part); dv: the sum of `parts` column blocks' parts.
+template <typename T, int RT>
+__global__ void __launch_bounds__(kThreads) bwd_in_kernel(Segs t, Slabs sl, const T* x, long ldx, const T* a,
+                                                          const float* dv_part, int parts, long total_rows, int r,
+                                                          int in, const T* dres, long lddr, T* dx, long lddx,
+                                                          float* da, float* da_part) {
+  constexpr int RP = 16 * RT, NP = Parts<T>::exact;
+  using U = Up<T, RP>;
+  __shared__ __align__(16) T wt[NP * RP * kTokStride];
+  __shared__ __align__(16) T wr[kStep][U::stride];
+  const int cols = (in + kBwdCols - 1) / kBwdCols;
+  const int slab = blockIdx.x / cols, cb = blockIdx.x - slab * cols;
+  Walk wk(t, sl, slab);
+  const int slot = wk.slot;
+  const bool live = slot >= 0;
+  if (!live && (!dx || dx == dres)) return;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  const int c0 = cb * kBwdCols + 128 * w;
+  // A as the first operand of dx = dv A, columns as in `up`
+  frag_t<T> wf[2][4][U::weights];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int col = c0 + 64 * h + 16 * (m >> 2) + 4 * q + (m & 3);
+#pragma unroll
+      for (int s = 0; s < U::weights; ++s) {
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int rk = U::rank(s, g) + e;
+          f[e] = live && dx && col < in && rk < r ? to_f32(a[((long)slot * r + rk) * in + col]) : 0.f;
+        }
+        wf[h][q][s] = pack8(f, (T*)nullptr);
+      }
+    }
+  f32x4 acc[8][RT];
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+#pragma unroll
+    for (int q = 0; q < RT; ++q) acc[j][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+  while (wk.step < wk.end) {
+    long row0;
+    const int rows = wk.next(t, &row0);
+    if (live) {
+      Vec8<T> xr[8];
+      load_tile(xr, x, ldx, row0, rows, c0, in, m, g);
+      __syncthreads();  // the step before has read wt and wr
+      for (int i = threadIdx.x; i < kStep * RP; i += kThreads) {
+        const int row = i / RP, c = i - row * RP;
+        float f = 0.f;
+        if (row < rows && c < r) {
+          const float* p = dv_part + (row0 + row) * r + c;
+          f = p[0];
+          for (int q = 1; q < parts; ++q) f += p[(long)q * total_rows * r];
+        }
+        float f2 = f;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) wt[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
+#pragma unroll
+        for (int p = 0; p < U::parts; ++p) wr[row][p * RP + c] = split(f2, (T*)nullptr);
+      }
+      __syncthreads();
+      outer<T, RT>(acc, xr, wt, m, g);
+    }
+    if (!dx) continue;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int col = c0 + 64 * h + 16 * g;
+        const long row = row0 + 16 * i + m;
+        const bool in_row = 16 * i + m < rows;
+        Vec8<T> bs[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          if (dres && in_row && col + 8 * u < in) bs[u].load(dres + row * lddr + col + 8 * u);
+          else bs[u].zero();
+        }
+        f32x4 d[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) d[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (live) {
+#pragma unroll
+          for (int s = 0; s < U::steps; ++s) {
+            Vec8<T> f;
+            if (U::live(s, g)) f.load(&wr[16 * i + m][8 * U::chunk(s, g)]);
+            else f.zero();
+#pragma unroll
+            for (int q = 0; q < 4; ++q) d[q] = mma16(wf[h][q][s % U::weights], f.frag(), d[q]);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float o[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] = bs[u].get(e) + d[2 * u + (e >> 2)][e & 3];
+          Vec8<T> ov;
+          ov.set(o);
+          if (in_row && col + 8 * u < in) ov.store(dx + row * lddx + col + 8 * u);
+        }
+      }
+  }
+  if (!live) return;
+  const bool add = wk.part < 0;
+  float* dst = add ? da + (long)slot * r * in : da_part + (long)wk.part * r * in;
+#pragma unroll
+  for (int q = 0; q < RT; ++q) {
+    const int k = 16 * q + m;
+    if (k >= r) continue;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int c = c0 + 8 * (4 * g + e);
+      if (c >= in) continue;
+      Vec8<float> o;
+      float s[8];
+      float* p = dst + (long)k * in + c;
+      if (add) o.load(p);
+      else o.zero();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] = o.get(j) + acc[j][q][e];
+      o.set(s);
+      o.store(p);
+    }
+  }
+}
+
+// out[slot] += the parts of its slabs, in order; n elements a slot.  blockIdx.y:
+// the slot's place in the table; .z: dA or dB.
+__global__ void __launch_bounds__(kThreads) join_kernel(Slabs sl, const float* part_a, float* da, long na,
+                                                        const float* part_b, float* db, long nb) {
+  const int k = blockIdx.y, slot = sl.slot[k], p0 = sl.part0[k];
+  if (slot < 0 || p0 < 0) return;
+  const int count = sl.slab0[k + 1] - sl.slab0[k];
+  const bool is_b = blockIdx.z;
+  const long n = is_b ? nb : na, e = ((long)blockIdx.x * kThreads + threadIdx.x) * 4;
+  if (e >= n) return;
+  const float* src = (is_b ? part_b : part_a) + p0 * n + e;
+  float* dst = (is_b ? db : da) + slot * n + e;
+  Vec4<float> o;
+  o.load(dst);
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < count; ++i) {
+    Vec4<float> f;
+    f.load(src + i * n);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[j] += f.get(j);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s[j] += o.get(j);
+  o.set(s);
+  o.store(dst);
+}
+
+// ---------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------
+
+bool al16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  if (!a || !b || !na || !nb) return false;
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + nb && y < x + na;
+}
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+int launch_status() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? FL_OK : set_error(FL_ERR_HIP, hipGetErrorString(e));
+}
+long cdiv(long a, long b) { return (a + b - 1) / b; }
+
+struct Run {
+  int row0, rows, slot;
+};
+// Runs of rows with one slot, in row order (adjacent clients of one slot make
+// one run); by_slot: sorted by slot, rows in order within it.
+int runs_of(const fl_batch_desc* b, const int32_t* client_adapter, bool by_slot, std::vector<Run>* out) {
+  try {
+    out->reserve(b->num_clients);
+    for (int c = 0; c < b->num_clients; ++c) {
+      const int r0 = b->cu_seqlens[b->client_seq_ptr[c]], r1 = b->cu_seqlens[b->client_seq_ptr[c + 1]];
+      if (!out->empty() && out->back().slot == client_adapter[c]) out->back().rows += r1 - r0;
+      else out->push_back({r0, r1 - r0, client_adapter[c]});
+    }
+    if (by_slot) {
+      std::sort(out->begin(), out->end(),
+                [](const Run& x, const Run& y) { return x.slot != y.slot ? x.slot < y.slot : x.row0 < y.row0; });
+    }
+  } catch (const std::bad_alloc&) {
+    return set_error(FL_ERR_NOMEM, "out of host memory for the table of clients");
+  }
+  return FL_OK;
+}
+
+// The next launch's segments from runs[i] on.
+void fill(const std::vector<Run>& runs, size_t* i, int rows_a_step, Segs* t) {
+  t->count = 0;
+  int32_t steps = 0;
+  for (; *i < runs.size() && t->count < kSegs; ++*i) {
+    const Run& q = runs[*i];
+    t->row0[t->count] = q.row0;
+    t->rows[t->count] = q.rows;
+    t->slot[t->count] = q.slot;
+    t->step0[t->count++] = steps;
+    steps += (int32_t)cdiv(q.rows, rows_a_step);
+  }
+  t->step0[t->count] = steps;
+}
+
+// Forward: workgroups along the reduction of v, for batches whose tiles alone
+// do not fill the chip; every wave has two steps at least.
+int splits_of(const fl_adapter_desc* d, const fl_batch_desc* b) {
+  const long tiles = b->total_tokens / kTile + b->num_clients;
+  return (int)std::max(1L, std::min<long>({512 / tiles, d->in_features / (32 * kWaves * 2), 16}));
+}
+// Backward: steps of a slab.  Long slabs mean few partial sums of dA and dB,
+// short ones many workgroups.
+int slab_steps(const fl_adapter_desc* d, const fl_batch_desc* b) {
+  const long steps = b->total_tokens / kStep + b->num_clients;
+  const long cols = cdiv(std::max(d->in_features, d->out_features), kBwdCols);
+  return (int)std::min(128L, std::max(4L, cdiv(steps * cols, 1024)));
+}
+
+struct AdapterWs {
+  float* v_part;   // forward: [splits][T][r]
+  float* dv_part;  // backward: [column blocks of out][T][r]
+  float *da_part, *db_part;
+  size_t total;
+};
+AdapterWs carve(const fl_adapter_desc* d, const fl_batch_desc* b, char* base) {
+  AdapterWs w;
+  size_t off = 0;
+  auto take = [&](size_t n) {
+    float* p = base ? (float*)(base + off) : nullptr;
+    off = align256(off + n);
+    return p;
+  };
+  const size_t v = (size_t)b->total_tokens * d->rank * 4;
+  const int splits = splits_of(d, b);
+  w.v_part = take(splits > 1 ? splits * v : 0);
+  const size_t fwd = off;
+  off = 0;
+  w.dv_part = take(cdiv(d->out_features, kBwdCols) * v);
+  // slots of several slabs have fewer than two slabs for each full one
+  const size_t slabs = 2 * (b->total_tokens / kStep + b->num_clients) / slab_steps(d, b) + 2;
+  w.da_part = take(slabs * d->rank * d->in_features * 4);
+  w.db_part = take(slabs * d->rank * d->out_features * 4);
+  w.total = std::max(std::max(fwd, off), (size_t)256);
+  return w;
+}
+
+int check_desc(const fl_adapter_desc* d) {
+  if (!d) return set_error(FL_ERR_NULL, "adapter descriptor is NULL");
+  if (d->dtype != FL_BF16 && d->dtype != FL_F32) return set_error(FL_ERR_SHAPE, "dtype must be bf16 or fp32");
+  if (d->num_adapters < 1 || d->num_adapters > (1 << 16))
+    return set_error(FL_ERR_SHAPE, "num_adapters must be in [1, 2^16]");
+  if (d->rank < 8 || d->rank > 64 || d->rank % 8) return set_error(FL_ERR_SHAPE, "rank must be a multiple of 8 in [8, 64]");
+  for (int n : {d->in_features, d->out_features})
+    if (n < 8 || n % 8 || n > 65536) return set_error(FL_ERR_SHAPE, "features must be multiples of 8 in [8, 65536]");
+  if (!std::isfinite(d->scale)) return set_error(FL_ERR_ARG, "scale is not finite");
+  return FL_OK;
+}
+// One [T, ld] operand of `width` columns.
+struct Mat {
+  const void* p;
+  int64_t ld;
+  int width;
+  size_t bytes(size_t T, size_t E) const { return p ? ((T - 1) * ld + width) * E : 0; }
+};
+// Whether two operands share an element: column ranges of one wider buffer
+// (equal row strides, no row of one reaching into the other's columns) do not.
+bool overlap(const Mat& a, const Mat& b, size_t T, size_t E) {
+  if (!overlap(a.p, a.bytes(T, E), b.p, b.bytes(T, E))) return false;
+  if (a.ld != b.ld) return true;
+  const size_t ld = (size_t)a.ld * E;
+  const size_t off = ((uintptr_t)b.p % ld + ld - (uintptr_t)a.p % ld) % ld;  // b's first column behind a's
+  return off < a.width * E || off + b.width * E > ld;
+}
+int check_mat(const Mat& m, bool required) {
+  if (!m.p) return required ? set_error(FL_ERR_NULL, "a matrix argument is NULL") : FL_OK;
+  if (!al16(m.p)) return set_error(FL_ERR_ALIGN, "a matrix argument is not 16-byte aligned");
+  if (m.ld < m.width || m.ld % 8 || m.ld > (int64_t(1) << 32))
+    return set_error(FL_ERR_SHAPE, "a row stride must be a multiple of 8, at least the row's width and at most 2^32");
+  return FL_OK;
+}
+
+// Calls f.template operator()<T, RT>() for the call's type and rank.
+template <typename F>
+int dispatch(const fl_adapter_desc* d, F&& f) {
+  const int rt = d->rank <= 16 ? 1 : d->rank <= 32 ? 2 : 4;
+  if (d->dtype == FL_BF16) {
+    if (rt == 1) return f((bf16*)nullptr, std::integral_constant<int, 1>());
+    if (rt == 2) return f((bf16*)nullptr, std::integral_constant<int, 2>());
+    return f((bf16*)nullptr, std::integral_constant<int, 4>());
+  }
+  if (rt == 1) return f((float*)nullptr, std::integral_constant<int, 1>());
+  if (rt == 2) return f((float*)nullptr, std::integral_constant<int, 2>());
+  return f((float*)nullptr, std::integral_constant<int, 4>());
+}
+
+}  // namespace
+
+namespace flglm {
+
+int adapter_check(const fl_adapter_desc* d, const fl_batch_desc* b, const int32_t* client_adapter, const void* ws,
+                  size_t ws_bytes) {
+  if (int rc = check_desc(d)) return rc;
+  if (int rc = check_batch(b)) return rc;
+  if (!client_adapter || !ws) return set_error(FL_ERR_NULL, "client_adapter / workspace is NULL");
+  for (int c = 0; c < b->num_clients; ++c)
+    if (client_adapter[c] < -1 || client_adapter[c] >= d->num_adapters)
+      return set_error(FL_ERR_ARG, "a client's adapter is outside [-1, num_adapters)");
+  if (!al16(ws)) return set_error(FL_ERR_ALIGN, "workspace is not 16-byte aligned");
+  if (ws_bytes < carve(d, b, nullptr).total) return set_error(FL_ERR_WORKSPACE, "workspace too small");
+  return FL_OK;
+}
+int adapter_workspace_bytes(const fl_adapter_desc* d, const fl_batch_desc* b, size_t* bytes) {
+  if (int rc = check_desc(d)) return rc;
+  if (int rc = check_batch(b)) return rc;
+  *bytes = carve(d, b, nullptr).total;
+  return FL_OK;
+}
+
+int adapter_forward(const fl_adapter_desc* d, const fl_batch_desc* batch, const int32_t* client_adapter, const void* x,
+                    int64_t ldx, const void* a, const void* b, const void* base, int64_t ld_base, void* y, int64_t ldy,
+                    float* v, void* ws, hipStream_t s) {
+  std::vector<Run> runs;
+  if (int rc = runs_of(batch, client_adapter, false, &runs)) return rc;
+  const AdapterWs w = carve(d, batch, (char*)ws);
+  const int splits = splits_of(d, batch);
+  const long T = batch->total_tokens;
+  const long cols = cdiv(d->out_features, kUpCols);
+  for (size_t i = 0; i < runs.size();) {
+    Segs t;
+    fill(runs, &i, kTile, &t);
+    const int rc = dispatch(d, [&](auto* type, auto rt) {
+      using E = std::remove_pointer_t<decltype(type)>;
+      constexpr int RT = decltype(rt)::value;
+      hipLaunchKernelGGL((down_kernel<E, RT>), dim3(t.step0[t.count], splits), dim3(kThreads), 0, s, t, (const E*)x,
+                         ldx, (const E*)a, d->rank, d->in_features, splits > 1 ? w.v_part : v, T);
+      if (int e = launch_status()) return e;
+      hipLaunchKernelGGL((up_kernel<E, 16 * RT>), dim3((unsigned)(t.step0[t.count] * cols)), dim3(kThreads), 0, s, t,
+                         splits > 1 ? w.v_part : v, splits, T, v, (const E*)b, d->rank, d->out_features, d->scale,
+                         (const E*)base, ld_base, (E*)y, ldy);
+      return launch_status();
+    });
+    if (rc) return rc;
+  }
+  return FL_OK;
+}
+
+int adapter_backward(const fl_adapter_desc* d, const fl_batch_desc* batch, const int32_t* client_adapter,
+                     const void* dy, int64_t ld_dy, const void* x, int64_t ldx, const void* a, const void* b,
+                     const float* v, const void* dres, int64_t ld_dres, void* dx, int64_t ld_dx, float* da, float* db,
+                     void* ws, hipStream_t s) {
+  std::vector<Run> runs;
+  if (int rc = runs_of(batch, client_adapter, true, &runs)) return rc;
+  const AdapterWs w = carve(d, batch, (char*)ws);
+  const long T = batch->total_tokens;
+  const int steps = slab_steps(d, batch);
+  const long na = (long)d->rank * d->in_features, nb = (long)d->rank * d->out_features;
+  const long cols_in = cdiv(d->in_features, kBwdCols), cols_out = cdiv(d->out_features, kBwdCols);
+  for (size_t i = 0; i < runs.size();) {
+    Segs t;
+    fill(runs, &i, kStep, &t);
+    Slabs sl;
+    sl.count = 0;
+    sl.steps = steps;
+    int32_t slabs = 0, parts = 0;
+    for (int k = 0; k < t.count; ++k) {
+      if (k && t.slot[k] == t.slot[k - 1]) continue;
+      int last = k;
+      while (last + 1 < t.count && t.slot[last + 1] == t.slot[k]) ++last;
+      const int n = (int)cdiv(t.step0[last + 1] - t.step0[k], steps);
+      sl.slot[sl.count] = t.slot[k];
+      sl.step0[sl.count] = t.step0[k];
+      sl.slab0[sl.count] = slabs;
+      sl.part0[sl.count++] = n > 1 && t.slot[k] >= 0 ? parts : -1;
+      slabs += n;
+      if (n > 1 && t.slot[k] >= 0) parts += n;
+    }
+    sl.slab0[sl.count] = slabs;
+    sl.step0[sl.count] = t.step0[t.count];
+    const int rc = dispatch(d, [&](auto* type, auto rt) {
+      using E = std::remove_pointer_t<decltype(type)>;
+      constexpr int RT = decltype(rt)::value;
+      hipLaunchKernelGGL((bwd_out_kernel<E, RT>), dim3((unsigned)(slabs * cols_out)), dim3(kThreads), 0, s, t, sl,
+                         (const E*)dy, ld_dy, (const E*)b, v, d->rank, d->out_features, d->scale, w.dv_part, T, db,
+                         w.db_part);
+      if (int e = launch_status()) return e;
+      hipLaunchKernelGGL((bwd_in_kernel<E, RT>), dim3((unsigned)(slabs * cols_in)), dim3(kThreads), 0, s, t, sl,
+                         (const E*)x, ldx, (const E*)a, w.dv_part, (int)cols_out, T, d->rank, d->in_features,
+                         (const E*)dres, ld_dres, (E*)dx, ld_dx, da, w.da_part);
+      return launch_status();
+    });
+    if (rc) return rc;
+    if (parts) {
+      hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(std::max(na, nb), 4 * kThreads), sl.count, 2), dim3(kThreads),
+                         0, s, sl, w.da_part, da, na, w.db_part, db, nb);
+      if (int e = launch_status()) return e;
+    }
+  }
+  return FL_OK;
+}
+
+}  // namespace flglm
+
+extern "C" {
+
+int fl_adapter_workspace_bytes(const fl_adapter_desc* desc, const fl_batch_desc* batch, size_t* bytes) {
+  if (!bytes) return set_error(FL_ERR_NULL, "bytes is NULL");
+  return adapter_workspace_bytes(desc, batch, bytes);
+}
+
+int fl_adapter_forward(const fl_adapter_desc* desc, const fl_batch_desc* batch, const int32_t* client_adapter,
+                       const void* x, int64_t ldx, const void* a, const void* b, const void* base, int64_t ld_base,
+                       void* y, int64_t ldy, float* v, void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = adapter_check(desc, batch, client_adapter, workspace, workspace_bytes)) return rc;
+  const int in = desc->in_features, out = desc->out_features;
+  const Mat mx{x, ldx, in}, mb{base, ld_base, out}, my{y, ldy, out};
+  if (int rc = check_mat(mx, true)) return rc;
+  if (int rc = check_mat(my, true)) return rc;
+  if (int rc = check_mat(mb, false)) return rc;
+  if (!a || !b || !v) return set_error(FL_ERR_NULL, "a / b / v is NULL");
+  if (!al16(a) || !al16(b) || !al16(v)) return set_error(FL_ERR_ALIGN, "a / b / v not 16-byte aligned");
+  const size_t T = batch->total_tokens, E = desc->dtype == FL_BF16 ? 2 : 4, n = desc->num_adapters;
+  const size_t na = n * desc->rank * in * E, nb = n * desc->rank * out * E, nv = T * desc->rank * 4;
+  if (overlap(my, mb, T, E) && !(y == base && ldy == ld_base))
+    return set_error(FL_ERR_ALIAS, "y overlaps base without being it");
+  if (overlap(my, mx, T, E)) return set_error(FL_ERR_ALIAS, "y overlaps x");
+  const void* p[7] = {x, base, y, a, b, v, workspace};
+  const size_t len[7] = {mx.bytes(T, E), mb.bytes(T, E), my.bytes(T, E), na, nb, nv, workspace_bytes};
+  for (int i = 0; i < 7; ++i)
+    for (int j = std::max(i + 1, 3); j < 7; ++j)  // a and b may share memory with x and base, all being read
+      if ((j >= 5 || i == 2) && overlap(p[i], len[i], p[j], len[j]))
+        return set_error(FL_ERR_ALIAS, "y, v or the workspace overlaps another argument");
+  return adapter_forward(desc, batch, client_adapter, x, ldx, a, b, base, ld_base, y, ldy, v, workspace,
+                         (hipStream_t)stream);
+}
+
+int fl_adapter_backward(const fl_adapter_desc* desc, const fl_batch_desc* batch, const int32_t* client_adapter,
+                        const void* dy, int64_t ld_dy, const void* x, int64_t ldx, const void* a, const void* b,
+                        const float* v, const void* dres, int64_t ld_dres, void* dx, int64_t ld_dx, float* da,
+                        float* db, void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = adapter_check(desc, batch, client_adapter, workspace, workspace_bytes)) return rc;
+  const int in = desc->in_features, out = desc->out_features;
+  const Mat mdy{dy, ld_dy, out}, mx{x, ldx, in}, mr{dres, ld_dres, in}, mdx{dx, ld_dx, in};
+  if (int rc = check_mat(mdy, true)) return rc;
+  if (int rc = check_mat(mx, true)) return rc;
+  if (int rc = check_mat(mr, false)) return rc;
+  if (int rc = check_mat(mdx, false)) return rc;
+  if (dres && !dx) return set_error(FL_ERR_NULL, "dres without dx");
+  if (!a || !b || !v || !da || !db) return set_error(FL_ERR_NULL, "a / b / v / da / db is NULL");
+  if (!al16(a) || !al16(b) || !al16(v) || !al16(da) || !al16(db))
+    return set_error(FL_ERR_ALIGN, "a / b / v / da / db not 16-byte aligned");
+  const size_t T = batch->total_tokens, E = desc->dtype == FL_BF16 ? 2 : 4, n = desc->num_adapters;
+  const size_t na = n * desc->rank * in, nb = n * desc->rank * out;
+  if (overlap(mdx, mr, T, E) && !(dx == dres && ld_dx == ld_dres))
+    return set_error(FL_ERR_ALIAS, "dx overlaps dres without being it");
+  if (overlap(mdx, mx, T, E) || overlap(mdx, mdy, T, E)) return set_error(FL_ERR_ALIAS, "dx overlaps x or dy");
+  const void* p[10] = {dy, x, dres, dx, a, b, v, da, db, workspace};
+  const size_t len[10] = {mdy.bytes(T, E), mx.bytes(T, E), mr.bytes(T, E), mdx.bytes(T, E), na * E, nb * E,
+                          T * desc->rank * 4, na * 4, nb * 4, workspace_bytes};
+  for (int i = 0; i < 10; ++i)
+    for (int j = std::max(i + 1, 4); j < 10; ++j)  // what is only read may share memory
+      if ((j >= 7 || i == 3) && overlap(p[i], len[i], p[j], len[j]))
+        return set_error(FL_ERR_ALIAS, "dx, da, db or the workspace overlaps another argument");
+  return adapter_backward(desc, batch, client_adapter, dy, ld_dy, x, ldx, a, b, v, dres, ld_dres, dx, ld_dx, da, db,
+                          workspace, (hipStream_t)stream);
+}
+
+}  // extern "C"

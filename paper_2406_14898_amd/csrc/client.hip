@@ -30,10 +30,6 @@
 #include "common.h"
 #include "kernels.h"
 
-namespace flglm {
-int set_error(int code, const char* msg);
-}
-
 using namespace flglm;
 
 struct fl_client {
@@ -286,6 +282,107 @@ int check_common(const fl_client* c, long T, void* ws, size_t ws_bytes) {
   return FL_OK;
 }
 
+// The final LayerNorm's arguments: both or neither, hidden <= 4096, eps > 0.
+int check_final_ln(const fl_client* c, const void* g, const void* b) {
+  if (!g && !b) return FL_OK;
+  if (!g || !b) return set_error(FL_ERR_NULL, "final LayerNorm gain / shift: both or neither");
+  if (!al16(g) || !al16(b)) return set_error(FL_ERR_ALIGN, "final LayerNorm parameters not 16-byte aligned");
+  if (c->d.hidden > 4096) return set_error(FL_ERR_SHAPE, "the final LayerNorm supports hidden <= 4096");
+  if (!(c->d.ln_eps > 0.f)) return set_error(FL_ERR_SHAPE, "the final LayerNorm needs ln_eps > 0");
+  return FL_OK;
+}
+
+int check_labels(const fl_client* c, const int32_t* labels, long T) {
+  for (long t = 0; t < T; ++t)
+    if (labels[t] >= c->d.vocab) return set_error(FL_ERR_ARG, "a label is >= vocab");
+  return FL_OK;
+}
+
+// Labels to the device, then the logits of [the final LayerNorm and] the
+// linear layer into the workspace.
+int head_logits(fl_client* c, const ClientWs& w, const void* h, const void* ln_g, const void* ln_b,
+                const void* w_vocab, const int32_t* labels, long T, hipStream_t s) {
+  if (int rc = upload(c, labels, (size_t)T * 4, w.labels, s)) return rc;
+  const int H = c->d.hidden;
+  const void* hin = h;
+  if (ln_g) {
+    CK(layernorm_fwd(dt_of(c), h, ln_g, ln_b, w.hn, w.mean, w.rstd, (int)T, H, c->d.ln_eps, s));
+    hin = w.hn;
+  }
+  GemmDesc g;
+  g.A = hin; g.B = w_vocab; g.C = w.logits;
+  g.M = (int)T; g.N = (int)c->vpad; g.K = H;
+  g.lda = H; g.ldb = H; g.ldc = c->vpad;
+  g.b_rows = (int)c->d.vocab;
+  g.part = w.part; g.part_bytes = w.part_bytes;
+  return herr(gemm(dt_of(c), GEMM_NT, EPI_STORE, g, s));
+}
+
+int check_head_backward(const fl_client* c, const void* h, const void* ln_g, const void* w_vocab, long T,
+                        float grad_scale, const void* dh, const float* dln_g, const float* dln_b,
+                        const float* dw_vocab, const void* workspace, size_t workspace_bytes) {
+  if (!h || !w_vocab || !dh) return set_error(FL_ERR_NULL, "h / w / dh is NULL");
+  if (ln_g && (!al16(ln_g) || c->d.hidden > 4096 || !(c->d.ln_eps > 0.f)))
+    return set_error(FL_ERR_ARG, "final LayerNorm gain misaligned, or hidden / ln_eps unsupported");
+  if (!ln_g && (dln_g || dln_b)) return set_error(FL_ERR_ARG, "LayerNorm gradients without a final LayerNorm");
+  if ((dln_g == nullptr) != (dln_b == nullptr)) return set_error(FL_ERR_NULL, "dln_g / dln_b: both or neither");
+  if ((dln_g && !al16(dln_g)) || (dln_b && !al16(dln_b))) return set_error(FL_ERR_ALIGN, "dln not aligned");
+  if (!al16(h) || !al16(w_vocab) || !al16(dh) || (dw_vocab && !al16(dw_vocab)))
+    return set_error(FL_ERR_ALIGN, "h / w / dh / dw not 16-byte aligned");
+  if (!std::isfinite(grad_scale)) return set_error(FL_ERR_ARG, "grad_scale is not finite");
+  const long V = c->d.vocab, H = c->d.hidden;
+  if (overlap(dh, T * H * c->E, h, T * H * c->E) || overlap(dh, T * H * c->E, workspace, workspace_bytes))
+    return set_error(FL_ERR_ALIAS, "dh overlaps h / the workspace");
+  if (dw_vocab && (overlap(dw_vocab, V * H * 4, workspace, workspace_bytes) ||
+                   overlap(dw_vocab, V * H * 4, dh, T * H * c->E)))
+    return set_error(FL_ERR_ALIAS, "dw overlaps dh / the workspace");
+  return FL_OK;
+}
+
+// From the logits' gradient, which the workspace holds in their place, to the
+// gradients of h, the weight and the final LayerNorm.
+int head_gradients(const fl_client* c, const ClientWs& w, const void* h, const void* ln_g, const void* w_vocab,
+                   long T, void* dh, float* dln_g, float* dln_b, float* dw_vocab, hipStream_t s) {
+  const long V = c->d.vocab, H = c->d.hidden;
+  // dh = dlogits W   (reduction over the padded vocabulary; W's rows past V
+  // read as zero); with the final LayerNorm this is the gradient at its output
+  GemmDesc g;
+  g.A = w.logits; g.B = w_vocab; g.C = ln_g ? (void*)w.dhn : dh;
+  g.M = (int)T; g.N = (int)H; g.K = (int)c->vpad;
+  g.lda = c->vpad; g.ldb = H; g.ldc = H;
+  g.b_rows = (int)V;
+  g.part = w.part; g.part_bytes = w.part_bytes;
+  CK(gemm(dt_of(c), GEMM_NN, EPI_STORE, g, s));
+  if (ln_g) {
+    CK(layernorm_bwd_dx(dt_of(c), w.dhn, h, w.mean, w.rstd, ln_g, nullptr, dh, (int)T, (int)H, s));
+    if (dln_g) {
+      const int nb = colsum_blocks((int)T);
+      CK(colsum_partial(dt_of(c), 1, w.dhn, H, h, w.mean, w.rstd, (int)T, (int)H, w.ln_part, w.ln_part2, s));
+      const ColsumJob jobs[2] = {{w.ln_part, dln_g, nb, (int)H}, {w.ln_part2, dln_b, nb, (int)H}};
+      CK(colsum_finish_n(jobs, 2, s));
+    }
+  }
+  if (!dw_vocab) return FL_OK;
+  // dW += dlogits^T hn   (rows m < V of the padded logits' columns; hn = h
+  // without the final LayerNorm)
+  GemmDesc gw;
+  gw.A = w.logits; gw.B = ln_g ? (const void*)w.hn : h; gw.C = dw_vocab;
+  gw.M = (int)V; gw.N = (int)H; gw.K = (int)T;
+  gw.lda = c->vpad; gw.ldb = H; gw.ldc = H;
+  gw.part = w.part; gw.part_bytes = w.part_bytes;
+  CK(gemm(dt_of(c), GEMM_TN, EPI_ACC_F32, gw, s));
+  return FL_OK;
+}
+
+// The loss's descriptor is of the client's own logits.
+int check_preference_head(const fl_client* c, const fl_preference_desc* pref, const fl_batch_desc* batch) {
+  if (!c) return set_error(FL_ERR_NULL, "client handle is NULL");
+  if (!pref) return set_error(FL_ERR_NULL, "preference descriptor is NULL");
+  if (pref->vocab != c->d.vocab || pref->dtype != c->d.dtype)
+    return set_error(FL_ERR_SHAPE, "the preference descriptor's vocab / dtype are not the client's");
+  return check_batch(batch);
+}
+
 }  // namespace
 
 extern "C" {
@@ -392,16 +489,6 @@ int fl_embedding_backward(fl_client* c, const int32_t* ids, int64_t T, const voi
   return herr(hipGetLastError());
 }
 
-// The final LayerNorm's arguments: both or neither, hidden <= 4096, eps > 0.
-int check_final_ln(const fl_client* c, const void* g, const void* b) {
-  if (!g && !b) return FL_OK;
-  if (!g || !b) return set_error(FL_ERR_NULL, "final LayerNorm gain / shift: both or neither");
-  if (!al16(g) || !al16(b)) return set_error(FL_ERR_ALIGN, "final LayerNorm parameters not 16-byte aligned");
-  if (c->d.hidden > 4096) return set_error(FL_ERR_SHAPE, "the final LayerNorm supports hidden <= 4096");
-  if (!(c->d.ln_eps > 0.f)) return set_error(FL_ERR_SHAPE, "the final LayerNorm needs ln_eps > 0");
-  return FL_OK;
-}
-
 int fl_lm_head_forward(fl_client* c, const void* h, const void* ln_g, const void* ln_b, const void* w_vocab,
                        const int32_t* labels, int64_t T, float* loss_tok, float* loss_sum, void* workspace,
                        size_t workspace_bytes, void* stream) {
@@ -413,24 +500,10 @@ int fl_lm_head_forward(fl_client* c, const void* h, const void* ln_g, const void
   if (overlap(loss_tok, T * 4, workspace, workspace_bytes) || overlap(loss_sum, 4, workspace, workspace_bytes) ||
       overlap(loss_tok, T * 4, loss_sum, 4))
     return set_error(FL_ERR_ALIAS, "loss outputs overlap each other or the workspace");
-  for (long t = 0; t < T; ++t)
-    if (labels[t] >= c->d.vocab) return set_error(FL_ERR_ARG, "a label is >= vocab");
+  if (int rc = check_labels(c, labels, T)) return rc;
   const ClientWs w = carve(c, T, (char*)workspace);
   hipStream_t s = (hipStream_t)stream;
-  if (int rc = upload(c, labels, (size_t)T * 4, w.labels, s)) return rc;
-  const int H = c->d.hidden;
-  const void* hin = h;
-  if (ln_g) {
-    CK(layernorm_fwd(dt_of(c), h, ln_g, ln_b, w.hn, w.mean, w.rstd, (int)T, H, c->d.ln_eps, s));
-    hin = w.hn;
-  }
-  GemmDesc g;
-  g.A = hin; g.B = w_vocab; g.C = w.logits;
-  g.M = (int)T; g.N = (int)c->vpad; g.K = H;
-  g.lda = H; g.ldb = H; g.ldc = c->vpad;
-  g.b_rows = (int)c->d.vocab;
-  g.part = w.part; g.part_bytes = w.part_bytes;
-  CK(gemm(dt_of(c), GEMM_NT, EPI_STORE, g, s));
+  if (int rc = head_logits(c, w, h, ln_g, ln_b, w_vocab, labels, T, s)) return rc;
   if (c->d.dtype == FL_BF16)
     hipLaunchKernelGGL(ce_fwd_kernel<bf16>, dim3((unsigned)T), dim3(kThreads), 0, s, (const bf16*)w.logits,
                        c->vpad, (int)c->d.vocab, w.labels, w.lse, loss_tok);
@@ -446,58 +519,69 @@ int fl_lm_head_backward(fl_client* c, const void* h, const void* ln_g, const voi
                         float grad_scale, void* dh, float* dln_g, float* dln_b, float* dw_vocab, void* workspace,
                         size_t workspace_bytes, void* stream) {
   if (int rc = check_common(c, T, workspace, workspace_bytes)) return rc;
-  if (!h || !w_vocab || !dh) return set_error(FL_ERR_NULL, "h / w / dh is NULL");
-  if (ln_g && (!al16(ln_g) || c->d.hidden > 4096 || !(c->d.ln_eps > 0.f)))
-    return set_error(FL_ERR_ARG, "final LayerNorm gain misaligned, or hidden / ln_eps unsupported");
-  if (!ln_g && (dln_g || dln_b)) return set_error(FL_ERR_ARG, "LayerNorm gradients without a final LayerNorm");
-  if ((dln_g == nullptr) != (dln_b == nullptr)) return set_error(FL_ERR_NULL, "dln_g / dln_b: both or neither");
-  if ((dln_g && !al16(dln_g)) || (dln_b && !al16(dln_b))) return set_error(FL_ERR_ALIGN, "dln not aligned");
-  if (!al16(h) || !al16(w_vocab) || !al16(dh) || (dw_vocab && !al16(dw_vocab)))
-    return set_error(FL_ERR_ALIGN, "h / w / dh / dw not 16-byte aligned");
-  if (!std::isfinite(grad_scale)) return set_error(FL_ERR_ARG, "grad_scale is not finite");
-  const long V = c->d.vocab, H = c->d.hidden;
-  if (overlap(dh, T * H * c->E, h, T * H * c->E) || overlap(dh, T * H * c->E, workspace, workspace_bytes))
-    return set_error(FL_ERR_ALIAS, "dh overlaps h / the workspace");
-  if (dw_vocab && (overlap(dw_vocab, V * H * 4, workspace, workspace_bytes) ||
-                   overlap(dw_vocab, V * H * 4, dh, T * H * c->E)))
-    return set_error(FL_ERR_ALIAS, "dw overlaps dh / the workspace");
+  if (int rc = check_head_backward(c, h, ln_g, w_vocab, T, grad_scale, dh, dln_g, dln_b, dw_vocab, workspace,
+                                   workspace_bytes))
+    return rc;
   const ClientWs w = carve(c, T, (char*)workspace);
   hipStream_t s = (hipStream_t)stream;
   if (c->d.dtype == FL_BF16)
     hipLaunchKernelGGL(ce_bwd_kernel<bf16>, dim3((unsigned)T), dim3(kThreads), 0, s, (bf16*)w.logits, c->vpad,
-                       (int)V, w.labels, w.lse, grad_scale);
+                       (int)c->d.vocab, w.labels, w.lse, grad_scale);
   else
     hipLaunchKernelGGL(ce_bwd_kernel<float>, dim3((unsigned)T), dim3(kThreads), 0, s, (float*)w.logits, c->vpad,
-                       (int)V, w.labels, w.lse, grad_scale);
+                       (int)c->d.vocab, w.labels, w.lse, grad_scale);
   CK(hipGetLastError());
-  // dh = dlogits W   (reduction over the padded vocabulary; W's rows past V
-  // read as zero); with the final LayerNorm this is the gradient at its output
-  GemmDesc g;
-  g.A = w.logits; g.B = w_vocab; g.C = ln_g ? (void*)w.dhn : dh;
-  g.M = (int)T; g.N = (int)H; g.K = (int)c->vpad;
-  g.lda = c->vpad; g.ldb = H; g.ldc = H;
-  g.b_rows = (int)V;
-  g.part = w.part; g.part_bytes = w.part_bytes;
-  CK(gemm(dt_of(c), GEMM_NN, EPI_STORE, g, s));
-  if (ln_g) {
-    CK(layernorm_bwd_dx(dt_of(c), w.dhn, h, w.mean, w.rstd, ln_g, nullptr, dh, (int)T, (int)H, s));
-    if (dln_g) {
-      const int nb = colsum_blocks((int)T);
-      CK(colsum_partial(dt_of(c), 1, w.dhn, H, h, w.mean, w.rstd, (int)T, (int)H, w.ln_part, w.ln_part2, s));
-      const ColsumJob jobs[2] = {{w.ln_part, dln_g, nb, (int)H}, {w.ln_part2, dln_b, nb, (int)H}};
-      CK(colsum_finish_n(jobs, 2, s));
-    }
-  }
-  if (!dw_vocab) return FL_OK;
-  // dW += dlogits^T hn   (rows m < V of the padded logits' columns; hn = h
-  // without the final LayerNorm)
-  GemmDesc gw;
-  gw.A = w.logits; gw.B = ln_g ? (const void*)w.hn : h; gw.C = dw_vocab;
-  gw.M = (int)V; gw.N = (int)H; gw.K = (int)T;
-  gw.lda = c->vpad; gw.ldb = H; gw.ldc = H;
-  gw.part = w.part; gw.part_bytes = w.part_bytes;
-  CK(gemm(dt_of(c), GEMM_TN, EPI_ACC_F32, gw, s));
-  return FL_OK;
+  return head_gradients(c, w, h, ln_g, w_vocab, T, dh, dln_g, dln_b, dw_vocab, s);
+}
+
+int fl_lm_head_preference_forward(fl_client* c, const fl_preference_desc* pref, const fl_batch_desc* batch,
+                                  const void* h, const void* ln_g, const void* ln_b, const void* w_vocab,
+                                  const int32_t* labels, const float* ref_logp, float* logp, float* loss,
+                                  float* loss_sum, void* workspace, size_t workspace_bytes, void* pref_workspace,
+                                  size_t pref_workspace_bytes, void* stream) {
+  if (int rc = check_preference_head(c, pref, batch)) return rc;
+  const long T = batch->total_tokens;
+  if (int rc = check_common(c, T, workspace, workspace_bytes)) return rc;
+  if (!h || !w_vocab || !labels) return set_error(FL_ERR_NULL, "h / w / labels is NULL");
+  if (int rc = check_final_ln(c, ln_g, ln_b)) return rc;
+  if (!al16(h) || !al16(w_vocab)) return set_error(FL_ERR_ALIGN, "h / w not 16-byte aligned");
+  if (int rc = preference_check(pref, batch, ref_logp, logp, loss, loss_sum, pref_workspace, pref_workspace_bytes))
+    return rc;
+  const size_t S = batch->num_seqs;
+  if (overlap(logp, 4 * S, workspace, workspace_bytes) || overlap(loss, 2 * S, workspace, workspace_bytes) ||
+      overlap(loss_sum, 4, workspace, workspace_bytes) ||
+      overlap(pref_workspace, pref_workspace_bytes, workspace, workspace_bytes))
+    return set_error(FL_ERR_ALIAS, "outputs or the loss's workspace overlap the client's workspace");
+  if (int rc = check_labels(c, labels, T)) return rc;
+  const ClientWs w = carve(c, T, (char*)workspace);
+  hipStream_t s = (hipStream_t)stream;
+  if (int rc = head_logits(c, w, h, ln_g, ln_b, w_vocab, labels, T, s)) return rc;
+  return preference_forward(pref, batch, w.logits, c->vpad, w.labels, ref_logp, logp, loss, loss_sum, pref_workspace,
+                            s);
+}
+
+int fl_lm_head_preference_backward(fl_client* c, const fl_preference_desc* pref, const fl_batch_desc* batch,
+                                   const void* h, const void* ln_g, const void* w_vocab, float grad_scale, void* dh,
+                                   float* dln_g, float* dln_b, float* dw_vocab, void* workspace,
+                                   size_t workspace_bytes, void* pref_workspace, size_t pref_workspace_bytes,
+                                   void* stream) {
+  if (int rc = check_preference_head(c, pref, batch)) return rc;
+  const long T = batch->total_tokens;
+  if (int rc = check_common(c, T, workspace, workspace_bytes)) return rc;
+  if (int rc = preference_check_backward(pref, batch, grad_scale, pref_workspace, pref_workspace_bytes)) return rc;
+  if (int rc = check_head_backward(c, h, ln_g, w_vocab, T, grad_scale, dh, dln_g, dln_b, dw_vocab, workspace,
+                                   workspace_bytes))
+    return rc;
+  if (overlap(pref_workspace, pref_workspace_bytes, workspace, workspace_bytes) ||
+      overlap(pref_workspace, pref_workspace_bytes, dh, T * c->d.hidden * c->E))
+    return set_error(FL_ERR_ALIAS, "the loss's workspace overlaps dh or the client's workspace");
+  const ClientWs w = carve(c, T, (char*)workspace);
+  hipStream_t s = (hipStream_t)stream;
+  // in place: the logits become their own gradient (padded columns: 0)
+  if (int rc = preference_gradient(pref, batch, w.logits, c->vpad, w.labels, grad_scale, w.logits, c->vpad,
+                                   (int)c->vpad, pref_workspace, s))
+    return rc;
+  return head_gradients(c, w, h, ln_g, w_vocab, T, dh, dln_g, dln_b, dw_vocab, s);
 }
 
 }  // extern "C"

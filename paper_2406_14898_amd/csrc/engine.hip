@@ -532,10 +532,22 @@ GemmDesc& with_part(GemmDesc& g, const Plan& plan) {
   return g;
 }
 
+// One block's low-rank adapters on the fused query / key / value projection.
+struct BlockAdapters {
+  const fl_adapter_desc* desc;
+  const fl_batch_desc* batch;
+  const int32_t* client_adapter;
+  const void *a, *b;
+  float* v;            // [T, r], kept from the forward for the backward
+  float *da, *db;      // backward only
+  void* ws;
+};
+
 // keep_z = false: the FFN's pre-activation z is not stored (nothing reads it
 // when the block's intermediates are not kept for a backward).
 int block_forward(fl_stack* st, const BatchInfo& bi, const Plan& plan, const fl_layer_params& p, const void* x,
-                  const Acts& a, void* out, hipStream_t s, bool keep_z = true) {
+                  const Acts& a, void* out, hipStream_t s, bool keep_z = true,
+                  const BlockAdapters* adapt = nullptr) {
   const DType dt = (DType)st->d.dtype;
   const int T = bi.T, H = st->d.hidden, F = st->d.ffn_hidden;
   const double E = st->E, TH = (double)T * H;
@@ -546,6 +558,11 @@ int block_forward(fl_stack* st, const BatchInfo& bi, const Plan& plan, const fl_
   g.lda = H; g.ldb = H; g.ldc = 3 * H; g.bias = p.b_qkv;
   LAUNCH(FL_PROF_GEMM_NT_BIAS, gemm_flops(T, 3 * H, H), gemm_bytes(T, 3 * H, H, E, E),
          gemm(dt, GEMM_NT, EPI_BIAS, with_part(g, plan), s));
+  if (adapt) {
+    const int rc = adapter_forward(adapt->desc, adapt->batch, adapt->client_adapter, a.u, H, adapt->a, adapt->b, a.qkv,
+                                   3 * H, a.qkv, 3 * H, adapt->v, adapt->ws, s);
+    if (rc) return rc;
+  }
   // q and k: the first rotary_dim features of every head, read and written.
   // A separate pass on purpose: folded into the QKV epilogue (a lane-pair
   // exchange plus table loads per row) it measured 0.5 ms slower per call
@@ -647,7 +664,7 @@ int ln_backward(fl_stack* st, DType dt, const void* dy, const void* xin, const f
 // that way by the block above.
 int block_backward(fl_stack* st, const BatchInfo& bi, const Plan& plan, const Work& w, const fl_layer_params& p,
                    const fl_layer_grads& gr, const void* x, const Acts& a, const void* dy, void* dx, hipStream_t s,
-                   float* dx_sum, bool b2_done) {
+                   float* dx_sum, bool b2_done, const BlockAdapters* adapt = nullptr) {
   const DType dt = (DType)st->d.dtype;
   const int T = bi.T, H = st->d.hidden, F = st->d.ffn_hidden;
   const double E = st->E;
@@ -768,6 +785,9 @@ int block_backward(fl_stack* st, const BatchInfo& bi, const Plan& plan, const Wo
   }
   if ((rc = linear(FL_PROF_GEMM_NN, alpha > 0.f ? EPI_RES : EPI_STORE, gd, gw, fused_bqkv ? nullptr : gr.b_qkv)))
     return rc;
+  if (adapt && (rc = adapter_backward(adapt->desc, adapt->batch, adapt->client_adapter, w.dqkv, 3 * H, a.u, H, adapt->a,
+                                      adapt->b, adapt->v, w.tmp, H, w.tmp, H, adapt->da, adapt->db, adapt->ws, s)))
+    return rc;
   // u = LN1(x); x also feeds h directly (plain residual)
   if ((rc = ln_backward(st, dt, w.tmp, x, a.mean1, a.rstd1, p.ln1_g, alpha > 0.f ? nullptr : w.dh, dx, gr.ln1_g,
                         gr.ln1_b, dx_sum, T, H, w.lnp[0], fin, s)))
@@ -779,6 +799,10 @@ int block_backward(fl_stack* st, const BatchInfo& bi, const Plan& plan, const Wo
 
 namespace flglm {
 int set_error(int code, const char* msg) { return fail(code, "%s", msg); }
+int check_batch(const fl_batch_desc* b) {
+  BatchInfo bi;
+  return validate_batch(b, &bi);
+}
 }  // namespace flglm
 
 // ---------------------------------------------------------------------------
@@ -823,6 +847,90 @@ struct ProfOff {
   explicit ProfOff(fl_stack* s) : st(s), was(s->prof_mask) { st->prof_mask = 0; }
   ~ProfOff() { st->prof_mask = was; }
 };
+
+}  // namespace
+
+// ---------------------------------------------------------------------------
+// Adapters of the whole stack: descriptor of one block's projection, and the
+// adapters' workspace (every block's v, then one call's scratch).
+// ---------------------------------------------------------------------------
+namespace {
+
+fl_adapter_desc adapter_desc(const fl_stack* st, const fl_stack_adapters* ad) {
+  fl_adapter_desc d;
+  d.num_adapters = ad->num_adapters;
+  d.rank = ad->rank;
+  d.in_features = st->d.hidden;
+  d.out_features = 3 * st->d.hidden;
+  d.scale = ad->scale;
+  d.dtype = st->d.dtype;
+  return d;
+}
+size_t adapter_v_bytes(const fl_stack* st, const fl_batch_desc* b, const fl_stack_adapters* ad) {
+  return align_up(sizeof(float) * (size_t)b->total_tokens * ad->rank);
+}
+
+struct StackAdapters {
+  const fl_stack_adapters* ad = nullptr;
+  const fl_batch_desc* batch = nullptr;
+  fl_adapter_desc desc;
+  char* v = nullptr;  // block l's: v + l * v_bytes
+  size_t v_bytes = 0;
+  void* scratch = nullptr;
+  BlockAdapters block(int l) const {
+    BlockAdapters r{};
+    if (!ad) return r;
+    r.desc = &desc;
+    r.batch = batch;
+    r.client_adapter = ad->client_adapter;
+    r.a = ad->layers[l].a;
+    r.b = ad->layers[l].b;
+    r.v = (float*)(v + l * v_bytes);
+    if (ad->grads) {
+      r.da = ad->grads[l].a;
+      r.db = ad->grads[l].b;
+    }
+    r.ws = scratch;
+    return r;
+  }
+};
+
+// Checks the adapters of a call and carves their workspace.
+int carve_adapters(const fl_stack* st, const fl_batch_desc* b, const BatchInfo& bi, const fl_stack_adapters* ad,
+                   bool backward, void* ws, size_t ws_bytes, StackAdapters* out) {
+  const int N = st->d.num_layers;
+  out->ad = ad;
+  out->batch = b;
+  out->desc = adapter_desc(st, ad);
+  if (!ws) return fail(FL_ERR_NULL, "the adapters' workspace is NULL");
+  if (!aligned16(ws)) return fail(FL_ERR_ALIGN, "the adapters' workspace must be 16-byte aligned");
+  // (the descriptor before its rank sizes anything)
+  size_t scratch;
+  if (int rc = adapter_workspace_bytes(&out->desc, b, &scratch)) return rc;
+  out->v_bytes = adapter_v_bytes(st, b, ad);
+  const size_t need = N * out->v_bytes + scratch;
+  if (ws_bytes < need) return fail(FL_ERR_WORKSPACE, "adapters' workspace %zu bytes < required %zu", ws_bytes, need);
+  out->v = (char*)ws;
+  out->scratch = out->v + N * out->v_bytes;
+  if (int rc = adapter_check(&out->desc, b, ad->client_adapter, out->scratch, scratch)) return rc;
+  if (!ad->layers || (backward && !ad->grads)) return fail(FL_ERR_NULL, "adapter layers / gradients are NULL");
+  const size_t n = (size_t)ad->num_adapters * ad->rank * st->d.hidden;
+  for (int l = 0; l < N; ++l) {
+    const fl_layer_adapters& p = ad->layers[l];
+    if (!p.a || !p.b) return fail(FL_ERR_NULL, "layer %d: an adapter is NULL", l);
+    if (!aligned16(p.a) || !aligned16(p.b)) return fail(FL_ERR_ALIGN, "layer %d: an adapter is not 16-byte aligned", l);
+    if (overlap(ws, ws_bytes, p.a, n * st->E) || overlap(ws, ws_bytes, p.b, 3 * n * st->E))
+      return fail(FL_ERR_ALIAS, "layer %d: an adapter overlaps the adapters' workspace", l);
+    if (!backward) continue;
+    const fl_layer_adapter_grads& g = ad->grads[l];
+    if (!g.a || !g.b) return fail(FL_ERR_NULL, "layer %d: an adapter gradient is NULL", l);
+    if (!aligned16(g.a) || !aligned16(g.b))
+      return fail(FL_ERR_ALIGN, "layer %d: an adapter gradient is not 16-byte aligned", l);
+    if (overlap(ws, ws_bytes, g.a, n * 4) || overlap(ws, ws_bytes, g.b, 3 * n * 4) || overlap(g.a, n * 4, g.b, 3 * n * 4))
+      return fail(FL_ERR_ALIAS, "layer %d: an adapter gradient overlaps the other or the adapters' workspace", l);
+  }
+  return FL_OK;
+}
 
 }  // namespace
 
@@ -939,8 +1047,9 @@ int fl_client_token_range(const fl_batch_desc* b, int32_t client, int64_t* begin
   return FL_OK;
 }
 
-int fl_server_stack_forward(fl_stack* st, const fl_batch_desc* b, const fl_layer_params* layers, const void* x,
-                            void* y, void* saved, int recompute, void* ws, size_t ws_bytes, void* stream) {
+static int stack_forward(fl_stack* st, const fl_batch_desc* b, const fl_layer_params* layers,
+                         const fl_stack_adapters* adapters, const void* x, void* y, void* saved, int recompute,
+                         void* ws, size_t ws_bytes, void* adapter_ws, size_t adapter_ws_bytes, void* stream) {
   if (!st) return fail(FL_ERR_NULL, "stack is NULL");
   BatchInfo bi;
   int rc = validate_batch(b, &bi);
@@ -959,6 +1068,13 @@ int fl_server_stack_forward(fl_stack* st, const fl_batch_desc* b, const fl_layer
   if (overlap(saved, nsaved, x, act) || overlap(saved, nsaved, y, act))
     return fail(FL_ERR_ALIAS, "saved overlaps x / y");
 
+  StackAdapters sa;
+  if (adapters) {
+    if ((rc = carve_adapters(st, b, bi, adapters, false, adapter_ws, adapter_ws_bytes, &sa))) return rc;
+    if (overlap(adapter_ws, adapter_ws_bytes, ws, ws_bytes) || overlap(adapter_ws, adapter_ws_bytes, x, act) ||
+        overlap(adapter_ws, adapter_ws_bytes, y, act) || overlap(adapter_ws, adapter_ws_bytes, saved, nsaved))
+      return fail(FL_ERR_ALIAS, "the adapters' workspace overlaps x / y / saved / workspace");
+  }
   hipStream_t s = (hipStream_t)stream;
   Carver cw(ws);
   Work w;
@@ -975,10 +1091,25 @@ int fl_server_stack_forward(fl_stack* st, const fl_batch_desc* b, const fl_layer
     const bool keep = saved && !recompute;  // intermediates kept for the backward
     const Acts& a = keep ? sv.acts[l] : w.acts;
     void* out = (l == N - 1) ? y : (saved ? sv.xin[l + 1] : w.ping[l & 1]);
-    if ((rc = block_forward(st, bi, w.plan, layers[l], cur, a, out, s, keep))) return rc;
+    const BlockAdapters ba = sa.block(l);
+    if ((rc = block_forward(st, bi, w.plan, layers[l], cur, a, out, s, keep, adapters ? &ba : nullptr))) return rc;
     cur = out;
   }
   return FL_OK;
+}
+
+int fl_server_stack_forward(fl_stack* st, const fl_batch_desc* b, const fl_layer_params* layers, const void* x,
+                            void* y, void* saved, int recompute, void* ws, size_t ws_bytes, void* stream) {
+  return stack_forward(st, b, layers, nullptr, x, y, saved, recompute, ws, ws_bytes, nullptr, 0, stream);
+}
+
+int fl_server_stack_forward_adapters(fl_stack* st, const fl_batch_desc* b, const fl_layer_params* layers,
+                                     const fl_stack_adapters* adapters, const void* x, void* y, void* saved,
+                                     int recompute, void* ws, size_t ws_bytes, void* adapter_ws,
+                                     size_t adapter_ws_bytes, void* stream) {
+  if (!adapters) return fail(FL_ERR_NULL, "adapters is NULL");
+  return stack_forward(st, b, layers, adapters, x, y, saved, recompute, ws, ws_bytes, adapter_ws, adapter_ws_bytes,
+                       stream);
 }
 
 int fl_server_stack_forward_noalloc(fl_stack* st, const fl_batch_desc* b, const fl_layer_params* layers,
@@ -1020,9 +1151,10 @@ int fl_server_stack_forward_noalloc(fl_stack* st, const fl_batch_desc* b, const 
   return FL_OK;
 }
 
-int fl_server_stack_backward(fl_stack* st, const fl_batch_desc* b, const fl_layer_params* layers,
-                             const fl_layer_grads* grads, const void* x, const void* saved, const void* dy, void* dx,
-                             int recompute, void* ws, size_t ws_bytes, void* stream) {
+static int stack_backward(fl_stack* st, const fl_batch_desc* b, const fl_layer_params* layers,
+                          const fl_layer_grads* grads, const fl_stack_adapters* adapters, const void* x,
+                          const void* saved, const void* dy, void* dx, int recompute, void* ws, size_t ws_bytes,
+                          void* adapter_ws, size_t adapter_ws_bytes, void* stream) {
   if (!st) return fail(FL_ERR_NULL, "stack is NULL");
   BatchInfo bi;
   int rc = validate_batch(b, &bi);
@@ -1042,6 +1174,14 @@ int fl_server_stack_backward(fl_stack* st, const fl_batch_desc* b, const fl_laye
       overlap(ws, ws_bytes, saved, nsaved))
     return fail(FL_ERR_ALIAS, "workspace overlaps x / saved / dy / dx");
 
+  StackAdapters sa;
+  if (adapters) {
+    if ((rc = carve_adapters(st, b, bi, adapters, true, adapter_ws, adapter_ws_bytes, &sa))) return rc;
+    if (overlap(adapter_ws, adapter_ws_bytes, ws, ws_bytes) || overlap(adapter_ws, adapter_ws_bytes, x, act) ||
+        overlap(adapter_ws, adapter_ws_bytes, dy, act) || overlap(adapter_ws, adapter_ws_bytes, dx, act) ||
+        overlap(adapter_ws, adapter_ws_bytes, saved, nsaved))
+      return fail(FL_ERR_ALIAS, "the adapters' workspace overlaps x / dy / dx / saved / workspace");
+  }
   hipStream_t s = (hipStream_t)stream;
   Carver cw(ws);
   Work w;
@@ -1055,8 +1195,10 @@ int fl_server_stack_backward(fl_stack* st, const fl_batch_desc* b, const fl_laye
   for (int l = N - 1; l >= 0; --l) {
     const void* xin = (l == 0) ? x : sv.xin[l];
     const Acts* a = &sv.acts[l];
+    const BlockAdapters ba = sa.block(l);
+    const BlockAdapters* ad = adapters ? &ba : nullptr;
     if (recompute) {
-      if ((rc = block_forward(st, bi, w.plan, layers[l], xin, w.acts, nullptr, s))) return rc;
+      if ((rc = block_forward(st, bi, w.plan, layers[l], xin, w.acts, nullptr, s, true, ad))) return rc;
       a = &w.acts;
     }
     void* gout = (l == 0) ? dx : w.ping[(N - 1 - l) & 1];
@@ -1064,10 +1206,36 @@ int fl_server_stack_backward(fl_stack* st, const fl_batch_desc* b, const fl_laye
     // come out of block l's last LayerNorm backward
     float* below_b2 = l > 0 ? grads[l - 1].b_2 : nullptr;
     const bool b2_done = l < N - 1 && grads[l].b_2 != nullptr;
-    if ((rc = block_backward(st, bi, w.plan, w, layers[l], grads[l], xin, *a, gcur, gout, s, below_b2, b2_done)))
+    if ((rc = block_backward(st, bi, w.plan, w, layers[l], grads[l], xin, *a, gcur, gout, s, below_b2, b2_done,
+                             ad)))
       return rc;
     gcur = gout;
   }
+  return FL_OK;
+}
+
+int fl_server_stack_backward(fl_stack* st, const fl_batch_desc* b, const fl_layer_params* layers,
+                             const fl_layer_grads* grads, const void* x, const void* saved, const void* dy, void* dx,
+                             int recompute, void* ws, size_t ws_bytes, void* stream) {
+  return stack_backward(st, b, layers, grads, nullptr, x, saved, dy, dx, recompute, ws, ws_bytes, nullptr, 0, stream);
+}
+
+int fl_server_stack_backward_adapters(fl_stack* st, const fl_batch_desc* b, const fl_layer_params* layers,
+                                      const fl_layer_grads* grads, const fl_stack_adapters* adapters, const void* x,
+                                      const void* saved, const void* dy, void* dx, int recompute, void* ws,
+                                      size_t ws_bytes, void* adapter_ws, size_t adapter_ws_bytes, void* stream) {
+  if (!adapters) return fail(FL_ERR_NULL, "adapters is NULL");
+  return stack_backward(st, b, layers, grads, adapters, x, saved, dy, dx, recompute, ws, ws_bytes, adapter_ws,
+                        adapter_ws_bytes, stream);
+}
+
+int fl_stack_adapter_bytes(const fl_stack* st, const fl_batch_desc* b, const fl_stack_adapters* adapters,
+                           size_t* bytes) {
+  if (!st || !adapters || !bytes) return fail(FL_ERR_NULL, "stack / adapters / bytes is NULL");
+  const fl_adapter_desc d = adapter_desc(st, adapters);
+  size_t scratch;
+  if (int rc = adapter_workspace_bytes(&d, b, &scratch)) return rc;
+  *bytes = adapter_v_bytes(st, b, adapters) * st->d.num_layers + scratch;
   return FL_OK;
 }
 

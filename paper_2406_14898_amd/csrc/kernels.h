@@ -4,7 +4,14 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "../../include/flglm.h"
+
 namespace flglm {
+
+// Sets the thread's error message; returns code.
+int set_error(int code, const char* msg);
+// The checks every entry point makes of a batch descriptor.
+int check_batch(const fl_batch_desc* b);
 
 enum DType : int { DT_BF16 = 0, DT_F32 = 1 };
 enum GemmLayout : int { GEMM_NT = 0, GEMM_NN = 1, GEMM_TN = 2 };
@@ -247,5 +254,31 @@ hipError_t attn_bwd_bf16(const AttnDesc& a, hipStream_t st);
 // rows of sequences s0 .. s0+nseq-1.  Unpacking zero-fills padded positions.
 hipError_t pack_client(DType dt, const void* client, void* packed, const int32_t* cu_dev, int s0, int nseq,
                        int Lmax, int H, bool unpack, hipStream_t st);
+
+// Preference loss on logits that the caller has checked (preference.hip); the
+// workspace holds a row's factors between the two.
+int preference_check(const fl_preference_desc* d, const fl_batch_desc* b, const float* ref, float* logp, float* loss,
+                     float* loss_sum, void* ws, size_t ws_bytes);
+int preference_check_backward(const fl_preference_desc* d, const fl_batch_desc* b, float grad_scale, void* ws,
+                              size_t ws_bytes);
+int preference_forward(const fl_preference_desc* d, const fl_batch_desc* b, const void* logits, long ld,
+                       const int32_t* labels, const float* ref, float* logp, float* loss, float* loss_sum, void* ws,
+                       hipStream_t s);
+int preference_gradient(const fl_preference_desc* d, const fl_batch_desc* b, const void* logits, long ld,
+                        const int32_t* labels, float grad_scale, void* dlogits, long ldd, int width, void* ws,
+                        hipStream_t s);
+
+// Low-rank adapters on arguments that the caller has checked (adapters.hip).
+// adapter_check: descriptor, batch, slots and workspace.
+int adapter_check(const fl_adapter_desc* d, const fl_batch_desc* b, const int32_t* client_adapter, const void* ws,
+                  size_t ws_bytes);
+int adapter_workspace_bytes(const fl_adapter_desc* d, const fl_batch_desc* b, size_t* bytes);
+int adapter_forward(const fl_adapter_desc* d, const fl_batch_desc* batch, const int32_t* client_adapter, const void* x,
+                    int64_t ldx, const void* a, const void* b, const void* base, int64_t ld_base, void* y, int64_t ldy,
+                    float* v, void* ws, hipStream_t s);
+int adapter_backward(const fl_adapter_desc* d, const fl_batch_desc* batch, const int32_t* client_adapter,
+                     const void* dy, int64_t ld_dy, const void* x, int64_t ldx, const void* a, const void* b,
+                     const float* v, const void* dres, int64_t ld_dres, void* dx, int64_t ld_dx, float* da, float* db,
+                     void* ws, hipStream_t s);
 
 }  // namespace flglm

@@ -1,0 +1,425 @@
+// Preference loss over pairs of packed sequences, and its gradient.
+//
+// Sequence 2p of the batch is the preferred answer of pair p, sequence 2p + 1
+// the rejected one.  With x_t the logits of row t, over the labelled rows of
+// a sequence s
+//   l_s = sum_t x_t[label_t] - logsumexp(x_t),
+//   z_p = beta ((l_2p - ref_2p) - (l_2p+1 - ref_2p+1)),
+//   L_p = (1 - eps) softplus(-z_p) + eps softplus(z_p),
+// and with k_s = beta dL_p/dz_p for the preferred, -k for the rejected one,
+//   dlogits_t = grad_scale k_s (onehot(label_t) - softmax(x_t)).
+//
+// The logits are read once for the loss and once for the gradient: k_s hangs
+// on whole sequences, so no row's gradient is known before the last row of
+// its pair has been read.  Rows without a label are read in neither.
+//
+//  * row kernel: the running (maximum, sum of exponentials) of a row's
+//    columns; a row is split over several workgroups when rows are few.
+//  * pair kernel: one workgroup a pair joins the parts of its rows, forms the
+//    sequence sums, the loss and each row's factors.  The last pair to finish
+//    adds the losses in pair order.
+//  * gradient kernel: one pass over the logits.
+//
+// Sums of exponentials are fp32 (values in [0, 1], at most 2^24 of them, added
+// in parts); log-probabilities and their sums over a sequence are 64 bits,
+// because z is a difference of sums of hundreds of rows.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/flglm.h"
+#include "common.h"
+#include "kernels.h"
+
+using namespace flglm;
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPairsArg = 128;       // pairs whose bounds travel in one launch's kernel arguments
+constexpr int kMaxSplits = 16;
+constexpr long kWantGroups = 2048;   // workgroups that fill the chip
+
+// (max, sum of exp(x - max)) pairs; an empty part is (-inf, 0).
+__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
+  if (m2 == -INFINITY) return;
+  if (m == -INFINITY) {
+    m = m2;
+    s = s2;
+    return;
+  }
+  const float mx = fmaxf(m, m2);
+  s = s * __expf(m - mx) + s2 * __expf(m2 - mx);
+  m = mx;
+}
+
+// Columns [c0, c1) of each labelled row: part[row][split] = (max, sum).
+template <typename T>
+__global__ void __launch_bounds__(kThreads) pref_row_kernel(const T* logits, long ld, int V, int cols,
+                                                            const int32_t* labels, float2* part, uint32_t* done) {
+  const long t = blockIdx.x;
+  const int sp = blockIdx.y;
+  if (t == 0 && sp == 0 && threadIdx.x == 0) *done = 0;  // the pair kernel's count, of the launch behind this one
+  const int lab = labels[t];
+  if (lab < 0 || lab >= V) return;
+  const T* row = logits + t * ld;
+  const int c0 = sp * cols, c1 = min(V, c0 + cols);
+  float m = -INFINITY, s = 0.f;
+  for (int j0 = c0 + threadIdx.x * 8; j0 < c1; j0 += kThreads * 8) {
+    Vec8<T> v;
+    v.load(row + j0);
+    float x[8], mx = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      x[k] = v.get(k);
+      mx = fmaxf(mx, x[k]);
+    }
+    if (mx == -INFINITY) {  // masked columns only, or NaN, which a maximum passes over
+#pragma unroll
+      for (int k = 0; k < 8; ++k) mx = x[k] != x[k] ? x[k] : mx;
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += __expf(x[k] - mx);
+    join(m, s, mx, sum);
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    const float m2 = __shfl_xor(m, o), s2 = __shfl_xor(s, o);
+    join(m, s, m2, s2);
+  }
+  __shared__ float sm[kThreads / 64], ss[kThreads / 64];
+  if ((threadIdx.x & 63) == 0) {
+    sm[threadIdx.x >> 6] = m;
+    ss[threadIdx.x >> 6] = s;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kThreads / 64; ++w) join(m, s, sm[w], ss[w]);
+    part[t * gridDim.y + sp] = make_float2(m, s);
+  }
+}
+
+struct PairArgs {
+  int32_t cu[2 * kPairsArg + 1];
+  int first, count, pairs;  // this launch's pairs [first, first + count) of `pairs`
+};
+
+__device__ __forceinline__ double block_sum(double v, double* sh) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double t = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) t += sh[w];
+  return t;
+}
+
+__device__ __forceinline__ double softplus(double u) { return fmax(u, 0.0) + log1p(exp(-fabs(u))); }
+
+// factors[t] = (max, k / sum of exponentials, k, 0): the gradient of row t is
+// k onehot - (k / sum) exp(x - max); k = 0 for a row without a label.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) pref_pair_kernel(PairArgs a, const T* logits, long ld, int V, int splits,
+                                                             const int32_t* labels, const float2* part,
+                                                             const float* ref, double beta, double eps, float* logp,
+                                                             float* loss, float* loss_sum, f32x4* factors,
+                                                             uint32_t* done) {
+  __shared__ double sh[kThreads / 64];
+  __shared__ bool last;
+  const int p = a.first + blockIdx.x;
+  double lp[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r0 = a.cu[2 * blockIdx.x + h], r1 = a.cu[2 * blockIdx.x + h + 1];
+    double sum = 0;
+    for (int t = r0 + threadIdx.x; t < r1; t += kThreads) {
+      const int lab = labels[t];
+      f32x4 f = {0.f, 0.f, 0.f, 0.f};
+      if (lab >= 0 && lab < V) {
+        float m = -INFINITY, s = 0.f;
+        for (int k = 0; k < splits; ++k) {
+          const float2 q = part[(long)t * splits + k];
+          join(m, s, q.x, q.y);
+        }
+        sum += ((double)to_f32(logits[(long)t * ld + lab]) - (double)m) - log((double)s);
+        f[0] = m;
+        f[1] = s;
+        f[2] = 1.f;
+      }
+      factors[t] = f;
+    }
+    lp[h] = block_sum(sum, sh);
+  }
+  double d = lp[0] - lp[1];
+  if (ref) d = (lp[0] - (double)ref[2 * p]) - (lp[1] - (double)ref[2 * p + 1]);
+  const double z = beta * d;
+  // (no 0 times infinity: z is infinite where a label has no probability)
+  const double L = (1.0 - eps) * softplus(-z) + (eps > 0.0 ? eps * softplus(z) : 0.0);
+  const double k = beta * (eps / (1.0 + exp(-z)) - (1.0 - eps) / (1.0 + exp(z)));
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r0 = a.cu[2 * blockIdx.x + h], r1 = a.cu[2 * blockIdx.x + h + 1];
+    const double kh = h ? -k : k;
+    for (int t = r0 + threadIdx.x; t < r1; t += kThreads) {
+      f32x4 f = factors[t];  // this thread's own
+      if (f[2] != 0.f) {
+        f[1] = (float)(kh / (double)f[1]);
+        f[2] = (float)kh;
+        factors[t] = f;
+      }
+    }
+  }
+  if (threadIdx.x == 0) {
+    logp[2 * p] = (float)lp[0];
+    logp[2 * p + 1] = (float)lp[1];
+    loss[p] = (float)L;
+    __threadfence();
+    last = atomicAdd(done, 1u) == (uint32_t)(a.pairs - 1);
+  }
+  __syncthreads();
+  if (!last) return;
+  // every pair's loss is written: added in pair order, whichever came last
+  __threadfence();
+  double sum = 0;
+  for (int i = threadIdx.x; i < a.pairs; i += kThreads) sum += (double)__hip_atomic_load(loss + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  sum = block_sum(sum, sh);
+  if (threadIdx.x == 0) *loss_sum = (float)sum;
+}
+
+// The first `width` columns of dlogits (past V: 0) of row t; may be the logits
+// themselves.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) pref_grad_kernel(const T* logits, long ld, int V, const int32_t* labels,
+                                                             const f32x4* factors, float scale, T* dlogits, long ldd,
+                                                             int width) {
+  const long t = blockIdx.x;
+  const f32x4 f = factors[t];
+  const int lab = labels[t];
+  const T* row = logits + t * ld;
+  T* out = dlogits + t * ldd;
+  const float m = f[0], ks = scale * f[1], k = scale * f[2];
+  const bool live = lab >= 0 && lab < V;
+  for (long j0 = ((long)blockIdx.y * kThreads + threadIdx.x) * 8; j0 < width; j0 += (long)gridDim.y * kThreads * 8) {
+    Vec8<T> v;
+    float g[8];
+    if (live && j0 < V) {
+      v.load(row + j0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] = (j0 + i == lab ? k : 0.f) - ks * __expf(v.get(i) - m);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] = 0.f;
+    }
+    v.set(g);
+    v.store(out + j0);
+  }
+}
+
+bool al16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + nb && y < x + na;
+}
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+int launch_status() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? FL_OK : set_error(FL_ERR_HIP, hipGetErrorString(e));
+}
+
+struct PrefWs {
+  f32x4* factors;  // [T]
+  float2* part;    // [T][splits]
+  uint32_t* done;
+  size_t total;
+};
+// Parts a row is split into: one when the rows alone fill the chip.
+int splits_of(long T, long V) {
+  const long most = std::max(1L, V / (8 * kThreads));
+  return (int)std::min<long>({(kWantGroups + T - 1) / T, most, (long)kMaxSplits});
+}
+PrefWs carve(long T, long V, char* base) {
+  PrefWs w;
+  size_t off = 0;
+  auto take = [&](size_t n) {
+    char* p = base ? base + off : nullptr;
+    off = align256(off + n);
+    return p;
+  };
+  w.factors = (f32x4*)take((size_t)T * sizeof(f32x4));
+  w.part = (float2*)take((size_t)T * splits_of(T, V) * sizeof(float2));
+  w.done = (uint32_t*)take(sizeof(uint32_t));
+  w.total = off;
+  return w;
+}
+
+int check_desc(const fl_preference_desc* d) {
+  if (!d) return set_error(FL_ERR_NULL, "preference descriptor is NULL");
+  if (d->dtype != FL_BF16 && d->dtype != FL_F32) return set_error(FL_ERR_SHAPE, "dtype must be bf16 or fp32");
+  if (d->vocab < 8 || d->vocab % 8 || d->vocab > (1 << 24))
+    return set_error(FL_ERR_SHAPE, "vocab must be a multiple of 8 in [8, 2^24]");
+  if (!std::isfinite(d->beta) || !(d->beta > 0.f)) return set_error(FL_ERR_ARG, "beta must be finite and > 0");
+  if (!(d->label_smoothing >= 0.f && d->label_smoothing <= 0.5f))
+    return set_error(FL_ERR_ARG, "label_smoothing must be in [0, 0.5]");
+  return FL_OK;
+}
+int check_pairs(const fl_batch_desc* b) {
+  if (int rc = check_batch(b)) return rc;
+  for (int c = 0; c < b->num_clients; ++c)
+    if ((b->client_seq_ptr[c + 1] - b->client_seq_ptr[c]) % 2)
+      return set_error(FL_ERR_CLIENTS, "every client's sequences come in pairs (preferred, rejected)");
+  return FL_OK;
+}
+int check_ws(const fl_preference_desc* d, const fl_batch_desc* b, void* ws, size_t bytes) {
+  if (!ws) return set_error(FL_ERR_NULL, "workspace is NULL");
+  if (!al16(ws)) return set_error(FL_ERR_ALIGN, "workspace is not 16-byte aligned");
+  if (bytes < carve(b->total_tokens, d->vocab, nullptr).total) return set_error(FL_ERR_WORKSPACE, "workspace too small");
+  return FL_OK;
+}
+int check_logits(const fl_preference_desc* d, const void* logits, int64_t ld, const int32_t* labels) {
+  if (!logits || !labels) return set_error(FL_ERR_NULL, "logits / labels is NULL");
+  if (!al16(logits) || ((uintptr_t)labels & 3)) return set_error(FL_ERR_ALIGN, "logits / labels misaligned");
+  if (ld < d->vocab || ld % 8 || ld > (int64_t(1) << 32))
+    return set_error(FL_ERR_SHAPE, "the logits' row stride must be a multiple of 8, at least vocab and at most 2^32");
+  return FL_OK;
+}
+
+template <typename T>
+int forward(const fl_preference_desc* d, const fl_batch_desc* b, const T* logits, long ld, const int32_t* labels,
+            const float* ref, float* logp, float* loss, float* loss_sum, const PrefWs& w, hipStream_t s) {
+  const long tokens = b->total_tokens;
+  const int V = (int)d->vocab, splits = splits_of(tokens, V);
+  const int cols = (int)(((V + splits - 1) / splits + 7) / 8 * 8);
+  hipLaunchKernelGGL(pref_row_kernel<T>, dim3((unsigned)tokens, splits), dim3(kThreads), 0, s, logits, ld, V, cols,
+                     labels, w.part, w.done);
+  if (int rc = launch_status()) return rc;
+  PairArgs a;
+  a.pairs = b->num_seqs / 2;
+  for (a.first = 0; a.first < a.pairs; a.first += a.count) {
+    a.count = std::min(a.pairs - a.first, kPairsArg);
+    std::copy(b->cu_seqlens + 2 * a.first, b->cu_seqlens + 2 * (a.first + a.count) + 1, a.cu);
+    hipLaunchKernelGGL(pref_pair_kernel<T>, dim3(a.count), dim3(kThreads), 0, s, a, logits, ld, V, splits, labels,
+                       w.part, ref, (double)d->beta, (double)d->label_smoothing, logp, loss, loss_sum, w.factors,
+                       w.done);
+    if (int rc = launch_status()) return rc;
+  }
+  return FL_OK;
+}
+
+template <typename T>
+int gradient(const fl_preference_desc* d, long tokens, const T* logits, long ld, const int32_t* labels,
+             float grad_scale, T* dlogits, long ldd, int width, const PrefWs& w, hipStream_t s) {
+  const int V = (int)d->vocab, splits = splits_of(tokens, V);
+  hipLaunchKernelGGL(pref_grad_kernel<T>, dim3((unsigned)tokens, splits), dim3(kThreads), 0, s, logits, ld, V, labels,
+                     w.factors, grad_scale, dlogits, ldd, width);
+  return launch_status();
+}
+
+}  // namespace
+
+namespace flglm {
+
+int preference_check(const fl_preference_desc* d, const fl_batch_desc* b, const float* ref, float* logp, float* loss,
+                     float* loss_sum, void* ws, size_t ws_bytes) {
+  if (int rc = check_desc(d)) return rc;
+  if (int rc = check_pairs(b)) return rc;
+  if (!logp || !loss || !loss_sum) return set_error(FL_ERR_NULL, "logp / loss / loss_sum is NULL");
+  if (((uintptr_t)logp & 3) || ((uintptr_t)loss & 3) || ((uintptr_t)loss_sum & 3) || ((uintptr_t)ref & 3))
+    return set_error(FL_ERR_ALIGN, "ref_logp / logp / loss / loss_sum misaligned");
+  if (int rc = check_ws(d, b, ws, ws_bytes)) return rc;
+  const size_t S = b->num_seqs;
+  const void* out[3] = {logp, loss, loss_sum};
+  const size_t n[3] = {4 * S, 2 * S, 4};
+  for (int i = 0; i < 3; ++i) {
+    for (int j = i + 1; j < 3; ++j)
+      if (overlap(out[i], n[i], out[j], n[j])) return set_error(FL_ERR_ALIAS, "logp / loss / loss_sum overlap");
+    if (overlap(out[i], n[i], ws, ws_bytes) || (ref && overlap(out[i], n[i], ref, 4 * S)))
+      return set_error(FL_ERR_ALIAS, "logp / loss / loss_sum overlap ref_logp or the workspace");
+  }
+  return FL_OK;
+}
+
+int preference_check_backward(const fl_preference_desc* d, const fl_batch_desc* b, float grad_scale, void* ws,
+                              size_t ws_bytes) {
+  if (int rc = check_desc(d)) return rc;
+  if (int rc = check_pairs(b)) return rc;
+  if (!std::isfinite(grad_scale)) return set_error(FL_ERR_ARG, "grad_scale is not finite");
+  return check_ws(d, b, ws, ws_bytes);
+}
+
+int preference_forward(const fl_preference_desc* d, const fl_batch_desc* b, const void* logits, long ld,
+                       const int32_t* labels, const float* ref, float* logp, float* loss, float* loss_sum, void* ws,
+                       hipStream_t s) {
+  const PrefWs w = carve(b->total_tokens, d->vocab, (char*)ws);
+  if (d->dtype == FL_BF16)
+    return forward(d, b, (const bf16*)logits, ld, labels, ref, logp, loss, loss_sum, w, s);
+  return forward(d, b, (const float*)logits, ld, labels, ref, logp, loss, loss_sum, w, s);
+}
+
+int preference_gradient(const fl_preference_desc* d, const fl_batch_desc* b, const void* logits, long ld,
+                        const int32_t* labels, float grad_scale, void* dlogits, long ldd, int width, void* ws,
+                        hipStream_t s) {
+  const PrefWs w = carve(b->total_tokens, d->vocab, (char*)ws);
+  if (d->dtype == FL_BF16)
+    return gradient(d, b->total_tokens, (const bf16*)logits, ld, labels, grad_scale, (bf16*)dlogits, ldd, width, w,
+                    s);
+  return gradient(d, b->total_tokens, (const float*)logits, ld, labels, grad_scale, (float*)dlogits, ldd, width, w, s);
+}
+
+}  // namespace flglm
+
+extern "C" {
+
+int fl_preference_workspace_bytes(const fl_preference_desc* desc, const fl_batch_desc* batch, size_t* bytes) {
+  if (!bytes) return set_error(FL_ERR_NULL, "bytes is NULL");
+  if (int rc = check_desc(desc)) return rc;
+  if (int rc = check_pairs(batch)) return rc;
+  *bytes = carve(batch->total_tokens, desc->vocab, nullptr).total;
+  return FL_OK;
+}
+
+int fl_preference_forward(const fl_preference_desc* desc, const fl_batch_desc* batch, const void* logits, int64_t ld,
+                          const int32_t* labels, const float* ref_logp, float* logp, float* loss, float* loss_sum,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = preference_check(desc, batch, ref_logp, logp, loss, loss_sum, workspace, workspace_bytes)) return rc;
+  if (int rc = check_logits(desc, logits, ld, labels)) return rc;
+  const size_t T = batch->total_tokens, S = batch->num_seqs;
+  const size_t nl = ((T - 1) * ld + desc->vocab) * (desc->dtype == FL_BF16 ? 2 : 4);
+  const void* out[4] = {logp, loss, loss_sum, workspace};
+  const size_t n[4] = {4 * S, 2 * S, 4, workspace_bytes};
+  for (int i = 0; i < 4; ++i)
+    if (overlap(out[i], n[i], logits, nl) || overlap(out[i], n[i], labels, 4 * T))
+      return set_error(FL_ERR_ALIAS, "an output or the workspace overlaps the logits or labels");
+  if (ref_logp && overlap(workspace, workspace_bytes, ref_logp, 4 * S))
+    return set_error(FL_ERR_ALIAS, "the workspace overlaps ref_logp");
+  return preference_forward(desc, batch, logits, ld, labels, ref_logp, logp, loss, loss_sum, workspace,
+                            (hipStream_t)stream);
+}
+
+int fl_preference_backward(const fl_preference_desc* desc, const fl_batch_desc* batch, const void* logits, int64_t ld,
+                           const int32_t* labels, float grad_scale, void* dlogits, int64_t ld_d, int64_t width_d,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = preference_check_backward(desc, batch, grad_scale, workspace, workspace_bytes)) return rc;
+  if (int rc = check_logits(desc, logits, ld, labels)) return rc;
+  if (!dlogits) return set_error(FL_ERR_NULL, "dlogits is NULL");
+  if (!al16(dlogits)) return set_error(FL_ERR_ALIGN, "dlogits is not 16-byte aligned");
+  if (ld_d < desc->vocab || ld_d % 8 || ld_d > (int64_t(1) << 32))
+    return set_error(FL_ERR_SHAPE, "dlogits' row stride must be a multiple of 8, at least vocab and at most 2^32");
+  if (width_d < desc->vocab || width_d % 8 || width_d > ld_d || width_d > (1 << 25))
+    return set_error(FL_ERR_SHAPE, "dlogits' width must be a multiple of 8 in [vocab, its row stride], at most 2^25");
+  const size_t T = batch->total_tokens, E = desc->dtype == FL_BF16 ? 2 : 4;
+  const size_t nl = ((T - 1) * ld + desc->vocab) * E, nd = ((T - 1) * ld_d + width_d) * E;
+  if (overlap(dlogits, nd, logits, nl) && !(dlogits == logits && ld == ld_d))
+    return set_error(FL_ERR_ALIAS, "dlogits overlaps the logits without being them");
+  if (overlap(dlogits, nd, labels, 4 * T) || overlap(dlogits, nd, workspace, workspace_bytes) ||
+      overlap(workspace, workspace_bytes, logits, nl) || overlap(workspace, workspace_bytes, labels, 4 * T))
+    return set_error(FL_ERR_ALIAS, "dlogits or the workspace overlaps another argument");
+  return preference_gradient(desc, batch, logits, ld, labels, grad_scale, dlogits, ld_d, (int)width_d, workspace,
+                             (hipStream_t)stream);
+}
+
+}  // extern "C"

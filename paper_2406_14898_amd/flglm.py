@@ -42,6 +42,11 @@ EXPORTS = (
     "fl_adam_step", "fl_average_replicas",
     "fl_client_create", "fl_client_destroy", "fl_client_workspace_bytes", "fl_embedding_forward",
     "fl_embedding_backward", "fl_lm_head_forward", "fl_lm_head_backward",
+    "fl_preference_workspace_bytes", "fl_preference_forward", "fl_preference_backward",
+    "fl_lm_head_preference_forward", "fl_lm_head_preference_backward",
+    "fl_adapter_workspace_bytes", "fl_adapter_forward", "fl_adapter_backward",
+    "fl_stack_adapter_bytes", "fl_server_stack_forward_adapters", "fl_server_stack_backward_adapters",
+    "fl_grad_norm_workspace_bytes", "fl_grad_norm", "fl_clip_grads",
     "fl_stack_profile", "fl_stack_profile_classes", "fl_stack_profile_read", "fl_profile_class_name",
     "fl_test_gemm", "fl_test_gemm_tiled", "fl_test_gemm_plan",
     "fl_test_linear_backward",
@@ -74,6 +79,27 @@ class fl_batch_desc(ctypes.Structure):
 class fl_client_desc(ctypes.Structure):
     _fields_ = [("vocab", ctypes.c_int64), ("hidden", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("ln_eps", ctypes.c_float)]
+
+
+class fl_preference_desc(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int64), ("dtype", ctypes.c_int32), ("beta", ctypes.c_float),
+                ("label_smoothing", ctypes.c_float)]
+
+
+class fl_adapter_desc(ctypes.Structure):
+    _fields_ = [("num_adapters", ctypes.c_int32), ("rank", ctypes.c_int32), ("in_features", ctypes.c_int32),
+                ("out_features", ctypes.c_int32), ("scale", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+class fl_layer_adapters(ctypes.Structure):
+    """One block's adapters, or (fl_layer_adapter_grads) their gradients."""
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p)]
+
+
+class fl_stack_adapters(ctypes.Structure):
+    _fields_ = [("num_adapters", ctypes.c_int32), ("rank", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("client_adapter", ctypes.POINTER(ctypes.c_int32)), ("layers", ctypes.POINTER(fl_layer_adapters)),
+                ("grads", ctypes.POINTER(fl_layer_adapters))]
 
 
 class fl_layer_params(ctypes.Structure):
@@ -121,6 +147,27 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "fl_embedding_backward": [vp, P(i32), i64, vp, vp, vp, sz, vp],
         "fl_lm_head_forward": [vp, vp, vp, vp, vp, P(i32), i64, vp, vp, vp, sz, vp],
         "fl_lm_head_backward": [vp, vp, vp, vp, i64, ctypes.c_float, vp, vp, vp, vp, vp, sz, vp],
+        "fl_preference_workspace_bytes": [P(fl_preference_desc), P(fl_batch_desc), P(sz)],
+        "fl_preference_forward": [P(fl_preference_desc), P(fl_batch_desc), vp, i64, vp, vp, vp, vp, vp, vp, sz, vp],
+        "fl_preference_backward": [P(fl_preference_desc), P(fl_batch_desc), vp, i64, vp, ctypes.c_float, vp, i64, i64, vp,
+                                   sz, vp],
+        "fl_lm_head_preference_forward": [vp, P(fl_preference_desc), P(fl_batch_desc), vp, vp, vp, vp, P(i32), vp, vp, vp,
+                                          vp, vp, sz, vp, sz, vp],
+        "fl_lm_head_preference_backward": [vp, P(fl_preference_desc), P(fl_batch_desc), vp, vp, vp, ctypes.c_float, vp,
+                                           vp, vp, vp, vp, sz, vp, sz, vp],
+        "fl_adapter_workspace_bytes": [P(fl_adapter_desc), P(fl_batch_desc), P(sz)],
+        "fl_adapter_forward": [P(fl_adapter_desc), P(fl_batch_desc), P(i32), vp, i64, vp, vp, vp, i64, vp, i64, vp, vp, sz,
+                               vp],
+        "fl_adapter_backward": [P(fl_adapter_desc), P(fl_batch_desc), P(i32), vp, i64, vp, i64, vp, vp, vp, vp, i64, vp,
+                                i64, vp, vp, vp, sz, vp],
+        "fl_stack_adapter_bytes": [vp, P(fl_batch_desc), P(fl_stack_adapters), P(sz)],
+        "fl_server_stack_forward_adapters": [vp, P(fl_batch_desc), P(fl_layer_params), P(fl_stack_adapters), vp, vp, vp,
+                                             ctypes.c_int, vp, sz, vp, sz, vp],
+        "fl_server_stack_backward_adapters": [vp, P(fl_batch_desc), P(fl_layer_params), P(fl_layer_grads),
+                                              P(fl_stack_adapters), vp, vp, vp, vp, ctypes.c_int, vp, sz, vp, sz, vp],
+        "fl_grad_norm_workspace_bytes": [i32, P(i64), P(sz)],
+        "fl_grad_norm": [i32, i32, P(vp), P(i64), ctypes.c_double, vp, vp, sz, vp],
+        "fl_clip_grads": [i32, i32, P(vp), P(vp), P(i64), vp, vp],
         "fl_stack_profile": [vp, ctypes.c_int],
         "fl_stack_profile_classes": [vp, ctypes.c_uint32],
         "fl_stack_profile_read": [vp, ctypes.c_int, P(i64), P(ctypes.c_double), P(ctypes.c_double),
@@ -177,6 +224,30 @@ def _ptr(t) -> Optional[int]:
     if getattr(t, "is_cuda", True) is False:
         raise FlglmError(FL_ERR_ARG, f"tensor on {t.device}: the library takes device memory")
     return t.data_ptr()
+
+
+def matrix(t, rows: int, width: int, dtype, name: str):
+    """(tensor, row stride) of a [rows, width] argument whose rows may lie apart
+    in memory; refused where the library would read something else."""
+    if t is None:
+        return None, 0
+    tensors((name, t, (rows, width), dtype), rows_apart=True)
+    return t, (t.stride(0) if rows > 1 else width)
+
+
+def tensors(*args, rows_apart: bool = False) -> None:
+    """Checks (name, tensor or None, shape, dtype) arguments: on the current
+    device, of that shape and type, contiguous (rows_apart: each row is)."""
+    import torch
+    for name, t, shape, dtype in args:
+        if t is None:
+            continue
+        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+            raise FlglmError(FL_ERR_ARG, f"{name} is on {t.device}, not on the current device")
+        if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+            raise FlglmError(FL_ERR_ARG, f"{name} is {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
+        if not (t.is_contiguous() or (rows_apart and t.stride(1) == 1)):
+            raise FlglmError(FL_ERR_ARG, f"{name} is not contiguous")
 
 
 def _stream(s) -> Optional[int]:
@@ -372,6 +443,147 @@ def fl_lm_head_backward(handle: int, h, w, T: int, grad_scale: float, dh, dw, wo
     _check(load().fl_lm_head_backward(handle, _ptr(h), _ptr(ln_g), _ptr(w), T, grad_scale, _ptr(dh), _ptr(dln_g),
                                       _ptr(dln_b), _ptr(dw), _ptr(workspace),
                                       workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def fl_preference_workspace_bytes(desc: fl_preference_desc, batch: BatchDesc) -> int:
+    n = ctypes.c_size_t()
+    _check(load().fl_preference_workspace_bytes(ctypes.byref(desc), ctypes.byref(batch.desc), ctypes.byref(n)))
+    return n.value
+
+
+def fl_preference_forward(desc: fl_preference_desc, batch: BatchDesc, logits, ld: int, labels, ref_logp, logp, loss,
+                          loss_sum, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(load().fl_preference_forward(ctypes.byref(desc), ctypes.byref(batch.desc), _ptr(logits), ld, _ptr(labels),
+                                        _ptr(ref_logp), _ptr(logp), _ptr(loss), _ptr(loss_sum), _ptr(workspace),
+                                        workspace_bytes, _stream(stream)))
+
+
+def fl_preference_backward(desc: fl_preference_desc, batch: BatchDesc, logits, ld: int, labels, grad_scale: float,
+                           dlogits, ld_d: int, width_d: int, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(load().fl_preference_backward(ctypes.byref(desc), ctypes.byref(batch.desc), _ptr(logits), ld, _ptr(labels),
+                                         grad_scale, _ptr(dlogits), ld_d, width_d, _ptr(workspace),
+                                         workspace_bytes, _stream(stream)))
+
+
+def fl_lm_head_preference_forward(handle: int, desc: fl_preference_desc, batch: BatchDesc, h, w, labels, ref_logp, logp,
+                                  loss, loss_sum, workspace, pref_workspace, stream=None, ln_g=None, ln_b=None) -> None:
+    arr, p = _host_i32(labels)
+    if arr.shape != (batch.total_tokens,):
+        raise FlglmError(FL_ERR_ARG, f"{arr.size} labels for {batch.total_tokens} tokens")
+    _check(load().fl_lm_head_preference_forward(
+        handle, ctypes.byref(desc), ctypes.byref(batch.desc), _ptr(h), _ptr(ln_g), _ptr(ln_b), _ptr(w), p,
+        _ptr(ref_logp), _ptr(logp), _ptr(loss), _ptr(loss_sum), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _ptr(pref_workspace),
+        pref_workspace.numel() * pref_workspace.element_size(), _stream(stream)))
+
+
+def fl_lm_head_preference_backward(handle: int, desc: fl_preference_desc, batch: BatchDesc, h, w, grad_scale: float, dh,
+                                   dw, workspace, pref_workspace, stream=None, ln_g=None, dln_g=None,
+                                   dln_b=None) -> None:
+    _check(load().fl_lm_head_preference_backward(
+        handle, ctypes.byref(desc), ctypes.byref(batch.desc), _ptr(h), _ptr(ln_g), _ptr(w), grad_scale, _ptr(dh),
+        _ptr(dln_g), _ptr(dln_b), _ptr(dw), _ptr(workspace), workspace.numel() * workspace.element_size(),
+        _ptr(pref_workspace), pref_workspace.numel() * pref_workspace.element_size(), _stream(stream)))
+
+
+def fl_adapter_workspace_bytes(desc: fl_adapter_desc, batch: BatchDesc) -> int:
+    n = ctypes.c_size_t()
+    _check(load().fl_adapter_workspace_bytes(ctypes.byref(desc), ctypes.byref(batch.desc), ctypes.byref(n)))
+    return n.value
+
+
+def _client_adapter(client_adapter, batch: BatchDesc):
+    arr, p = _host_i32(client_adapter)
+    if arr.shape != (batch.desc.num_clients,):
+        raise FlglmError(FL_ERR_ARG, f"{arr.size} adapter slots for {batch.desc.num_clients} clients")
+    return arr, p
+
+
+def fl_adapter_forward(desc: fl_adapter_desc, batch: BatchDesc, client_adapter, x, ldx: int, a, b, base, ld_base: int, y,
+                       ldy: int, v, workspace, workspace_bytes: int, stream=None) -> None:
+    arr, p = _client_adapter(client_adapter, batch)
+    _check(load().fl_adapter_forward(ctypes.byref(desc), ctypes.byref(batch.desc), p, _ptr(x), ldx, _ptr(a), _ptr(b),
+                                     _ptr(base), ld_base, _ptr(y), ldy, _ptr(v), _ptr(workspace), workspace_bytes,
+                                     _stream(stream)))
+
+
+def fl_adapter_backward(desc: fl_adapter_desc, batch: BatchDesc, client_adapter, dy, ld_dy: int, x, ldx: int, a, b, v,
+                        dres, ld_dres: int, dx, ld_dx: int, da, db, workspace, workspace_bytes: int,
+                        stream=None) -> None:
+    arr, p = _client_adapter(client_adapter, batch)
+    _check(load().fl_adapter_backward(ctypes.byref(desc), ctypes.byref(batch.desc), p, _ptr(dy), ld_dy, _ptr(x), ldx,
+                                      _ptr(a), _ptr(b), _ptr(v), _ptr(dres), ld_dres, _ptr(dx), ld_dx, _ptr(da),
+                                      _ptr(db), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def stack_adapters(num_adapters: int, rank: int, scale: float, batch: BatchDesc, client_adapter, layers,
+                   grads=None) -> fl_stack_adapters:
+    """layers / grads: one dict of device tensors "a", "b" a block.  The record
+    keeps the host arrays that it points at."""
+    arr, p = _client_adapter(client_adapter, batch)
+    la = (fl_layer_adapters * len(layers))(*[fl_layer_adapters(_ptr(d["a"]), _ptr(d["b"])) for d in layers])
+    ga = None
+    if grads is not None:
+        ga = (fl_layer_adapters * len(grads))(*[fl_layer_adapters(_ptr(d["a"]), _ptr(d["b"])) for d in grads])
+    r = fl_stack_adapters(num_adapters, rank, scale, p, la, ga)
+    r._keep = (arr, la, ga)
+    return r
+
+
+def fl_stack_adapter_bytes(handle: int, batch: BatchDesc, adapters: fl_stack_adapters) -> int:
+    n = ctypes.c_size_t()
+    _check(load().fl_stack_adapter_bytes(handle, ctypes.byref(batch.desc), ctypes.byref(adapters), ctypes.byref(n)))
+    return n.value
+
+
+def fl_server_stack_forward_adapters(handle: int, batch: BatchDesc, layers: Sequence[fl_layer_params],
+                                     adapters: fl_stack_adapters, x, y, saved, recompute: bool, workspace,
+                                     workspace_bytes: int, adapter_workspace, adapter_workspace_bytes: int,
+                                     stream=None) -> None:
+    arr = (fl_layer_params * len(layers))(*layers)
+    _check(load().fl_server_stack_forward_adapters(
+        handle, ctypes.byref(batch.desc), arr, ctypes.byref(adapters), _ptr(x), _ptr(y), _ptr(saved), int(recompute),
+        _ptr(workspace), workspace_bytes, _ptr(adapter_workspace), adapter_workspace_bytes, _stream(stream)))
+
+
+def fl_server_stack_backward_adapters(handle: int, batch: BatchDesc, layers: Sequence[fl_layer_params],
+                                      grads: Sequence[fl_layer_grads], adapters: fl_stack_adapters, x, saved, dy, dx,
+                                      recompute: bool, workspace, workspace_bytes: int, adapter_workspace,
+                                      adapter_workspace_bytes: int, stream=None) -> None:
+    pa = (fl_layer_params * len(layers))(*layers)
+    ga = (fl_layer_grads * len(grads))(*grads)
+    _check(load().fl_server_stack_backward_adapters(
+        handle, ctypes.byref(batch.desc), pa, ga, ctypes.byref(adapters), _ptr(x), _ptr(saved), _ptr(dy), _ptr(dx),
+        int(recompute), _ptr(workspace), workspace_bytes, _ptr(adapter_workspace), adapter_workspace_bytes,
+        _stream(stream)))
+
+
+def _sizes(sizes):
+    return (ctypes.c_int64 * len(sizes))(*sizes)
+
+
+def _pointers(tensors):
+    return (ctypes.c_void_p * len(tensors))(*[_ptr(t) for t in tensors])
+
+
+def fl_grad_norm_workspace_bytes(sizes) -> int:
+    n = ctypes.c_size_t()
+    _check(load().fl_grad_norm_workspace_bytes(len(sizes), _sizes(sizes), ctypes.byref(n)))
+    return n.value
+
+
+def fl_grad_norm(dtype: int, grads, sizes, max_norm: float, norm_coef, workspace, workspace_bytes: int,
+                 stream=None) -> None:
+    """grads: device tensors (or addresses); sizes: their element counts."""
+    _check(load().fl_grad_norm(dtype, len(grads), _pointers(grads), _sizes(sizes), max_norm, _ptr(norm_coef),
+                               _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def fl_clip_grads(dtype: int, grads, out, sizes, norm_coef, stream=None) -> None:
+    if len(out) != len(grads):
+        raise FlglmError(FL_ERR_ARG, f"{len(out)} outputs for {len(grads)} gradients")
+    _check(load().fl_clip_grads(dtype, len(grads), _pointers(grads), _pointers(out), _sizes(sizes), _ptr(norm_coef),
+                                _stream(stream)))
 
 
 def fl_stack_profile(handle: int, enable: bool) -> None:

@@ -38,6 +38,7 @@ class ParamArena:
         self.exp_avg_sq = torch.zeros(max(n, _ALIGN), **z)
         self.compute = torch.zeros(max(n, _ALIGN), dtype=torch.bfloat16, device=device) if bf16_copy else None
         self.step_count = 0
+        self._norm: Optional[GradNorm] = None
 
     def _view(self, buf, name):
         off, shape = self.offsets[name]
@@ -69,12 +70,63 @@ class ParamArena:
         if self.compute is not None:
             self.compute.copy_(self.master)
 
+    def clip_grad_norm(self, max_norm: float, stream=None):
+        """Scales the gradients in place so that their global norm is at most
+        max_norm; returns the norm before (device fp32 [1])."""
+        if self._norm is None or self._norm.grads[0] is not self.grad:
+            self._norm = GradNorm([self.grad])
+        return self._norm.clip(max_norm, stream=stream)
+
     def adam_step(self, lr: float = 2e-2, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                   zero_grad: bool = True, stream=None) -> None:
         """One Adam step over every tensor of the arena (time step advances)."""
         self.step_count += 1
         F.fl_adam_step(self.master, self.grad, self.exp_avg, self.exp_avg_sq, self.compute, self.n, self.step_count,
                        lr, beta1, beta2, eps, zero_grad, stream)
+
+
+class GradNorm:
+    """Global norm of a list of gradients (fp32 or bf16, all of one type) and
+    their clipping.  Owns the workspace and the result: calls of one GradNorm
+    on different streams, or graphs captured from it, must not overlap."""
+
+    def __init__(self, grads: Sequence):
+        import torch
+        if not grads:
+            raise F.FlglmError(F.FL_ERR_ARG, "no gradients")
+        self.grads = list(grads)
+        self.dtype = self.grads[0].dtype
+        if self.dtype not in (torch.float32, torch.bfloat16):
+            raise F.FlglmError(F.FL_ERR_ARG, f"gradients are fp32 or bf16, not {self.dtype}")
+        for i, g in enumerate(self.grads):
+            F.tensors((f"gradient {i}", g, g.shape, self.dtype))
+        self.sizes = [g.numel() for g in self.grads]
+        device = self.grads[0].device
+        self.workspace = torch.empty(F.fl_grad_norm_workspace_bytes(self.sizes), dtype=torch.uint8, device=device)
+        self.result = torch.empty(2, dtype=torch.float32, device=device)  # norm, coefficient
+
+    def norm(self, max_norm: float = float("inf"), stream=None):
+        """Device fp32 [1]: the norm of the gradients' present values.  The
+        coefficient min(1, max_norm / (norm + 1e-6)) is left in result[1]."""
+        F.fl_grad_norm(F.FL_F32 if self._f32 else F.FL_BF16, self.grads, self.sizes, max_norm, self.result,
+                       self.workspace, self.workspace.numel(), stream)
+        return self.result[:1]
+
+    def clip(self, max_norm: float, out: Optional[Sequence] = None, stream=None):
+        """Gradients times the coefficient, into `out` (tensors like the
+        gradients; None: in place); returns the norm before."""
+        norm = self.norm(max_norm, stream)
+        if out is not None:
+            for i, (o, g) in enumerate(zip(out, self.grads)):
+                F.tensors((f"output {i}", o, g.shape, self.dtype))
+        F.fl_clip_grads(F.FL_F32 if self._f32 else F.FL_BF16, self.grads, self.grads if out is None else out, self.sizes,
+                        self.result, stream)
+        return norm
+
+    @property
+    def _f32(self) -> bool:
+        import torch
+        return self.dtype == torch.float32
 
 
 def average(arenas: Sequence[ParamArena], stream=None) -> None:

@@ -49,14 +49,26 @@ class ServerStack:
         return saved, ws
 
     def forward(self, batch: F.BatchDesc, params: Sequence[Dict], x, y, saved, workspace, recompute: bool = False,
-                stream=None) -> None:
+                stream=None, adapters=None) -> None:
+        """adapters: the batch's StackAdapters."""
         layers = [F.layer_params(p) for p in params]
+        if adapters is not None:
+            F.fl_server_stack_forward_adapters(self.handle, batch, layers, adapters.record, x, y, saved, recompute,
+                                               workspace, workspace.numel(), adapters.workspace,
+                                               adapters.workspace.numel(), stream)
+            return
         F.fl_server_stack_forward(self.handle, batch, layers, x, y, saved, recompute, workspace,
                                   workspace.numel(), stream)
 
     def backward(self, batch: F.BatchDesc, params: Sequence[Dict], grads: Sequence[Dict], x, saved, dy, dx,
-                 workspace, recompute: bool = False, stream=None) -> None:
+                 workspace, recompute: bool = False, stream=None, adapters=None) -> None:
+        """adapters: the StackAdapters (with gradients) of the forward."""
         layers = [F.layer_params(p) for p in params]
         gl = [F.layer_grads(g) for g in grads]
+        if adapters is not None:
+            F.fl_server_stack_backward_adapters(self.handle, batch, layers, gl, adapters.record, x, saved, dy, dx,
+                                                recompute, workspace, workspace.numel(), adapters.workspace,
+                                                adapters.workspace.numel(), stream)
+            return
         F.fl_server_stack_backward(self.handle, batch, layers, gl, x, saved, dy, dx, recompute, workspace,
                                    workspace.numel(), stream)

@@ -1,0 +1,307 @@
+"""The preference loss and its gradient against a plain float64 computation.
+
+Bounds: a row's sum of exponentials is off by E = (8 + 2^-24 4 (max - min)) steps
+of 2^-23 (each exponential by its argument's rounding and its own, the sums by a
+few steps more, as their parts are added in a tree); a label's log-probability
+by that E; a sequence's by the sum over its labelled rows, and a last rounding.
+"""
+
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+from paper_2406_14898_amd import BatchDesc, ClientHead, PreferenceLoss  # noqa: E402
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+u = 2.0 ** -23
+
+
+def _oracle(x, V, labels, cu, ref, beta, eps, scale):
+    """float64: (logp, loss, dlogits, per-row relative error of a probability)."""
+    x = x[:, :V].double().cpu().numpy()
+    S = len(cu) - 1
+    logp, err = np.zeros(S), np.zeros(x.shape[0])
+    with np.errstate(all="ignore"):
+        top = x.max(1)
+        e = np.exp(x - top[:, None])
+        s = e.sum(1)
+        low = np.where(np.isfinite(x), x, np.inf).min(1)
+        err = (16 + math.log2(V) + 2 * (top - low)) * u
+        for q in range(S):
+            for t in range(cu[q], cu[q + 1]):
+                if 0 <= labels[t] < V:
+                    logp[q] += x[t, labels[t]] - top[t] - math.log(s[t])
+        d = logp - (0 if ref is None else ref.double().cpu().numpy())
+        z = beta * (d[0::2] - d[1::2])
+        soft = lambda w: np.maximum(w, 0) + np.log1p(np.exp(-np.abs(w)))  # noqa: E731
+        loss = (1 - eps) * soft(-z) + (eps * soft(z) if eps else 0)
+        k = beta * (eps / (1 + np.exp(-z)) - (1 - eps) / (1 + np.exp(z)))
+        g = np.zeros_like(x)
+        for q in range(S):
+            for t in range(cu[q], cu[q + 1]):
+                if 0 <= labels[t] < V:
+                    g[t] = -e[t] / s[t]
+                    g[t, labels[t]] += 1
+                    g[t] *= scale * (k[q // 2] if q % 2 == 0 else -k[q // 2])
+    return logp, loss, g, err, z
+
+
+def _check(x, V, labels, cu, ref, beta, eps, scale, dt, logp, loss, total, dl):
+    labels = labels.cpu().numpy()
+    wl, wloss, wg, err, z = _oracle(x, V, labels, cu, ref, beta, eps, scale)
+    S = len(cu) - 1
+    el = np.array([sum(err[t] for t in range(cu[q], cu[q + 1]) if 0 <= labels[t] < V) for q in range(S)])
+    got = lambda t: t.double().cpu().numpy()  # noqa: E731
+    assert (np.abs(got(logp) - wl) <= el + 2.0 ** -24 * np.abs(wl)).all(), np.abs(got(logp) - wl).max()
+    ez = beta * (el[0::2] + el[1::2]) + 1e-14 * (1 + np.abs(z))  # the loss's slope by z is at most 1 in size
+    assert (np.abs(got(loss) - wloss) <= ez + 2.0 ** -24 * wloss).all()
+    assert abs(float(total) - wloss.sum()) <= ez.sum() + 2.0 ** -23 * wloss.sum()
+    if dl is None:
+        return
+    # a slope beta (eps s(z) - (1 - eps) s(-z)) moves by at most beta / 4 times z's error
+    pair = np.repeat(np.searchsorted(cu, np.arange(x.shape[0]), side="right")[:, None] - 1, 1, 1)[:, 0] // 2
+    p = np.abs(wg)
+    bound = scale * beta * ez[pair][:, None] / 4 * 1.0 + p * (2 * err[:, None] + 4 * u) + HALF[dt] * p
+    # at the label 1 - p cancels: p's error counts whole
+    rows = np.nonzero((labels >= 0) & (labels < V))[0]
+    bound[rows, labels[rows]] += scale * beta * (2 * err[rows] + 4 * u)
+    off = np.abs(got(dl)[:, :V] - wg)
+    tiny = 2.0 ** -126  # results under the smallest normal number may be flushed
+    assert (off <= bound + tiny).all(), (off / (bound + tiny)).max()
+    assert (got(dl)[:, V:] == 0).all()
+    assert (got(dl)[~((labels >= 0) & (labels < V))] == 0).all()
+
+
+def _case(lens, V, dt, seed=0, pad=0, std=2.0, unlabelled=0.3, empty=(), masked=0, clients=None):
+    g = torch.Generator().manual_seed(seed)
+    cu = [0]
+    for n in lens:
+        cu.append(cu[-1] + n)
+    T = cu[-1]
+    x = (torch.randn((T, V + pad), generator=g) * std).to(DT[dt])
+    labels = torch.randint(0, V - masked, (T,), generator=g, dtype=torch.int32)
+    labels[torch.rand(T, generator=g) < unlabelled] = -100
+    for q in empty:
+        labels[cu[q]:cu[q + 1]] = -1
+    if masked:
+        x[:, V - masked:V] = -math.inf
+    ref = torch.randn(len(lens), generator=g) * 3 - 4.0 * torch.tensor(lens)
+    csp = clients or [0, len(lens)]
+    return x.cuda(), labels.cuda(), cu, ref.cuda(), BatchDesc(cu, csp)
+
+
+def _run(x, labels, cu, ref, batch, V, dt, beta=0.2, eps=0.0, scale=0.5, inplace=False, backward=True):
+    op = PreferenceLoss(V, dt, beta, eps)
+    ws = op.workspace(batch)
+    ws.fill_(255)
+    logp, loss, total = op.outputs(batch)
+    keep = x.clone()
+    print(f"[preference] T={cu[-1]} pairs={len(cu) // 2} V={V} {dt}", flush=True)
+    op.forward(batch, x, labels, ref, logp, loss, total, ws)
+    dl = None
+    if backward:
+        dl = x if inplace else torch.full_like(x, 5.0)
+        op.backward(batch, x, labels, scale, dl, ws)
+    return keep, logp, loss, total, dl
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,V,kw", [
+    ([1, 1], 8, {}), ([1, 2], 16, dict(unlabelled=0.0)), ([5, 9, 14, 3], 1000, {}),
+    ([70, 3, 1, 40], 8200, dict(pad=24)), ([33, 64], 4096, dict(empty=(0,))), ([9, 6], 256, dict(empty=(0, 1))),
+    ([12, 20, 7, 8], 1000, dict(masked=40, pad=24)), ([300, 257], 2056, dict(std=8.0)),
+    ([2, 3, 4, 5, 6, 7], 520, dict(clients=[0, 2, 6])),
+])
+def test_loss_and_gradient_match_float64(lens, V, kw, dt):
+    x, labels, cu, ref, batch = _case(lens, V, dt, **kw)
+    _check(x, V, labels, cu, ref, 0.2, 0.0, 0.5, dt, *_run(x, labels, cu, ref, batch, V, dt)[1:])
+
+
+@pytest.mark.parametrize("beta,eps,scale,with_ref", [(0.1, 0.0, 1.0, True), (0.1, 0.2, 0.125, True),
+                                                     (1.0, 0.5, 1.0, False), (0.01, 0.1, 3.0, False)])
+def test_parameters(beta, eps, scale, with_ref):
+    x, labels, cu, ref, batch = _case([21, 30, 17, 40], 1000, "f32", seed=3)
+    ref = ref if with_ref else None
+    r = _run(x, labels, cu, ref, batch, 1000, "f32", beta, eps, scale)
+    _check(x, 1000, labels, cu, ref, beta, eps, scale, "f32", *r[1:])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_gradient_in_place_and_padded_columns(dt):
+    x, labels, cu, ref, batch = _case([30, 22], 1000, dt, pad=24)
+    apart = _run(x.clone(), labels, cu, ref, batch, 1000, dt)
+    inside = _run(x.clone(), labels, cu, ref, batch, 1000, dt, inplace=True)
+    assert all(torch.equal(p, q) for p, q in zip(apart[1:], inside[1:]))
+    # a view that ends at vocab: what lies behind its rows stays
+    buf = torch.full((52, 1040), 7.0, dtype=DT[dt], device="cuda")
+    op = PreferenceLoss(1000, dt, 0.2, 0.0)
+    ws, out = op.workspace(batch), op.outputs(batch)
+    op.forward(batch, x, labels, ref, *out, ws)
+    op.backward(batch, x, labels, 0.5, buf[:, 16:1016], ws)
+    assert torch.equal(buf[:, 16:1016], apart[4][:, :1000])
+    assert (buf[:, :16] == 7).all() and (buf[:, 1016:] == 7).all()
+
+
+def test_labels_past_the_vocabulary_are_none():
+    x, labels, cu, ref, batch = _case([10, 12], 1000, "f32")
+    other = labels.clone()
+    other[labels < 0] = 1000
+    other[labels == -100] = 2 ** 30
+    a, b = (_run(x, t, cu, ref, batch, 1000, "f32") for t in (labels, other))
+    assert all(torch.equal(p, q) for p, q in zip(a[1:], b[1:]))
+
+
+def test_more_pairs_than_one_launch_takes():
+    rng = np.random.default_rng(1)
+    lens = [int(n) for n in rng.integers(1, 6, 2 * 300)]
+    x, labels, cu, ref, batch = _case(lens, 64, "f32", clients=[0, 100, 600])
+    _check(x, 64, labels, cu, ref, 0.2, 0.1, 0.5, "f32", *_run(x, labels, cu, ref, batch, 64, "f32", eps=0.1)[1:])
+
+
+def test_full_vocabulary():
+    x, labels, cu, ref, batch = _case([40, 25], 130528, "bf16")
+    _check(x, 130528, labels, cu, ref, 0.2, 0.0, 0.5, "bf16", *_run(x, labels, cu, ref, batch, 130528, "bf16")[1:])
+
+
+def test_a_label_without_probability():
+    """A preferred label at a masked id: l = -inf, the loss infinite, the slope
+    -beta, every gradient finite; on the rejected side the loss is 0."""
+    x, labels, cu, ref, batch = _case([4, 5], 64, "f32", unlabelled=0.0)
+    for row, want in ((1, math.inf), (6, 0.0)):
+        y = x.clone()
+        y[row, int(labels[row])] = -math.inf
+        _, logp, loss, total, dl = _run(y, labels, cu, ref, batch, 64, "f32")
+        assert float(logp[0 if row < 4 else 1]) == -math.inf and float(loss) == want == float(total)
+        assert torch.isfinite(dl).all()
+        if row < 4:  # slope -beta: scale beta (softmax - onehot)
+            p = torch.softmax(y[0].double(), 0)
+            p[int(labels[0])] -= 1
+            assert torch.allclose(dl[0].double(), 0.5 * 0.2 * p, rtol=0, atol=64 * u)
+        else:
+            assert (dl == 0).all()
+
+
+def test_nan_reaches_its_own_pair_only():
+    x, labels, cu, ref, batch = _case([4, 5, 6, 3], 1000, "f32", unlabelled=0.0)
+    _, logp, loss, _, dl = _run(x, labels, cu, ref, batch, 1000, "f32")
+    for j in (0, 513, 999):
+        y = x.clone()
+        y[2, :] = -math.inf if j == 513 else y[2, :]
+        y[2, j] = math.nan
+        _, logp2, loss2, total2, dl2 = _run(y, labels, cu, ref, batch, 1000, "f32")
+        assert math.isnan(float(logp2[0])) and math.isnan(float(loss2[0])) and math.isnan(float(total2))
+        assert torch.equal(logp2[1:], logp[1:]) and torch.equal(loss2[1:], loss[1:]) and torch.equal(dl2[9:], dl[9:])
+
+
+def test_results_repeat_and_replay():
+    x, labels, cu, ref, batch = _case([50, 61, 20, 33], 8200, "bf16")
+    op = PreferenceLoss(8200, "bf16", 0.1, 0.1)
+    ws, ws2 = op.workspace(batch), op.workspace(batch)
+    a, b = (op.outputs(batch) + (torch.empty_like(x),) for _ in range(2))
+
+    def both(o, w):
+        op.forward(batch, x, labels, ref, *o[:3], w)
+        op.backward(batch, x, labels, 0.25, o[3], w)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both(a, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(a, ws)
+    for i in range(4):
+        x.copy_(torch.randn_like(x))
+        both(b, ws2)
+        for t in a:
+            t.fill_(3)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(a, b)), i
+
+
+def test_offsets_past_32_bits():
+    """17000 rows of the full vocabulary: the last lie past 2^31 elements."""
+    V, T = 130528, 17000
+    batch = BatchDesc([0, 8500, T], [0, 2])
+    x = torch.empty((T, V), dtype=torch.bfloat16, device="cuda")
+    rows = [0, 8499, 8500, 16450, T - 1]
+    labels = torch.full((T,), -100, dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(0)
+    for i, t in enumerate(rows):
+        x[t] = torch.randn(V, generator=g, device="cuda").bfloat16()
+        labels[t] = 1000 * i + 7
+    op = PreferenceLoss(V, "bf16", 0.5, 0.0)
+    ws = op.workspace(batch)
+    logp, loss, total = op.outputs(batch)
+    op.forward(batch, x, labels, None, logp, loss, total, ws)
+    op.backward(batch, x, labels, 1.0, x, ws)
+    few = BatchDesc([0, 2, 5], [0, 2])
+    y = torch.empty((5, V), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(0)
+    for i in range(5):
+        y[i] = torch.randn(V, generator=g, device="cuda").bfloat16()
+    ws2, out = op.workspace(few), op.outputs(few)
+    op.forward(few, y, labels[rows].contiguous(), None, *out, ws2)
+    # the two batches split a row's sum differently
+    assert torch.allclose(logp, out[0], rtol=0, atol=40 * 64 * u) and torch.allclose(loss, out[1], rtol=0, atol=1e-3)
+    dl = torch.empty_like(y)
+    op.backward(few, y, labels[rows].contiguous(), 1.0, dl, ws2)
+    assert torch.allclose(x[rows].float(), dl.float(), rtol=2.0 ** -6, atol=1e-9)
+    assert (x[16449] == 0).all() and (x[T - 2] == 0).all()
+
+
+def test_gradient_against_differences():
+    """The kernel's own losses at x +- h d and x +- h d / 2, extrapolated."""
+    x, labels, cu, ref, batch = _case([7, 9, 5, 6], 64, "f32", std=1.0)
+    d = torch.randn(x.shape, generator=torch.Generator().manual_seed(2)).cuda()
+    _, _, loss, _, dl = _run(x, labels, cu, ref, batch, 64, "f32", eps=0.1, scale=1.0)
+    f = lambda y: float(_run(y, labels, cu, ref, batch, 64, "f32", eps=0.1, backward=False)[2].double().sum())  # noqa: E731
+    h = 0.25
+    wide, half = (f(x + h * d) - f(x - h * d)) / (2 * h), (f(x + h / 2 * d) - f(x - h / 2 * d)) / h
+    diff = (4 * half - wide) / 3
+    rounding = 8 * 2.0 ** -24 * float(loss.sum()) / h + 1e-4
+    got = float((dl.double() * d.double()).sum())
+    assert abs(got - diff) <= abs(wide - half) + rounding, (got, diff, wide, half)
+
+
+@pytest.mark.parametrize("dt,final_ln", [("bf16", True), ("f32", False), ("f32", True)])
+def test_head_with_the_preference_loss(dt, final_ln):
+    """ClientHead: the loss from the hidden states, with gradients of the hidden
+    states, the vocabulary layer and the final LayerNorm, against autograd in
+    float64 (bf16: logits and their gradient are rounded on the way)."""
+    V, H = 1000, 256
+    _, labels, cu, ref, batch = _case([19, 30, 8, 11], V, dt, seed=5)
+    g = torch.Generator().manual_seed(6)
+    f = lambda *s, std=1.0, mean=0.0: (torch.randn(s, generator=g) * std + mean).to(DT[dt]).cuda()  # noqa: E731
+    h, w = f(cu[-1], H), f(V, H, std=0.05)
+    ln = (f(H, std=0.1, mean=1.0), f(H, std=0.1)) if final_ln else (None, None)
+    head, op = ClientHead(V, H, dt), PreferenceLoss(V, dt, 0.1, 0.05)
+    ws, pws = head.workspace(cu[-1]), op.workspace(batch)
+    logp, loss, total = op.outputs(batch)
+    host = labels.cpu().numpy()
+    head.preference_forward(op, batch, h, w, host, ref, logp, loss, total, ws, pws, ln_g=ln[0], ln_b=ln[1])
+    dh, dw = torch.empty_like(h), torch.zeros((V, H), device="cuda")
+    dl = [torch.zeros(H, device="cuda") for _ in range(2)] if final_ln else [None, None]
+    head.preference_backward(op, batch, h, w, 0.5, dh, dw, ws, pws, ln_g=ln[0], dln_g=dl[0], dln_b=dl[1])
+    leaves = [t.double().requires_grad_(True) for t in (h, w) + (ln if final_ln else ())]
+    y = leaves[0]
+    if final_ln:
+        y = torch.nn.functional.layer_norm(y, (H,), leaves[2], leaves[3], 1e-5)
+    lp = torch.log_softmax(y @ leaves[1].t(), 1)
+    tok = torch.where(labels >= 0, lp.gather(1, labels.clamp(min=0).long()[:, None])[:, 0], 0.0)
+    seq = torch.stack([tok[a:b].sum() for a, b in zip(cu, cu[1:])])
+    z = 0.1 * ((seq - ref.double())[0::2] - (seq - ref.double())[1::2])
+    want = 0.95 * torch.nn.functional.softplus(-z) + 0.05 * torch.nn.functional.softplus(z)
+    grads = torch.autograd.grad(0.5 * want.sum(), leaves)
+    tol = {"bf16": 2e-2, "f32": 1e-4}[dt]
+    rel = lambda p, q: float((p.double() - q).norm() / q.norm())  # noqa: E731
+    assert rel(logp, seq.detach()) < tol and rel(loss, want.detach()) < tol
+    for got, q in zip([dh, dw] + dl, grads):
+        assert rel(got, q) < tol
+    head.close()
