@@ -369,7 +369,8 @@ int fl_lm_head_preference_backward(fl_client* client, const fl_preference_desc* 
  * over all rows of all clients that share slot s.  v stays in fp32 between
  * the two products, and products with it keep its digits (bf16 inputs give
  * the results of an fp32 computation rounded once).
- * Row strides are in elements, multiples of 8, at least the row's width. */
+ * Row strides are in elements, multiples of 8, at least the row's width and at
+ * most 2^24. */
 typedef struct fl_adapter_desc {
   int32_t num_adapters;  /* slots n, 1 .. 2^16 */
   int32_t rank;          /* r: a multiple of 8 in [8, 64] */

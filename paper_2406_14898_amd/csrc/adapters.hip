@@ -44,18 +44,23 @@ constexpr int kSegs = 128;     // segments a launch (2 KB of kernel arguments, 3
 constexpr int kTile = 64;      // forward: rows of a tile
 constexpr int kUpCols = 256;   // forward: columns of a workgroup of `up`
 constexpr int kStep = 32;      // backward: rows of a step
-constexpr int kBwdCols = 128 * kWaves;  // backward: columns of a workgroup
+constexpr int64_t kMaxStride = 1 << 24;  // elements between rows
+constexpr int kInCols = 128 * kWaves;  // backward: columns of a workgroup of bwd_in
 
 struct Segs {
   int32_t row0[kSegs], rows[kSegs], slot[kSegs];
   int32_t step0[kSegs + 1];  // first tile / step of each, within the launch
   int count;
 };
-// Slabs: runs of `steps` steps of one slot, over its segments in row order.
-struct Slabs {
-  int32_t slot[kSegs], step0[kSegs + 1], slab0[kSegs + 1];
-  int32_t part0[kSegs];  // first partial sum of a slot of several slabs; -1: one slab, which adds to the output itself
-  int count, steps;
+// Backward: which steps belong to which slot (segments sorted by slot), and how
+// they are shared out: worker i takes steps [base + i share, base + (i + 1)
+// share), whatever slots these are of, and hands on its sums where the slot
+// changes.  A slot that one worker has alone goes straight to dA / dB; else its
+// workers' sums are parts, part0 + (worker - the slot's first).
+struct Slots {
+  int32_t slot[kSegs], step0[kSegs + 1], part0[kSegs];
+  int count, base, share;
+  __device__ __host__ int worker(int step) const { return (step - base) / share; }
 };
 
 __device__ __forceinline__ int find(const int32_t* first, int count, int v) {
@@ -66,6 +71,14 @@ __device__ __forceinline__ int find(const int32_t* first, int count, int v) {
     else hi = mid;
   }
   return lo;
+}
+
+// Element `off` behind element `base` of p.  A uniform base and a 32-bit offset
+// of the lane's own cost one address register for any number of rows (strides
+// are at most 2^24 elements: kMaxStride).
+template <typename T>
+__device__ __forceinline__ T* at(T* p, long base, uint32_t off) {
+  return (T*)((uintptr_t)(p + base) + off * (uint32_t)sizeof(T));
 }
 
 // How many parts of T an fp32 factor is held in, under a T and an fp32 result.
@@ -98,12 +111,7 @@ template <typename T, int RP> struct Up {
   __device__ static __forceinline__ int rank(int s, int g) { return chunk(s, g) % (RP / 8) * 8; }
 };
 
-template <typename T>
-__device__ __forceinline__ frag_t<T> zero_frag() {
-  Vec8<T> z;
-  z.zero();
-  return z.frag();
-}
+__device__ __forceinline__ int up_col(int q, int mm) { return 32 * (q >> 1) + 8 * (mm >> 2) + 4 * (q & 1) + (mm & 3); }
 
 // ---------------------------------------------------------------------------
 // Forward
@@ -132,26 +140,42 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // 32-column steps, dealt to the splits and then to the waves in turn
-  const int nk = (in + 31) / 32, stride = gridDim.y * kWaves;
-  for (int k = blockIdx.y * kWaves + w; k < nk; k += stride) {
-    const int c = 32 * k + 8 * g;
-    Vec8<T> av[RT];
+  // 64-column steps, dealt to the splits and then to the waves in turn; a lane
+  // takes columns 16 g .. 16 g + 15 of a step (a wave whole 128-byte lines), as
+  // two products of 32 slots
+  const int nk = (in + 63) / 64, stride = gridDim.y * kWaves;
+  auto step = [&](int k, int count) {
+    const int c = 64 * k + 16 * g;
+    Vec8<T> av[2][RT], xv[2][4];
 #pragma unroll
-    for (int j = 0; j < RT; ++j) {
-      if (16 * j + m < r && c < in) av[j].load(as + (long)(16 * j + m) * in + c);
-      else av[j].zero();
-    }
+    for (int i = 0; i < 4; ++i)
+      if (i < count) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (i >= tiles) break;
-      Vec8<T> xv;
-      if (16 * i + m < rows && c < in) xv.load(x + (row0 + 16 * i + m) * ldx + c);
-      else xv.zero();
+        for (int h = 0; h < 2; ++h) {
+          if (16 * i + m < rows && c + 8 * h < in) xv[h][i].load(x + (row0 + 16 * i + m) * ldx + c + 8 * h);
+          else xv[h][i].zero();
+        }
+      }
 #pragma unroll
-      for (int j = 0; j < RT; ++j) acc[i][j] = mma16(xv.frag(), av[j].frag(), acc[i][j]);
-    }
-  }
+    for (int j = 0; j < RT; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (16 * j + m < r && c + 8 * h < in) av[h][j].load(as + (long)(16 * j + m) * in + c + 8 * h);
+        else av[h][j].zero();
+      }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < count) {
+#pragma unroll
+          for (int j = 0; j < RT; ++j) acc[i][j] = mma16(xv[h][i].frag(), av[h][j].frag(), acc[i][j]);
+        }
+  };
+  if (tiles == 4)
+    for (int k = blockIdx.y * kWaves + w; k < nk; k += stride) step(k, 4);
+  else
+    for (int k = blockIdx.y * kWaves + w; k < nk; k += stride) step(k, tiles);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -202,13 +226,14 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
   }
   __syncthreads();
   // a wave's 64 columns: column tile q, first-operand row mm is column
-  // 16 (mm / 4) + 4 q + mm % 4, so that a lane's results are 16 neighbours
+  // 32 (q / 2) + 8 (mm / 4) + 4 (q % 2) + mm % 4, so that tiles 2h and 2h + 1
+  // give a lane eight neighbours, and its row's four lanes 32
   const int c0 = cb * kUpCols + 64 * w;
   if (c0 >= out_features) return;
   frag_t<T> wf[4][U::weights];
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const int col = c0 + 16 * (m >> 2) + 4 * q + (m & 3);
+    const int col = c0 + up_col(q, m);
 #pragma unroll
     for (int s = 0; s < U::weights; ++s) {
       const int rk = U::rank(s, g);
@@ -218,16 +243,16 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
       wf[q][s] = f.frag();
     }
   }
-  const int col = c0 + 16 * g;
+  const int col = c0 + 8 * g;
+  const uint32_t off_b = m * (uint32_t)ldb + col, off_y = m * (uint32_t)ldy + col;
 #pragma unroll
   for (int i = 0; i < kTile / 16; ++i) {
     if (16 * i >= rows) break;
-    const long row = row0 + 16 * i + m;
     const bool in_row = 16 * i + m < rows;
     Vec8<T> bs[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      if (base && in_row && col + 8 * h < out_features) bs[h].load(base + row * ldb + col + 8 * h);
+      if (base && in_row && col + 32 * h < out_features) bs[h].load(at(base, (row0 + 16 * i) * ldb, off_b) + 32 * h);
       else bs[h].zero();
     }
     f32x4 acc[4];
@@ -250,7 +275,7 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
       for (int e = 0; e < 8; ++e) o[e] = bs[h].get(e) + scale * acc[2 * h + (e >> 2)][e & 3];
       Vec8<T> ov;
       ov.set(o);
-      if (in_row && col + 8 * h < out_features) ov.store(y + row * ldy + col + 8 * h);
+      if (in_row && col + 32 * h < out_features) ov.store(at(y, (row0 + 16 * i) * ldy, off_y) + 32 * h);
     }
   }
 }
@@ -259,18 +284,9 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
 // Backward
 // ---------------------------------------------------------------------------
 
-// Walks the steps of a slab.
+// Walks the steps [step, end) of one worker and slot.
 struct Walk {
-  int slot, step, end, seg, part;
-  __device__ __forceinline__ Walk(const Segs& t, const Slabs& sl, int slab) {
-    const int k = find(sl.slab0, sl.count, slab);
-    slot = sl.slot[k];
-    const int i = slab - sl.slab0[k];
-    step = sl.step0[k] + i * sl.steps;
-    end = min(sl.step0[k + 1], step + sl.steps);
-    seg = find(t.step0, t.count, step);
-    part = sl.part0[k] < 0 ? -1 : sl.part0[k] + i;
-  }
+  int step, end, seg;
   // The current step's first row and its rows; moves on.
   __device__ __forceinline__ int next(const Segs& t, long* row0) {
     while (step >= t.step0[seg + 1]) ++seg;
@@ -280,6 +296,21 @@ struct Walk {
     return min(kStep, t.rows[seg] - first);
   }
 };
+// Calls run(walk, slot, part) for each slot of a worker's steps; part: where its
+// sums go, -1 for the output itself.
+template <typename F>
+__device__ __forceinline__ void for_slots(const Segs& t, const Slots& sl, int worker, F&& run) {
+  int step = sl.base + worker * sl.share;
+  const int end = min(sl.step0[sl.count], step + sl.share);
+  int k = find(sl.step0, sl.count, step);
+  Walk wk;
+  wk.seg = find(t.step0, t.count, step);
+  for (; step < end; ++k) {
+    wk.step = step;
+    wk.end = step = min(end, sl.step0[k + 1]);
+    run(wk, sl.slot[k], sl.part0[k] < 0 ? -1 : sl.part0[k] + worker - sl.worker(sl.step0[k]));
+  }
+}
 
 // LDS rows of a factor [32 tokens][RP] turned to [part][rank][token].
 constexpr int kTokStride = kStep + 8;
@@ -290,19 +321,19 @@ template <typename T>
 __device__ __forceinline__ void load_tile(Vec8<T> (&xr)[8], const T* x, long ld, long row0, int rows, int c0, int width,
                                           int m, int g) {
   const int c = c0 + 8 * m;
+  const uint32_t off = 8 * g * (uint32_t)ld + c;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if (8 * g + i < rows && c < width) xr[i].load(x + (row0 + 8 * g + i) * ld + c);
+    if (8 * g + i < rows && c < width) xr[i].load(at(x, (row0 + i) * ld, off));
     else xr[i].zero();
   }
 }
 
-// acc[j][q] += X^T W over the tile's 32 rows: columns 8 m + j, ranks 16 q + n.
+// acc[j][q] += X^T W over the tile's 32 rows (xt: the tile turned): columns
+// 8 m + j, ranks 16 q + n.
 template <typename T, int RT>
-__device__ __forceinline__ void outer(f32x4 (&acc)[8][RT], const Vec8<T> (&xr)[8], const T* wt, int m, int g) {
+__device__ __forceinline__ void outer(f32x4 (&acc)[8][RT], const Vec8<T> (&xt)[8], const T* wt, int m, int g) {
   constexpr int NP = Parts<T>::exact;
-  Vec8<T> xt[8];
-  transpose8x8(xr, xt);
 #pragma unroll
   for (int p = 0; p < NP; ++p)
 #pragma unroll
@@ -314,25 +345,67 @@ __device__ __forceinline__ void outer(f32x4 (&acc)[8][RT], const Vec8<T> (&xr)[8
     }
 }
 
-// dv parts (one for each column block) and dB (or its slab's part).
+// Waves of a bwd_out workgroup: as many as registers and LDS let run on a CU
+// (two a SIMD, one for ranks past 32 and in fp32), because every workgroup
+// along the columns leaves a part of dv.
+template <typename T, int RT> struct OutWaves { static constexpr int n = sizeof(T) == 2 && RT <= 2 ? 8 : 4; };
+
+// LDS traffic of this wave before the barrier is done, and every wave is here.
+// (Global loads and stores stay in flight: __syncthreads would wait for them.)
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// One step's factor [32][r] on its way to LDS: loaded a step ahead.
+template <int RP, int NT> struct Factor {
+  static constexpr int n = (kStep * RP + NT - 1) / NT;
+  float f[n];
+  __device__ __forceinline__ void load(const float* v, long row0, int rows, int r, int tid) {
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const int e = tid + i * NT, row = e / RP, c = e - row * RP;
+      f[i] = (row < rows && c < r) ? v[(row0 + row) * r + c] : 0.f;
+    }
+  }
+};
+
+// dv parts (one for each column block) and dB (or its slab's part).  A step:
+// the tile (loaded during the step before) goes to the wave's own LDS in rows,
+// and through registers, turned, into dB; dv reads the rows back and leaves its
+// result in their place; one barrier, and the waves' results are added.
 template <typename T, int RT>
-__global__ void __launch_bounds__(kThreads) bwd_out_kernel(Segs t, Slabs sl, const T* dy, long lddy, const T* b,
-                                                           const float* v, int r, int out_features, float scale,
-                                                           float* dv_part, long total_rows, float* db,
-                                                           float* db_part) {
+__global__ void __launch_bounds__((64 * OutWaves<T, RT>::n))
+    bwd_out_kernel(Segs t, Slots sl, const T* dy, long lddy, const T* b, const float* v, int r, int out_features,
+                   float scale, float* dv_part, long total_rows, float* db, float* db_part) {
+  constexpr int NW = OutWaves<T, RT>::n, NT = 64 * NW;
   constexpr int RP = 16 * RT, NP = Parts<T>::exact;
   constexpr int kRow = 128 + 16 / (int)sizeof(T);
-  __shared__ __align__(16) T wt[NP * RP * kTokStride];
-  __shared__ __align__(16) T tile[kWaves][kStep][kRow];
-  __shared__ float dvs[kWaves][kStep][RP + 1];
-  const int cols = (out_features + kBwdCols - 1) / kBwdCols;
-  const int slab = blockIdx.x / cols, cb = blockIdx.x - slab * cols;
-  Walk wk(t, sl, slab);
-  if (wk.slot < 0) return;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-  const int c0 = cb * kBwdCols + 128 * w;
-  const T* bs = b + (long)wk.slot * out_features * r;
+  constexpr int kDv = RP + 1;
+  static_assert(kStep * kDv * 4 <= kStep * kRow * (int)sizeof(T), "dv fits its tile's place");
+  __shared__ __align__(16) T wt[2][NP * RP * kTokStride];
+  __shared__ __align__(16) T tile[2][NW][kStep * kRow];
+  const int cols = (out_features + 128 * NW - 1) / (128 * NW);
+  const int worker = blockIdx.x / cols, cb = blockIdx.x - worker * cols;
+  for_slots(t, sl, worker, [&](Walk& wk, int slot, int part) {
+  int tid = threadIdx.x;
+  settle(tid);  // addresses are formed anew for each slot: held across slots, they would not fit the registers
+  const int lane = tid & 63, w = tid >> 6, m = lane & 15, g = lane >> 4;
+  const int c0 = cb * 128 * NW + 128 * w;
+  long row0, row1 = 0;
+  int rows = wk.next(t, &row0), rows1 = 0;
+  Vec8<T> xr[8], xn[8], xt[8];
+  Factor<RP, NT> vn;
+  load_tile(xr, dy, lddy, row0, rows, c0, out_features, m, g);
+  vn.load(v, row0, rows, r, tid);
+  auto stage = [&](T* dst) {
+#pragma unroll
+    for (int i = 0; i < Factor<RP, NT>::n; ++i) {
+      const int e = tid + i * NT, row = e / RP, c = e - row * RP;
+      float f = vn.f[i];
+#pragma unroll
+      for (int p = 0; p < NP; ++p) dst[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
+    }
+  };
   // B as the second operand of dv = dy B: rank 16 q + m, columns 32 k + 8 g ..
+  const T* bs = b + (long)slot * out_features * r;
   frag_t<T> bf[4][RT];
 #pragma unroll
   for (int k = 0; k < 4; ++k)
@@ -351,50 +424,61 @@ __global__ void __launch_bounds__(kThreads) bwd_out_kernel(Segs t, Slabs sl, con
   for (int j = 0; j < 8; ++j)
 #pragma unroll
     for (int q = 0; q < RT; ++q) acc[j][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-  while (wk.step < wk.end) {
-    long row0;
-    const int rows = wk.next(t, &row0);
-    Vec8<T> xr[8];
-    load_tile(xr, dy, lddy, row0, rows, c0, out_features, m, g);
-    for (int i = threadIdx.x; i < kStep * RP; i += kThreads) {
-      const int row = i / RP, c = i - row * RP;
-      float f = row < rows && c < r ? v[(row0 + row) * r + c] : 0.f;
-#pragma unroll
-      for (int p = 0; p < NP; ++p) wt[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
+  stage(wt[0]);
+  lds_barrier();
+  for (int buf = 0;; buf ^= 1) {
+    const bool more = wk.step < wk.end;
+    if (more) {  // in flight until the next step begins
+      rows1 = wk.next(t, &row1);
+      load_tile(xn, dy, lddy, row1, rows1, c0, out_features, m, g);
+      vn.load(v, row1, rows1, r, tid);
     }
+    T* mine = tile[buf][w];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) xr[i].store(&tile[w][8 * g + i][8 * m]);
-    __syncthreads();
-    outer<T, RT>(acc, xr, wt, m, g);
+    for (int i = 0; i < 8; ++i) xr[i].store(mine + (8 * g + i) * kRow + 8 * m);
+    transpose8x8(xr, xt);
+    __builtin_amdgcn_wave_barrier();
+    outer<T, RT>(acc, xt, wt[buf], m, g);
+    f32x4 d[2][RT];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      f32x4 d[RT];
 #pragma unroll
-      for (int q = 0; q < RT; ++q) d[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int q = 0; q < RT; ++q) d[h][q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         Vec8<T> f;
-        f.load(&tile[w][16 * h + m][32 * k + 8 * g]);
+        f.load(mine + (16 * h + m) * kRow + 32 * k + 8 * g);
 #pragma unroll
-        for (int q = 0; q < RT; ++q) d[q] = mma16(f.frag(), bf[k][q], d[q]);
+        for (int q = 0; q < RT; ++q) d[h][q] = mma16(f.frag(), bf[k][q], d[h][q]);
       }
+    }
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");  // the rows are read: dv takes their place
+    float* dvs = (float*)mine;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int q = 0; q < RT; ++q)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) dvs[w][16 * h + 4 * g + e][16 * q + m] = d[q][e];
-    }
-    __syncthreads();
+        for (int e = 0; e < 4; ++e) dvs[(16 * h + 4 * g + e) * kDv + 16 * q + m] = d[h][q][e];
+    if (more) stage(wt[buf ^ 1]);
+    lds_barrier();
     float* dst = dv_part + ((long)cb * total_rows + row0) * r;
-    for (int i = threadIdx.x; i < rows * r; i += kThreads) {
+    for (int i = tid; i < rows * r; i += NT) {
       const int row = i / r, c = i - row * r;
-      float s = dvs[0][row][c];
+      float s = 0.f;
 #pragma unroll
-      for (int q = 1; q < kWaves; ++q) s += dvs[q][row][c];
+      for (int q = 0; q < NW; ++q) s += ((const float*)tile[buf][q])[row * kDv + c];
       dst[i] = scale * s;
     }
+    if (!more) break;
+    row0 = row1;
+    rows = rows1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) xr[i] = xn[i];
   }
-  const bool add = wk.part < 0;
-  float* dst = add ? db + (long)wk.slot * out_features * r : db_part + (long)wk.part * out_features * r;
+  const bool add = part < 0;
+  float* dst = add ? db + (long)slot * out_features * r : db_part + (long)part * out_features * r;
 #pragma unroll
   for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -409,114 +493,182 @@ __global__ void __launch_bounds__(kThreads) bwd_out_kernel(Segs t, Slabs sl, con
         *p = (add ? *p : 0.f) + scale * acc[j][q][e];
       }
     }
+  });
 }
 
-// dx and dA (or its slab's part); dv: the sum of `parts` column blocks' parts.
+// dv: the column blocks' parts added, into the first of them.
+__global__ void __launch_bounds__(kThreads) dv_sum_kernel(float* dv_part, int parts, long n) {
+  const long e = ((long)blockIdx.x * kThreads + threadIdx.x) * 4;
+  if (e >= n) return;  // n is a multiple of 8
+  f32x4 s = *reinterpret_cast<const f32x4*>(dv_part + e);
+#pragma unroll 4
+  for (int q = 1; q < parts; ++q) s += *reinterpret_cast<const f32x4*>(dv_part + q * n + e);
+  *reinterpret_cast<f32x4*>(dv_part + e) = s;
+}
+
+// dx and dA (or its slab's part).
 template <typename T, int RT>
-__global__ void __launch_bounds__(kThreads) bwd_in_kernel(Segs t, Slabs sl, const T* x, long ldx, const T* a,
-                                                          const float* dv_part, int parts, long total_rows, int r,
-                                                          int in, const T* dres, long lddr, T* dx, long lddx,
-                                                          float* da, float* da_part) {
+__global__ void __launch_bounds__(kThreads, (OutWaves<T, RT>::n / 4)) bwd_in_kernel(Segs t, Slots sl, const T* x, long ldx, const T* a,
+                                                          const float* dv, int r, int in, const T* dres, long lddr,
+                                                          T* dx, long lddx, float* da, float* da_part) {
   constexpr int RP = 16 * RT, NP = Parts<T>::exact;
   using U = Up<T, RP>;
-  __shared__ __align__(16) T wt[NP * RP * kTokStride];
-  __shared__ __align__(16) T wr[kStep][U::stride];
-  const int cols = (in + kBwdCols - 1) / kBwdCols;
-  const int slab = blockIdx.x / cols, cb = blockIdx.x - slab * cols;
-  Walk wk(t, sl, slab);
-  const int slot = wk.slot;
+  __shared__ __align__(16) T wt[2][NP * RP * kTokStride];
+  __shared__ __align__(16) T wr[2][kStep * U::stride];
+  constexpr bool kTurned = sizeof(T) == 2;
+  constexpr int kTurnedRow = RP + 8;
+  __shared__ __align__(16) T aw[kTurned ? kInCols * kTurnedRow : 8];
+  const int cols = (in + kInCols - 1) / kInCols;
+  const int worker = blockIdx.x / cols, cb = blockIdx.x - worker * cols;
+  for_slots(t, sl, worker, [&](Walk& wk, int slot, int part) {
+  int tid = threadIdx.x;
+  settle(tid);  // as in bwd_out
+  const int lane = tid & 63, w = tid >> 6, m = lane & 15, g = lane >> 4;
+  const int c0 = cb * kInCols + 128 * w;
   const bool live = slot >= 0;
   if (!live && (!dx || dx == dres)) return;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-  const int c0 = cb * kBwdCols + 128 * w;
-  // A as the first operand of dx = dv A, columns as in `up`
-  frag_t<T> wf[2][4][U::weights];
+  long row0, row1 = 0;
+  int rows = wk.next(t, &row0), rows1 = 0;
+  Vec8<T> xr[8], xt[8];
+  Factor<RP, kThreads> vn;
+  auto stage = [&](T* turned, T* in_rows) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+    for (int i = 0; i < Factor<RP, kThreads>::n; ++i) {
+      const int e = tid + i * kThreads, row = e / RP, c = e - row * RP;
+      float f = vn.f[i], f2 = f;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int col = c0 + 64 * h + 16 * (m >> 2) + 4 * q + (m & 3);
+      for (int p = 0; p < NP; ++p) turned[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
 #pragma unroll
-      for (int s = 0; s < U::weights; ++s) {
-        float f[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int rk = U::rank(s, g) + e;
-          f[e] = live && dx && col < in && rk < r ? to_f32(a[((long)slot * r + rk) * in + col]) : 0.f;
-        }
-        wf[h][q][s] = pack8(f, (T*)nullptr);
-      }
+      for (int p = 0; p < U::parts; ++p) in_rows[row * U::stride + p * RP + c] = split(f2, (T*)nullptr);
     }
+  };
+  if (live) {
+    load_tile(xr, x, ldx, row0, rows, c0, in, m, g);
+    vn.load(dv, row0, rows, r, tid);
+  }
+  // A as the first operand of dx = dv A, columns as in `up`: bf16, turned to
+  // [column][rank] in LDS (in registers it would cost a second wave a SIMD);
+  // fp32, in registers (it would not fit LDS)
+  frag_t<T> wf[kTurned ? 1 : 2][4][U::weights];
+  if constexpr (!kTurned) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int col = c0 + 64 * h + up_col(q, m);
+#pragma unroll
+        for (int s = 0; s < U::weights; ++s) {
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int rk = U::rank(s, g) + e;
+            f[e] = live && dx && col < in && rk < r ? to_f32(a[((long)slot * r + rk) * in + col]) : 0.f;
+          }
+          wf[h][q][s] = pack8(f, (T*)nullptr);
+        }
+      }
+  }
   f32x4 acc[8][RT];
 #pragma unroll
   for (int j = 0; j < 8; ++j)
 #pragma unroll
     for (int q = 0; q < RT; ++q) acc[j][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-  while (wk.step < wk.end) {
-    long row0;
-    const int rows = wk.next(t, &row0);
-    if (live) {
-      Vec8<T> xr[8];
-      load_tile(xr, x, ldx, row0, rows, c0, in, m, g);
-      __syncthreads();  // the step before has read wt and wr
-      for (int i = threadIdx.x; i < kStep * RP; i += kThreads) {
-        const int row = i / RP, c = i - row * RP;
-        float f = 0.f;
-        if (row < rows && c < r) {
-          const float* p = dv_part + (row0 + row) * r + c;
-          f = p[0];
-          for (int q = 1; q < parts; ++q) f += p[(long)q * total_rows * r];
-        }
-        float f2 = f;
+  lds_barrier();  // the slot before has read what LDS holds
+  if (live) {
+    stage(wt[0], wr[0]);
+    if constexpr (kTurned) {
+      for (int i = tid; i < RP * (kInCols / 8); i += kThreads) {
+        const int rk = i / (kInCols / 8), c = 8 * (i - rk * (kInCols / 8));
+        Vec8<T> f;
+        if (rk < r && cb * kInCols + c < in) f.load(a + ((long)slot * r + rk) * in + cb * kInCols + c);
+        else f.zero();
+        const auto e = f.frag();
 #pragma unroll
-        for (int p = 0; p < NP; ++p) wt[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
-#pragma unroll
-        for (int p = 0; p < U::parts; ++p) wr[row][p * RP + c] = split(f2, (T*)nullptr);
+        for (int j = 0; j < 8; ++j) aw[(c + j) * kTurnedRow + rk] = e[j];
       }
-      __syncthreads();
-      outer<T, RT>(acc, xr, wt, m, g);
     }
-    if (!dx) continue;
+  }
+  lds_barrier();
+  const uint32_t off_r = m * (uint32_t)lddr + c0 + 8 * g, off_x = m * (uint32_t)lddx + c0 + 8 * g;
+  for (int buf = 0;; buf ^= 1) {
+    const bool more = wk.step < wk.end;
+    // what this step adds to, then what the next one takes
+    Vec8<T> bs[2][2][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int col = c0 + 64 * h + 16 * g;
-        const long row = row0 + 16 * i + m;
-        const bool in_row = 16 * i + m < rows;
-        Vec8<T> bs[2];
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          if (dres && in_row && col + 8 * u < in) bs[u].load(dres + row * lddr + col + 8 * u);
-          else bs[u].zero();
+          const int col = c0 + 64 * h + 8 * g + 32 * u;
+          if (dx && dres && 16 * i + m < rows && col < in) bs[h][i][u].load(at(dres, (row0 + 16 * i) * lddr, off_r) + 64 * h + 32 * u);
+          else bs[h][i][u].zero();
         }
-        f32x4 d[4];
+    if (live) transpose8x8(xr, xt);
+    if (more) {
+      rows1 = wk.next(t, &row1);
+      if (live) {
+        load_tile(xr, x, ldx, row1, rows1, c0, in, m, g);
+        vn.load(dv, row1, rows1, r, tid);
+      }
+    }
+    if (live) outer<T, RT>(acc, xt, wt[buf], m, g);
+    if (dx) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) d[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < 2; ++i) {
+        Vec8<T> f[U::steps];
         if (live) {
 #pragma unroll
           for (int s = 0; s < U::steps; ++s) {
-            Vec8<T> f;
-            if (U::live(s, g)) f.load(&wr[16 * i + m][8 * U::chunk(s, g)]);
-            else f.zero();
-#pragma unroll
-            for (int q = 0; q < 4; ++q) d[q] = mma16(wf[h][q][s % U::weights], f.frag(), d[q]);
+            if (U::live(s, g)) f[s].load(wr[buf] + (16 * i + m) * U::stride + 8 * U::chunk(s, g));
+            else f[s].zero();
           }
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          float o[8];
+        for (int h = 0; h < 2; ++h) {
+          f32x4 d[4];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] = bs[u].get(e) + d[2 * u + (e >> 2)][e & 3];
-          Vec8<T> ov;
-          ov.set(o);
-          if (in_row && col + 8 * u < in) ov.store(dx + row * lddx + col + 8 * u);
+          for (int q = 0; q < 4; ++q) d[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if (live) {
+            if constexpr (kTurned) {
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int s = 0; s < U::weights; ++s) {
+                  Vec8<T> wv;
+                  wv.load(aw + (128 * w + 64 * h + up_col(q, m)) * kTurnedRow + U::rank(s, g));
+#pragma unroll
+                  for (int p = s; p < U::steps; p += U::weights) d[q] = mma16(wv.frag(), f[p].frag(), d[q]);
+                }
+            } else {
+#pragma unroll
+              for (int s = 0; s < U::steps; ++s)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) d[q] = mma16(wf[h][q][s % U::weights], f[s].frag(), d[q]);
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int col = c0 + 64 * h + 8 * g + 32 * u;
+            float o[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = bs[h][i][u].get(e) + d[2 * u + (e >> 2)][e & 3];
+            Vec8<T> ov;
+            ov.set(o);
+            if (16 * i + m < rows && col < in) ov.store(at(dx, (row0 + 16 * i) * lddx, off_x) + 64 * h + 32 * u);
+          }
         }
       }
+    }
+    if (!more) break;
+    if (live) stage(wt[buf ^ 1], wr[buf ^ 1]);
+    lds_barrier();
+    row0 = row1;
+    rows = rows1;
   }
   if (!live) return;
-  const bool add = wk.part < 0;
-  float* dst = add ? da + (long)slot * r * in : da_part + (long)wk.part * r * in;
+  const bool add = part < 0;
+  float* dst = add ? da + (long)slot * r * in : da_part + (long)part * r * in;
 #pragma unroll
   for (int q = 0; q < RT; ++q) {
     const int k = 16 * q + m;
@@ -536,33 +688,22 @@ __global__ void __launch_bounds__(kThreads) bwd_in_kernel(Segs t, Slabs sl, cons
       o.store(p);
     }
   }
+  });
 }
 
-// out[slot] += the parts of its slabs, in order; n elements a slot.  blockIdx.y:
-// the slot's place in the table; .z: dA or dB.
-__global__ void __launch_bounds__(kThreads) join_kernel(Slabs sl, const float* part_a, float* da, long na,
-                                                        const float* part_b, float* db, long nb) {
-  const int k = blockIdx.y, slot = sl.slot[k], p0 = sl.part0[k];
-  if (slot < 0 || p0 < 0) return;
-  const int count = sl.slab0[k + 1] - sl.slab0[k];
-  const bool is_b = blockIdx.z;
-  const long n = is_b ? nb : na, e = ((long)blockIdx.x * kThreads + threadIdx.x) * 4;
-  if (e >= n) return;
-  const float* src = (is_b ? part_b : part_a) + p0 * n + e;
-  float* dst = (is_b ? db : da) + slot * n + e;
-  Vec4<float> o;
-  o.load(dst);
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < count; ++i) {
-    Vec4<float> f;
-    f.load(src + i * n);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) s[j] += f.get(j);
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) s[j] += o.get(j);
-  o.set(s);
-  o.store(dst);
+// out[slot] += the parts of its workers, in order; n elements a slot.
+// blockIdx.y: the slot's place in the table.
+__global__ void __launch_bounds__(kThreads) join_kernel(Slots sl, const float* part, float* out, long n) {
+  const int k = blockIdx.y, p0 = sl.part0[k];
+  const long e = ((long)blockIdx.x * kThreads + threadIdx.x) * 4;
+  if (p0 < 0 || e >= n) return;
+  const int count = sl.worker(sl.step0[k + 1] - 1) - sl.worker(sl.step0[k]) + 1;
+  const float* src = part + p0 * n + e;
+  f32x4* dst = reinterpret_cast<f32x4*>(out + sl.slot[k] * n + e);
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = 0; i < count; ++i) s += *reinterpret_cast<const f32x4*>(src + i * n);
+  *dst += s;
 }
 
 // ---------------------------------------------------------------------------
@@ -621,17 +762,47 @@ void fill(const std::vector<Run>& runs, size_t* i, int rows_a_step, Segs* t) {
 }
 
 // Forward: workgroups along the reduction of v, for batches whose tiles alone
-// do not fill the chip; every wave has two steps at least.
+// do not fill the chip; every wave has a step at least.
 int splits_of(const fl_adapter_desc* d, const fl_batch_desc* b) {
   const long tiles = b->total_tokens / kTile + b->num_clients;
-  return (int)std::max(1L, std::min<long>({512 / tiles, d->in_features / (32 * kWaves * 2), 16}));
+  return (int)std::max(1L, std::min<long>({512 / tiles, d->in_features / (64 * kWaves), 16}));
 }
-// Backward: steps of a slab.  Long slabs mean few partial sums of dA and dB,
-// short ones many workgroups.
-int slab_steps(const fl_adapter_desc* d, const fl_batch_desc* b) {
-  const long steps = b->total_tokens / kStep + b->num_clients;
-  const long cols = cdiv(std::max(d->in_features, d->out_features), kBwdCols);
-  return (int)std::min(128L, std::max(4L, cdiv(steps * cols, 1024)));
+// Backward: columns of a workgroup of bwd_out (OutWaves).
+long out_cols(const fl_adapter_desc* d) {
+  return cdiv(d->out_features, 128 * (d->dtype == FL_BF16 && d->rank <= 32 ? 8 : 4));
+}
+long in_cols(const fl_adapter_desc* d) { return cdiv(d->in_features, kInCols); }
+// Backward: workers that share the steps, for each block of columns; the chip
+// holds one workgroup of bwd_out a CU, two of bwd_in (one for ranks past 32 and
+// in fp32).
+constexpr long kCus = 256;
+long out_workers(const fl_adapter_desc* d) { return std::max(1L, kCus / out_cols(d)); }
+long in_workers(const fl_adapter_desc* d) {
+  return std::max(1L, kCus * (d->dtype == FL_BF16 && d->rank <= 32 ? 2 : 1) / in_cols(d));
+}
+// Shares the steps from the first of a slot >= first_slot on out among
+// `workers`; returns their number, and the number of parts of slots that
+// several have.
+int share_out(const Segs& t, int first_slot, long workers, Slots* sl, int* parts) {
+  sl->count = 0;
+  sl->base = -1;
+  for (int k = 0; k < t.count; ++k) {
+    if (t.slot[k] < first_slot || (sl->count && sl->slot[sl->count - 1] == t.slot[k])) continue;
+    if (sl->base < 0) sl->base = t.step0[k];
+    sl->slot[sl->count] = t.slot[k];
+    sl->step0[sl->count++] = t.step0[k];
+  }
+  *parts = 0;
+  if (!sl->count) return 0;
+  const int end = t.step0[t.count], steps = end - sl->base;
+  sl->step0[sl->count] = end;
+  sl->share = (int)cdiv(steps, workers);
+  for (int k = 0; k < sl->count; ++k) {
+    const int n = sl->worker(sl->step0[k + 1] - 1) - sl->worker(sl->step0[k]) + 1;
+    sl->part0[k] = n > 1 && sl->slot[k] >= 0 ? *parts : -1;
+    if (sl->part0[k] >= 0) *parts += n;
+  }
+  return (int)cdiv(steps, sl->share);
 }
 
 struct AdapterWs {
@@ -653,11 +824,10 @@ AdapterWs carve(const fl_adapter_desc* d, const fl_batch_desc* b, char* base) {
   w.v_part = take(splits > 1 ? splits * v : 0);
   const size_t fwd = off;
   off = 0;
-  w.dv_part = take(cdiv(d->out_features, kBwdCols) * v);
-  // slots of several slabs have fewer than two slabs for each full one
-  const size_t slabs = 2 * (b->total_tokens / kStep + b->num_clients) / slab_steps(d, b) + 2;
-  w.da_part = take(slabs * d->rank * d->in_features * 4);
-  w.db_part = take(slabs * d->rank * d->out_features * 4);
+  w.dv_part = take(out_cols(d) * v);
+  // a slot of n parts has n - 1 boundaries between workers: n <= 2 (n - 1)
+  w.da_part = take(2 * in_workers(d) * d->rank * d->in_features * 4);
+  w.db_part = take(2 * out_workers(d) * d->rank * d->out_features * 4);
   w.total = std::max(std::max(fwd, off), (size_t)256);
   return w;
 }
@@ -692,8 +862,8 @@ bool overlap(const Mat& a, const Mat& b, size_t T, size_t E) {
 int check_mat(const Mat& m, bool required) {
   if (!m.p) return required ? set_error(FL_ERR_NULL, "a matrix argument is NULL") : FL_OK;
   if (!al16(m.p)) return set_error(FL_ERR_ALIGN, "a matrix argument is not 16-byte aligned");
-  if (m.ld < m.width || m.ld % 8 || m.ld > (int64_t(1) << 32))
-    return set_error(FL_ERR_SHAPE, "a row stride must be a multiple of 8, at least the row's width and at most 2^32");
+  if (m.ld < m.width || m.ld % 8 || m.ld > kMaxStride)
+    return set_error(FL_ERR_SHAPE, "a row stride must be a multiple of 8, at least the row's width and at most 2^24");
   return FL_OK;
 }
 
@@ -770,46 +940,44 @@ int adapter_backward(const fl_adapter_desc* d, const fl_batch_desc* batch, const
   if (int rc = runs_of(batch, client_adapter, true, &runs)) return rc;
   const AdapterWs w = carve(d, batch, (char*)ws);
   const long T = batch->total_tokens;
-  const int steps = slab_steps(d, batch);
   const long na = (long)d->rank * d->in_features, nb = (long)d->rank * d->out_features;
-  const long cols_in = cdiv(d->in_features, kBwdCols), cols_out = cdiv(d->out_features, kBwdCols);
+  const long cols_in = in_cols(d), cols_out = out_cols(d);
   for (size_t i = 0; i < runs.size();) {
     Segs t;
     fill(runs, &i, kStep, &t);
-    Slabs sl;
-    sl.count = 0;
-    sl.steps = steps;
-    int32_t slabs = 0, parts = 0;
-    for (int k = 0; k < t.count; ++k) {
-      if (k && t.slot[k] == t.slot[k - 1]) continue;
-      int last = k;
-      while (last + 1 < t.count && t.slot[last + 1] == t.slot[k]) ++last;
-      const int n = (int)cdiv(t.step0[last + 1] - t.step0[k], steps);
-      sl.slot[sl.count] = t.slot[k];
-      sl.step0[sl.count] = t.step0[k];
-      sl.slab0[sl.count] = slabs;
-      sl.part0[sl.count++] = n > 1 && t.slot[k] >= 0 ? parts : -1;
-      slabs += n;
-      if (n > 1 && t.slot[k] >= 0) parts += n;
-    }
-    sl.slab0[sl.count] = slabs;
-    sl.step0[sl.count] = t.step0[t.count];
+    Slots so, si;
+    int parts_out, parts_in;
+    const int workers_out = share_out(t, 0, out_workers(d), &so, &parts_out);
+    const int workers_in = share_out(t, -1, in_workers(d), &si, &parts_in);
     const int rc = dispatch(d, [&](auto* type, auto rt) {
       using E = std::remove_pointer_t<decltype(type)>;
       constexpr int RT = decltype(rt)::value;
-      hipLaunchKernelGGL((bwd_out_kernel<E, RT>), dim3((unsigned)(slabs * cols_out)), dim3(kThreads), 0, s, t, sl,
-                         (const E*)dy, ld_dy, (const E*)b, v, d->rank, d->out_features, d->scale, w.dv_part, T, db,
-                         w.db_part);
-      if (int e = launch_status()) return e;
-      hipLaunchKernelGGL((bwd_in_kernel<E, RT>), dim3((unsigned)(slabs * cols_in)), dim3(kThreads), 0, s, t, sl,
-                         (const E*)x, ldx, (const E*)a, w.dv_part, (int)cols_out, T, d->rank, d->in_features,
-                         (const E*)dres, ld_dres, (E*)dx, ld_dx, da, w.da_part);
+      static_assert(OutWaves<E, RT>::n == (sizeof(E) == 2 && RT <= 2 ? 8 : 4), "out_cols, in_workers");
+      if (workers_out) {
+        hipLaunchKernelGGL((bwd_out_kernel<E, RT>), dim3((unsigned)(workers_out * cols_out)),
+                           dim3(64 * OutWaves<E, RT>::n), 0, s, t, so, (const E*)dy, ld_dy, (const E*)b, v, d->rank,
+                           d->out_features, d->scale, w.dv_part, T, db, w.db_part);
+        if (int e = launch_status()) return e;
+        if (cols_out > 1) {
+          hipLaunchKernelGGL(dv_sum_kernel, dim3((unsigned)cdiv(T * d->rank, 4 * kThreads)), dim3(kThreads), 0, s,
+                             w.dv_part, (int)cols_out, T * d->rank);
+          if (int e = launch_status()) return e;
+        }
+      }
+      hipLaunchKernelGGL((bwd_in_kernel<E, RT>), dim3((unsigned)(workers_in * cols_in)), dim3(kThreads), 0, s, t, si,
+                         (const E*)x, ldx, (const E*)a, w.dv_part, d->rank, d->in_features, (const E*)dres, ld_dres,
+                         (E*)dx, ld_dx, da, w.da_part);
       return launch_status();
     });
     if (rc) return rc;
-    if (parts) {
-      hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(std::max(na, nb), 4 * kThreads), sl.count, 2), dim3(kThreads),
-                         0, s, sl, w.da_part, da, na, w.db_part, db, nb);
+    if (parts_out) {
+      hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(nb, 4 * kThreads), so.count), dim3(kThreads), 0, s, so,
+                         w.db_part, db, nb);
+      if (int e = launch_status()) return e;
+    }
+    if (parts_in) {
+      hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(na, 4 * kThreads), si.count), dim3(kThreads), 0, s, si,
+                         w.da_part, da, na);
       if (int e = launch_status()) return e;
     }
   }
