@@ -44,7 +44,7 @@ constexpr int kSegs = 128;     // segments a launch (2 KB of kernel arguments, 3
 constexpr int kTile = 64;      // forward: rows of a tile
 constexpr int kUpCols = 256;   // forward: columns of a workgroup of `up`
 constexpr int kStep = 32;      // backward: rows of a step
-constexpr int64_t kMaxStride = 1 << 24;  // elements between rows
+constexpr int64_t kMaxStride = 1 << 22;  // elements between rows: 64 of them span at most 2^30 bytes
 constexpr int kInCols = 128 * kWaves;  // backward: columns of a workgroup of bwd_in
 
 struct Segs {
@@ -55,8 +55,8 @@ struct Segs {
 // Backward: which steps belong to which slot (segments sorted by slot), and how
 // they are shared out: worker i takes steps [base + i share, base + (i + 1)
 // share), whatever slots these are of, and hands on its sums where the slot
-// changes.  A slot that one worker has alone goes straight to dA / dB; else its
-// workers' sums are parts, part0 + (worker - the slot's first).
+// changes: a slot's first worker to dA / dB itself, the others to parts, part0 +
+// (worker - the slot's first) - 1, which join adds.
 struct Slots {
   int32_t slot[kSegs], step0[kSegs + 1], part0[kSegs];
   int count, base, share;
@@ -73,13 +73,42 @@ __device__ __forceinline__ int find(const int32_t* first, int count, int v) {
   return lo;
 }
 
-// Element `off` behind element `base` of p.  A uniform base and a 32-bit offset
-// of the lane's own cost one address register for any number of rows (strides
-// are at most 2^24 elements: kMaxStride).
+// Rows [row0, row0 + rows) of a matrix as a buffer: what lies past the last row
+// reads as zero and is not written, without a branch (which would keep loads
+// from being counted, and so every wait would be for all of them).  A lane
+// whose column does not exist takes the offset kNowhere.  A NULL matrix reads
+// as zero.
+typedef __amdgpu_buffer_rsrc_t Buf;
+constexpr uint32_t kNowhere = 1u << 31;
 template <typename T>
-__device__ __forceinline__ T* at(T* p, long base, uint32_t off) {
-  return (T*)((uintptr_t)(p + base) + off * (uint32_t)sizeof(T));
+__device__ __forceinline__ Buf rows_of(const T* p, long row0, long ld, int rows, int width) {
+  const int bytes = p ? (int)(((rows - 1) * ld + width) * (long)sizeof(T)) : 0;
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(p + row0 * ld), 0, bytes, 0x00020000);
 }
+// Byte offset of a lane's column in its row, kNowhere past the width.
+template <typename T>
+__device__ __forceinline__ uint32_t col_off(int row, long ld, int c, int width) {
+  return c < width ? ((uint32_t)row * (uint32_t)ld + c) * (uint32_t)sizeof(T) : kNowhere;
+}
+__device__ __forceinline__ u32x4 buf_ld16(Buf b, uint32_t off) {
+  return __builtin_amdgcn_raw_buffer_load_b128(b, off, 0, 0);
+}
+__device__ __forceinline__ void buf_ld8(Vec8<bf16>& v, Buf b, uint32_t off) { v.r = buf_ld16(b, off); }
+__device__ __forceinline__ void buf_ld8(Vec8<float>& v, Buf b, uint32_t off) {
+  v.r0 = buf_ld16(b, off);
+  v.r1 = buf_ld16(b, off + 16);
+}
+__device__ __forceinline__ void buf_st8(const Vec8<bf16>& v, Buf b, uint32_t off) {
+  __builtin_amdgcn_raw_buffer_store_b128(v.r, b, off, 0, 0);
+}
+__device__ __forceinline__ void buf_st8(const Vec8<float>& v, Buf b, uint32_t off) {
+  __builtin_amdgcn_raw_buffer_store_b128(v.r0, b, off, 0, 0);
+  __builtin_amdgcn_raw_buffer_store_b128(v.r1, b, off + 16, 0, 0);
+}
+__device__ __forceinline__ float buf_ldf(Buf b, uint32_t off) {
+  return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, off, 0, 0));
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // How many parts of T an fp32 factor is held in, under a T and an fp32 result.
 template <typename T> struct Parts;
@@ -125,8 +154,8 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
   __shared__ float sh[kWaves][kTile][RP + 1];
   const int seg = find(t.step0, t.count, blockIdx.x);
   const int first = (blockIdx.x - t.step0[seg]) * kTile;
-  const int rows = min(kTile, t.rows[seg] - first), slot = t.slot[seg];
-  const long row0 = t.row0[seg] + first;
+  const int rows = uniform(min(kTile, t.rows[seg] - first)), slot = uniform(t.slot[seg]);
+  const long row0 = uniform(t.row0[seg] + first);
   float* out = v + ((long)blockIdx.y * total_rows + row0) * r;
   if (slot < 0) {
     for (int i = threadIdx.x; i < rows * r; i += kThreads) out[i] = 0.f;
@@ -134,7 +163,7 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
   }
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
   const int tiles = (rows + 15) / 16;
-  const T* as = a + (long)slot * r * in;
+  const Buf xb = rows_of(x, row0, ldx, rows, in), ab = rows_of(a, (long)slot * r, in, r, in);
   f32x4 acc[4][RT];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -144,38 +173,50 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
   // takes columns 16 g .. 16 g + 15 of a step (a wave whole 128-byte lines), as
   // two products of 32 slots
   const int nk = (in + 63) / 64, stride = gridDim.y * kWaves;
-  auto step = [&](int k, int count) {
-    const int c = 64 * k + 16 * g;
+  const uint32_t xrow = (uint32_t)ldx * 16 * sizeof(T), arow = (uint32_t)in * 16 * sizeof(T);
+  struct Step {
     Vec8<T> av[2][RT], xv[2][4];
+  };
+  auto load = [&](Step& s, int k, int count) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < count) {
+    for (int h = 0; h < 2; ++h) {
+      const int c = 64 * k + 16 * g + 8 * h;
+      const uint32_t xo = col_off<T>(m, ldx, c, in), ao = col_off<T>(m, in, c, in);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (16 * i + m < rows && c + 8 * h < in) xv[h][i].load(x + (row0 + 16 * i + m) * ldx + c + 8 * h);
-          else xv[h][i].zero();
-        }
-      }
+      for (int i = 0; i < 4; ++i)
+        if (i < count) buf_ld8(s.xv[h][i], xb, xo + i * xrow);
 #pragma unroll
-    for (int j = 0; j < RT; ++j)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (16 * j + m < r && c + 8 * h < in) av[h][j].load(as + (long)(16 * j + m) * in + c + 8 * h);
-        else av[h][j].zero();
-      }
+      for (int j = 0; j < RT; ++j) buf_ld8(s.av[h][j], ab, ao + j * arow);
+    }
+  };
+  auto multiply = [&](Step& s, int count) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (i < count) {
 #pragma unroll
-          for (int j = 0; j < RT; ++j) acc[i][j] = mma16(xv[h][i].frag(), av[h][j].frag(), acc[i][j]);
+          for (int j = 0; j < RT; ++j) acc[i][j] = mma16(s.xv[h][i].frag(), s.av[h][j].frag(), acc[i][j]);
         }
   };
-  if (tiles == 4)
-    for (int k = blockIdx.y * kWaves + w; k < nk; k += stride) step(k, 4);
-  else
-    for (int k = blockIdx.y * kWaves + w; k < nk; k += stride) step(k, tiles);
+  int k = blockIdx.y * kWaves + w;
+  if (tiles == 4) {
+    // two steps in flight in turn (past the last they read zero)
+    Step s0, s1;
+    load(s0, k, 4);
+    for (; k < nk; k += 2 * stride) {
+      load(s1, k + stride, 4);
+      multiply(s0, 4);
+      load(s0, k + 2 * stride, 4);
+      multiply(s1, 4);
+    }
+  } else {
+    Step s0;
+    for (; k < nk; k += stride) {
+      load(s0, k, tiles);
+      multiply(s0, tiles);
+    }
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -204,8 +245,8 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
   const int tile = blockIdx.x / cols, cb = blockIdx.x - tile * cols;
   const int seg = find(t.step0, t.count, tile);
   const int first = (tile - t.step0[seg]) * kTile;
-  const int rows = min(kTile, t.rows[seg] - first), slot = t.slot[seg];
-  const long row0 = t.row0[seg] + first;
+  const int rows = uniform(min(kTile, t.rows[seg] - first)), slot = uniform(t.slot[seg]);
+  const long row0 = uniform(t.row0[seg] + first);
   if (slot < 0 && base == y) return;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
   if (slot >= 0) {
@@ -243,18 +284,14 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
       wf[q][s] = f.frag();
     }
   }
-  const int col = c0 + 8 * g;
-  const uint32_t off_b = m * (uint32_t)ldb + col, off_y = m * (uint32_t)ldy + col;
+  const Buf bb = rows_of(base, row0, ldb, rows, out_features), yb = rows_of(y, row0, ldy, rows, out_features);
+  uint32_t bo[2], yo[2];
 #pragma unroll
-  for (int i = 0; i < kTile / 16; ++i) {
-    if (16 * i >= rows) break;
-    const bool in_row = 16 * i + m < rows;
-    Vec8<T> bs[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (base && in_row && col + 32 * h < out_features) bs[h].load(at(base, (row0 + 16 * i) * ldb, off_b) + 32 * h);
-      else bs[h].zero();
-    }
+  for (int h = 0; h < 2; ++h) {
+    bo[h] = col_off<T>(m, ldb, c0 + 8 * g + 32 * h, out_features);
+    yo[h] = col_off<T>(m, ldy, c0 + 8 * g + 32 * h, out_features);
+  }
+  auto rows16 = [&](int i, Vec8<T> (&bs)[2]) {
     f32x4 acc[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -273,9 +310,25 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
       float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = bs[h].get(e) + scale * acc[2 * h + (e >> 2)][e & 3];
-      Vec8<T> ov;
-      ov.set(o);
-      if (in_row && col + 32 * h < out_features) ov.store(at(y, (row0 + 16 * i) * ldy, off_y) + 32 * h);
+      bs[h].set(o);
+      buf_st8(bs[h], yb, yo[h] + (uint32_t)(16 * i * sizeof(T)) * (uint32_t)ldy);
+    }
+  };
+  auto load16 = [&](int i, Vec8<T> (&bs)[2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) buf_ld8(bs[h], bb, bo[h] + (uint32_t)(16 * i * sizeof(T)) * (uint32_t)ldb);
+  };
+  if (rows > kTile - 16) {
+    Vec8<T> bs[kTile / 16][2];
+#pragma unroll
+    for (int i = 0; i < kTile / 16; ++i) load16(i, bs[i]);
+#pragma unroll
+    for (int i = 0; i < kTile / 16; ++i) rows16(i, bs[i]);
+  } else {
+    for (int i = 0; 16 * i < rows; ++i) {
+      Vec8<T> bs[2];
+      load16(i, bs);
+      rows16(i, bs);
     }
   }
 }
@@ -287,13 +340,24 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
 // Walks the steps [step, end) of one worker and slot.
 struct Walk {
   int step, end, seg;
-  // The current step's first row and its rows; moves on.
-  __device__ __forceinline__ int next(const Segs& t, long* row0) {
-    while (step >= t.step0[seg + 1]) ++seg;
+  int row, left;  // the next step's first row, and the rows from there on in its segment
+  __device__ __forceinline__ void start(const Segs& t) {
     const int first = (step - t.step0[seg]) * kStep;
-    *row0 = t.row0[seg] + first;
-    ++step;
-    return min(kStep, t.rows[seg] - first);
+    row = uniform(t.row0[seg] + first);
+    left = uniform(t.rows[seg] - first);
+  }
+  // The current step's first row and its rows; moves on.
+  __device__ __forceinline__ int next(const Segs& t, int* row0) {
+    const int rows = min(kStep, left);
+    *row0 = row;
+    row += kStep;
+    left -= kStep;
+    if (++step < end && left <= 0) {
+      ++seg;
+      row = uniform(t.row0[seg]);
+      left = uniform(t.rows[seg]);
+    }
+    return rows;
   }
 };
 // Calls run(walk, slot, part) for each slot of a worker's steps; part: where its
@@ -303,12 +367,14 @@ __device__ __forceinline__ void for_slots(const Segs& t, const Slots& sl, int wo
   int step = sl.base + worker * sl.share;
   const int end = min(sl.step0[sl.count], step + sl.share);
   int k = find(sl.step0, sl.count, step);
-  Walk wk;
-  wk.seg = find(t.step0, t.count, step);
   for (; step < end; ++k) {
+    Walk wk;
     wk.step = step;
     wk.end = step = min(end, sl.step0[k + 1]);
-    run(wk, sl.slot[k], sl.part0[k] < 0 ? -1 : sl.part0[k] + worker - sl.worker(sl.step0[k]));
+    wk.seg = find(t.step0, t.count, wk.step);
+    wk.start(t);
+    const int nth = worker - sl.worker(sl.step0[k]);  // of this slot's workers
+    run(wk, uniform(sl.slot[k]), uniform(nth == 0 ? -1 : sl.part0[k] + nth - 1));
   }
 }
 
@@ -318,15 +384,12 @@ constexpr int kTokStride = kStep + 8;
 // One 32-row x 128-column tile of X in a wave's registers: lane (m, g) holds
 // rows 8g .. 8g + 7 at columns 8m .. 8m + 7.
 template <typename T>
-__device__ __forceinline__ void load_tile(Vec8<T> (&xr)[8], const T* x, long ld, long row0, int rows, int c0, int width,
+__device__ __forceinline__ void load_tile(Vec8<T> (&xr)[8], const T* x, long ld, int row0, int rows, int c0, int width,
                                           int m, int g) {
-  const int c = c0 + 8 * m;
-  const uint32_t off = 8 * g * (uint32_t)ld + c;
+  const Buf b = rows_of(x, row0, ld, rows, width);
+  const uint32_t off = col_off<T>(8 * g, ld, c0 + 8 * m, width), row = (uint32_t)ld * sizeof(T);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (8 * g + i < rows && c < width) xr[i].load(at(x, (row0 + i) * ld, off));
-    else xr[i].zero();
-  }
+  for (int i = 0; i < 8; ++i) buf_ld8(xr[i], b, off + i * row);
 }
 
 // acc[j][q] += X^T W over the tile's 32 rows (xt: the tile turned): columns
@@ -346,66 +409,81 @@ __device__ __forceinline__ void outer(f32x4 (&acc)[8][RT], const Vec8<T> (&xt)[8
 }
 
 // Waves of a bwd_out workgroup: as many as registers and LDS let run on a CU
-// (two a SIMD, one for ranks past 32 and in fp32), because every workgroup
-// along the columns leaves a part of dv.
-template <typename T, int RT> struct OutWaves { static constexpr int n = sizeof(T) == 2 && RT <= 2 ? 8 : 4; };
+// (two a SIMD; one in fp32), because every workgroup along the columns leaves
+// a part of dv.
+template <typename T> struct OutWaves { static constexpr int n = sizeof(T) == 2 ? 8 : 4; };
 
 // LDS traffic of this wave before the barrier is done, and every wave is here.
 // (Global loads and stores stay in flight: __syncthreads would wait for them.)
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// One step's factor [32][r] on its way to LDS: loaded a step ahead.
+// One step's factor, `ranks` columns of rows `stride` floats apart, on its way
+// to LDS: loaded a step ahead.
 template <int RP, int NT> struct Factor {
-  static constexpr int n = (kStep * RP + NT - 1) / NT;
+  static_assert(NT % RP == 0, "a thread keeps its rank");
+  static constexpr int n = kStep * RP / NT;
   float f[n];
-  __device__ __forceinline__ void load(const float* v, long row0, int rows, int r, int tid) {
+  __device__ static __forceinline__ int rank(int tid) { return tid % RP; }
+  __device__ static __forceinline__ int row(int tid, int i) { return tid / RP + i * (NT / RP); }
+  __device__ __forceinline__ void load(const float* v, int row0, int rows, int stride, int ranks, int tid) {
+    const Buf b = rows_of(v, row0, stride, rows, ranks);
+    const uint32_t off = col_off<float>(row(tid, 0), stride, rank(tid), ranks);
 #pragma unroll
-    for (int i = 0; i < n; ++i) {
-      const int e = tid + i * NT, row = e / RP, c = e - row * RP;
-      f[i] = (row < rows && c < r) ? v[(row0 + row) * r + c] : 0.f;
-    }
+    for (int i = 0; i < n; ++i) f[i] = buf_ldf(b, off + i * (NT / RP * 4) * (uint32_t)stride);
   }
 };
 
-// dv parts (one for each column block) and dB (or its slab's part).  A step:
-// the tile (loaded during the step before) goes to the wave's own LDS in rows,
-// and through registers, turned, into dB; dv reads the rows back and leaves its
-// result in their place; one barrier, and the waves' results are added.
+// dv parts (one for each column block) and dB (or a part of it), for the ranks
+// [r0, r0 + 16 RT): ranks past 32 are two slices, each with workgroups of its
+// own, because the sums of 64 would leave no registers to overlap anything in.
+// The slices of a tile run eight workgroups apart, so on one XCD and its L2.
+// A step: the tile (loaded during the step before) goes to the wave's own LDS
+// in rows, and through registers, turned, into dB; dv reads the rows back and
+// leaves its result in their place; one barrier, and the waves' results are
+// added.
 template <typename T, int RT>
-__global__ void __launch_bounds__((64 * OutWaves<T, RT>::n))
-    bwd_out_kernel(Segs t, Slots sl, const T* dy, long lddy, const T* b, const float* v, int r, int out_features,
-                   float scale, float* dv_part, long total_rows, float* db, float* db_part) {
-  constexpr int NW = OutWaves<T, RT>::n, NT = 64 * NW;
+__global__ void __launch_bounds__((64 * OutWaves<T>::n))
+    bwd_out_kernel(Segs t, Slots sl, const T* dy, long lddy, const T* b, const float* v, int stride, int out_features,
+                   float scale, float* dv_part, long total_rows, float* db, float* db_part, int groups, int slices) {
+  constexpr int NW = OutWaves<T>::n, NT = 64 * NW;
   constexpr int RP = 16 * RT, NP = Parts<T>::exact;
   constexpr int kRow = 128 + 16 / (int)sizeof(T);
   constexpr int kDv = RP + 1;
   static_assert(kStep * kDv * 4 <= kStep * kRow * (int)sizeof(T), "dv fits its tile's place");
   __shared__ __align__(16) T wt[2][NP * RP * kTokStride];
   __shared__ __align__(16) T tile[2][NW][kStep * kRow];
+  const int group = slices == 1 ? blockIdx.x : (blockIdx.x >> 4) * 8 + (blockIdx.x & 7);
+  if (group >= groups) return;
+  const int r0 = slices == 1 ? 0 : RP * ((blockIdx.x >> 3) & 1), r = min(RP, stride - r0);
+  b += r0;
+  v += r0;
+  dv_part += r0;
+  db += r0;
+  db_part += r0;
   const int cols = (out_features + 128 * NW - 1) / (128 * NW);
-  const int worker = blockIdx.x / cols, cb = blockIdx.x - worker * cols;
+  const int worker = group / cols, cb = group - worker * cols;
   for_slots(t, sl, worker, [&](Walk& wk, int slot, int part) {
   int tid = threadIdx.x;
   settle(tid);  // addresses are formed anew for each slot: held across slots, they would not fit the registers
   const int lane = tid & 63, w = tid >> 6, m = lane & 15, g = lane >> 4;
   const int c0 = cb * 128 * NW + 128 * w;
-  long row0, row1 = 0;
+  int row0, row1 = 0;
   int rows = wk.next(t, &row0), rows1 = 0;
   Vec8<T> xr[8], xn[8], xt[8];
   Factor<RP, NT> vn;
+  vn.load(v, row0, rows, stride, r, tid);
   load_tile(xr, dy, lddy, row0, rows, c0, out_features, m, g);
-  vn.load(v, row0, rows, r, tid);
   auto stage = [&](T* dst) {
 #pragma unroll
     for (int i = 0; i < Factor<RP, NT>::n; ++i) {
-      const int e = tid + i * NT, row = e / RP, c = e - row * RP;
+      const int row = Factor<RP, NT>::row(tid, i), c = Factor<RP, NT>::rank(tid);
       float f = vn.f[i];
 #pragma unroll
       for (int p = 0; p < NP; ++p) dst[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
     }
   };
   // B as the second operand of dv = dy B: rank 16 q + m, columns 32 k + 8 g ..
-  const T* bs = b + (long)slot * out_features * r;
+  const T* bs = b + (long)slot * out_features * stride;
   frag_t<T> bf[4][RT];
 #pragma unroll
   for (int k = 0; k < 4; ++k)
@@ -415,7 +493,7 @@ __global__ void __launch_bounds__((64 * OutWaves<T, RT>::n))
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int c = c0 + 32 * k + 8 * g + e;
-        f[e] = (c < out_features && 16 * q + m < r) ? to_f32(bs[(long)c * r + 16 * q + m]) : 0.f;
+        f[e] = (c < out_features && 16 * q + m < r) ? to_f32(bs[(long)c * stride + 16 * q + m]) : 0.f;
       }
       bf[k][q] = pack8(f, (T*)nullptr);
     }
@@ -430,8 +508,8 @@ __global__ void __launch_bounds__((64 * OutWaves<T, RT>::n))
     const bool more = wk.step < wk.end;
     if (more) {  // in flight until the next step begins
       rows1 = wk.next(t, &row1);
+      vn.load(v, row1, rows1, stride, r, tid);
       load_tile(xn, dy, lddy, row1, rows1, c0, out_features, m, g);
-      vn.load(v, row1, rows1, r, tid);
     }
     T* mine = tile[buf][w];
 #pragma unroll
@@ -463,13 +541,16 @@ __global__ void __launch_bounds__((64 * OutWaves<T, RT>::n))
         for (int e = 0; e < 4; ++e) dvs[(16 * h + 4 * g + e) * kDv + 16 * q + m] = d[h][q][e];
     if (more) stage(wt[buf ^ 1]);
     lds_barrier();
-    float* dst = dv_part + ((long)cb * total_rows + row0) * r;
-    for (int i = tid; i < rows * r; i += NT) {
-      const int row = i / r, c = i - row * r;
+    const Buf dst = rows_of(dv_part + cb * total_rows * stride, row0, stride, rows, r);
+    const uint32_t off = col_off<float>(Factor<RP, NT>::row(tid, 0), stride, Factor<RP, NT>::rank(tid), r);
+#pragma unroll
+    for (int i = 0; i < Factor<RP, NT>::n; ++i) {
+      const int row = Factor<RP, NT>::row(tid, i), c = Factor<RP, NT>::rank(tid);
       float s = 0.f;
 #pragma unroll
       for (int q = 0; q < NW; ++q) s += ((const float*)tile[buf][q])[row * kDv + c];
-      dst[i] = scale * s;
+      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(scale * s), dst, off + i * (NT / RP * 4) * (uint32_t)stride,
+                                            0, 0);
     }
     if (!more) break;
     row0 = row1;
@@ -478,7 +559,7 @@ __global__ void __launch_bounds__((64 * OutWaves<T, RT>::n))
     for (int i = 0; i < 8; ++i) xr[i] = xn[i];
   }
   const bool add = part < 0;
-  float* dst = add ? db + (long)slot * out_features * r : db_part + (long)part * out_features * r;
+  float* dst = (add ? db + (long)slot * out_features * stride : db_part + (long)part * out_features * stride);
 #pragma unroll
   for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -489,7 +570,7 @@ __global__ void __launch_bounds__((64 * OutWaves<T, RT>::n))
       for (int q = 0; q < RT; ++q) {
         const int k = 16 * q + m;
         if (k >= r) continue;
-        float* p = dst + (long)c * r + k;
+        float* p = dst + (long)c * stride + k;
         *p = (add ? *p : 0.f) + scale * acc[j][q][e];
       }
     }
@@ -508,7 +589,7 @@ __global__ void __launch_bounds__(kThreads) dv_sum_kernel(float* dv_part, int pa
 
 // dx and dA (or its slab's part).
 template <typename T, int RT>
-__global__ void __launch_bounds__(kThreads, (OutWaves<T, RT>::n / 4)) bwd_in_kernel(Segs t, Slots sl, const T* x, long ldx, const T* a,
+__global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1)) bwd_in_kernel(Segs t, Slots sl, const T* x, long ldx, const T* a,
                                                           const float* dv, int r, int in, const T* dres, long lddr,
                                                           T* dx, long lddx, float* da, float* da_part) {
   constexpr int RP = 16 * RT, NP = Parts<T>::exact;
@@ -527,14 +608,14 @@ __global__ void __launch_bounds__(kThreads, (OutWaves<T, RT>::n / 4)) bwd_in_ker
   const int c0 = cb * kInCols + 128 * w;
   const bool live = slot >= 0;
   if (!live && (!dx || dx == dres)) return;
-  long row0, row1 = 0;
+  int row0, row1 = 0;
   int rows = wk.next(t, &row0), rows1 = 0;
   Vec8<T> xr[8], xt[8];
   Factor<RP, kThreads> vn;
   auto stage = [&](T* turned, T* in_rows) {
 #pragma unroll
     for (int i = 0; i < Factor<RP, kThreads>::n; ++i) {
-      const int e = tid + i * kThreads, row = e / RP, c = e - row * RP;
+      const int row = Factor<RP, kThreads>::row(tid, i), c = Factor<RP, kThreads>::rank(tid);
       float f = vn.f[i], f2 = f;
 #pragma unroll
       for (int p = 0; p < NP; ++p) turned[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
@@ -543,8 +624,8 @@ __global__ void __launch_bounds__(kThreads, (OutWaves<T, RT>::n / 4)) bwd_in_ker
     }
   };
   if (live) {
+    vn.load(dv, row0, rows, r, r, tid);
     load_tile(xr, x, ldx, row0, rows, c0, in, m, g);
-    vn.load(dv, row0, rows, r, tid);
   }
   // A as the first operand of dx = dv A, columns as in `up`: bf16, turned to
   // [column][rank] in LDS (in registers it would cost a second wave a SIMD);
@@ -589,27 +670,32 @@ __global__ void __launch_bounds__(kThreads, (OutWaves<T, RT>::n / 4)) bwd_in_ker
     }
   }
   lds_barrier();
-  const uint32_t off_r = m * (uint32_t)lddr + c0 + 8 * g, off_x = m * (uint32_t)lddx + c0 + 8 * g;
+  uint32_t ro[2][2], xo[2][2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      ro[h][u] = col_off<T>(m, lddr, c0 + 64 * h + 32 * u + 8 * g, in);
+      xo[h][u] = col_off<T>(m, lddx, c0 + 64 * h + 32 * u + 8 * g, in);
+    }
+  const uint32_t rrow = 16 * sizeof(T) * (uint32_t)lddr, xrow = 16 * sizeof(T) * (uint32_t)lddx;
   for (int buf = 0;; buf ^= 1) {
     const bool more = wk.step < wk.end;
     // what this step adds to, then what the next one takes
+    const Buf rb = rows_of(dx ? dres : nullptr, row0, lddr, rows, in), xb = rows_of(dx, row0, lddx, rows, in);
     Vec8<T> bs[2][2][2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int col = c0 + 64 * h + 8 * g + 32 * u;
-          if (dx && dres && 16 * i + m < rows && col < in) bs[h][i][u].load(at(dres, (row0 + 16 * i) * lddr, off_r) + 64 * h + 32 * u);
-          else bs[h][i][u].zero();
-        }
+        for (int u = 0; u < 2; ++u) buf_ld8(bs[h][i][u], rb, ro[h][u] + i * rrow);
     if (live) transpose8x8(xr, xt);
     if (more) {
       rows1 = wk.next(t, &row1);
       if (live) {
+        vn.load(dv, row1, rows1, r, r, tid);
         load_tile(xr, x, ldx, row1, rows1, c0, in, m, g);
-        vn.load(dv, row1, rows1, r, tid);
       }
     }
     if (live) outer<T, RT>(acc, xt, wt[buf], m, g);
@@ -649,13 +735,11 @@ __global__ void __launch_bounds__(kThreads, (OutWaves<T, RT>::n / 4)) bwd_in_ker
           }
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const int col = c0 + 64 * h + 8 * g + 32 * u;
             float o[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] = bs[h][i][u].get(e) + d[2 * u + (e >> 2)][e & 3];
-            Vec8<T> ov;
-            ov.set(o);
-            if (16 * i + m < rows && col < in) ov.store(at(dx, (row0 + 16 * i) * lddx, off_x) + 64 * h + 32 * u);
+            bs[h][i][u].set(o);
+            buf_st8(bs[h][i][u], xb, xo[h][u] + i * xrow);
           }
         }
       }
@@ -692,18 +776,29 @@ __global__ void __launch_bounds__(kThreads, (OutWaves<T, RT>::n / 4)) bwd_in_ker
 }
 
 // out[slot] += the parts of its workers, in order; n elements a slot.
-// blockIdx.y: the slot's place in the table.
-__global__ void __launch_bounds__(kThreads) join_kernel(Slots sl, const float* part, float* out, long n) {
-  const int k = blockIdx.y, p0 = sl.part0[k];
+// blockIdx.y: the slot's place in the table; .z: dA or dB.
+struct Join {
+  Slots sl;
+  const float* part;
+  float* out;
+  long n;
+};
+__device__ __forceinline__ void join(const Join& j) {
+  const int k = blockIdx.y;
   const long e = ((long)blockIdx.x * kThreads + threadIdx.x) * 4;
-  if (p0 < 0 || e >= n) return;
-  const int count = sl.worker(sl.step0[k + 1] - 1) - sl.worker(sl.step0[k]) + 1;
-  const float* src = part + p0 * n + e;
-  f32x4* dst = reinterpret_cast<f32x4*>(out + sl.slot[k] * n + e);
-  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (k >= j.sl.count || j.sl.slot[k] < 0 || e >= j.n) return;
+  const int count = j.sl.worker(j.sl.step0[k + 1] - 1) - j.sl.worker(j.sl.step0[k]);
+  if (count == 0) return;
+  const float* src = j.part + j.sl.part0[k] * j.n + e;
+  f32x4* dst = reinterpret_cast<f32x4*>(j.out + j.sl.slot[k] * j.n + e);
+  f32x4 s = *dst;
 #pragma unroll 4
-  for (int i = 0; i < count; ++i) s += *reinterpret_cast<const f32x4*>(src + i * n);
-  *dst += s;
+  for (int i = 0; i < count; ++i) s += *reinterpret_cast<const f32x4*>(src + i * j.n);
+  *dst = s;
+}
+__global__ void __launch_bounds__(kThreads) join_kernel(Join ja, Join jb) {
+  if (blockIdx.z) join(jb);
+  else join(ja);
 }
 
 // ---------------------------------------------------------------------------
@@ -769,20 +864,20 @@ int splits_of(const fl_adapter_desc* d, const fl_batch_desc* b) {
 }
 // Backward: columns of a workgroup of bwd_out (OutWaves).
 long out_cols(const fl_adapter_desc* d) {
-  return cdiv(d->out_features, 128 * (d->dtype == FL_BF16 && d->rank <= 32 ? 8 : 4));
+  return cdiv(d->out_features, 128 * (d->dtype == FL_BF16 ? OutWaves<bf16>::n : OutWaves<float>::n));
 }
+int out_slices(const fl_adapter_desc* d) { return d->rank > 32 ? 2 : 1; }
 long in_cols(const fl_adapter_desc* d) { return cdiv(d->in_features, kInCols); }
 // Backward: workers that share the steps, for each block of columns; the chip
 // holds one workgroup of bwd_out a CU, two of bwd_in (one for ranks past 32 and
 // in fp32).
 constexpr long kCus = 256;
-long out_workers(const fl_adapter_desc* d) { return std::max(1L, kCus / out_cols(d)); }
+long out_workers(const fl_adapter_desc* d) { return std::max(1L, kCus / (out_cols(d) * out_slices(d))); }
 long in_workers(const fl_adapter_desc* d) {
   return std::max(1L, kCus * (d->dtype == FL_BF16 && d->rank <= 32 ? 2 : 1) / in_cols(d));
 }
 // Shares the steps from the first of a slot >= first_slot on out among
-// `workers`; returns their number, and the number of parts of slots that
-// several have.
+// `workers`; returns their number, and the number of parts.
 int share_out(const Segs& t, int first_slot, long workers, Slots* sl, int* parts) {
   sl->count = 0;
   sl->base = -1;
@@ -798,9 +893,8 @@ int share_out(const Segs& t, int first_slot, long workers, Slots* sl, int* parts
   sl->step0[sl->count] = end;
   sl->share = (int)cdiv(steps, workers);
   for (int k = 0; k < sl->count; ++k) {
-    const int n = sl->worker(sl->step0[k + 1] - 1) - sl->worker(sl->step0[k]) + 1;
-    sl->part0[k] = n > 1 && sl->slot[k] >= 0 ? *parts : -1;
-    if (sl->part0[k] >= 0) *parts += n;
+    sl->part0[k] = *parts;
+    if (sl->slot[k] >= 0) *parts += sl->worker(sl->step0[k + 1] - 1) - sl->worker(sl->step0[k]);
   }
   return (int)cdiv(steps, sl->share);
 }
@@ -825,9 +919,9 @@ AdapterWs carve(const fl_adapter_desc* d, const fl_batch_desc* b, char* base) {
   const size_t fwd = off;
   off = 0;
   w.dv_part = take(out_cols(d) * v);
-  // a slot of n parts has n - 1 boundaries between workers: n <= 2 (n - 1)
-  w.da_part = take(2 * in_workers(d) * d->rank * d->in_features * 4);
-  w.db_part = take(2 * out_workers(d) * d->rank * d->out_features * 4);
+  // at most one part for each boundary between workers
+  w.da_part = take((in_workers(d) - 1) * d->rank * d->in_features * 4);
+  w.db_part = take((out_workers(d) - 1) * d->rank * d->out_features * 4);
   w.total = std::max(std::max(fwd, off), (size_t)256);
   return w;
 }
@@ -952,11 +1046,12 @@ int adapter_backward(const fl_adapter_desc* d, const fl_batch_desc* batch, const
     const int rc = dispatch(d, [&](auto* type, auto rt) {
       using E = std::remove_pointer_t<decltype(type)>;
       constexpr int RT = decltype(rt)::value;
-      static_assert(OutWaves<E, RT>::n == (sizeof(E) == 2 && RT <= 2 ? 8 : 4), "out_cols, in_workers");
       if (workers_out) {
-        hipLaunchKernelGGL((bwd_out_kernel<E, RT>), dim3((unsigned)(workers_out * cols_out)),
-                           dim3(64 * OutWaves<E, RT>::n), 0, s, t, so, (const E*)dy, ld_dy, (const E*)b, v, d->rank,
-                           d->out_features, d->scale, w.dv_part, T, db, w.db_part);
+        const int groups = (int)(workers_out * cols_out), slices = out_slices(d);
+        hipLaunchKernelGGL((bwd_out_kernel<E, (RT < 2 ? RT : 2)>),
+                           dim3((unsigned)(slices == 1 ? groups : cdiv(groups, 8) * 16)),
+                           dim3(64 * OutWaves<E>::n), 0, s, t, so, (const E*)dy, ld_dy, (const E*)b, v, d->rank,
+                           d->out_features, d->scale, w.dv_part, T, db, w.db_part, groups, slices);
         if (int e = launch_status()) return e;
         if (cols_out > 1) {
           hipLaunchKernelGGL(dv_sum_kernel, dim3((unsigned)cdiv(T * d->rank, 4 * kThreads)), dim3(kThreads), 0, s,
@@ -970,14 +1065,10 @@ int adapter_backward(const fl_adapter_desc* d, const fl_batch_desc* batch, const
       return launch_status();
     });
     if (rc) return rc;
-    if (parts_out) {
-      hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(nb, 4 * kThreads), so.count), dim3(kThreads), 0, s, so,
-                         w.db_part, db, nb);
-      if (int e = launch_status()) return e;
-    }
-    if (parts_in) {
-      hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(na, 4 * kThreads), si.count), dim3(kThreads), 0, s, si,
-                         w.da_part, da, na);
+    if (parts_out || parts_in) {
+      const Join ja{si, w.da_part, da, na}, jb{so, w.db_part, db, nb};
+      hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(std::max(na, nb), 4 * kThreads), std::max(si.count, so.count), 2),
+                         dim3(kThreads), 0, s, ja, jb);
       if (int e = launch_status()) return e;
     }
   }
