@@ -42,6 +42,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kSegs = 128;     // segments a launch (2 KB of kernel arguments, 3.5 KB with the slabs)
 constexpr int kTile = 64;      // forward: rows of a tile
+constexpr int kDown = 64;      // forward: rows of a workgroup of `down`
 constexpr int kUpCols = 256;   // forward: columns of a workgroup of `up`
 constexpr int kStep = 32;      // backward: rows of a step
 constexpr int64_t kMaxStride = 1 << 22;  // elements between rows: 64 of them span at most 2^30 bytes
@@ -76,13 +77,13 @@ __device__ __forceinline__ int find(const int32_t* first, int count, int v) {
 // Rows [row0, row0 + rows) of a matrix as a buffer: what lies past the last row
 // reads as zero and is not written, without a branch (which would keep loads
 // from being counted, and so every wait would be for all of them).  A lane
-// whose column does not exist takes the offset kNowhere.  A NULL matrix reads
-// as zero.
+// whose column does not exist takes the offset kNowhere.  A NULL matrix, or one
+// without rows, reads as zero.
 typedef __amdgpu_buffer_rsrc_t Buf;
 constexpr uint32_t kNowhere = 1u << 31;
 template <typename T>
 __device__ __forceinline__ Buf rows_of(const T* p, long row0, long ld, int rows, int width) {
-  const int bytes = p ? (int)(((rows - 1) * ld + width) * (long)sizeof(T)) : 0;
+  const int bytes = p && rows > 0 ? (int)(((rows - 1) * ld + width) * (long)sizeof(T)) : 0;
   return __builtin_amdgcn_make_buffer_rsrc((void*)(p + row0 * ld), 0, bytes, 0x00020000);
 }
 // Byte offset of a lane's column in its row, kNowhere past the width.
@@ -90,13 +91,19 @@ template <typename T>
 __device__ __forceinline__ uint32_t col_off(int row, long ld, int c, int width) {
   return c < width ? ((uint32_t)row * (uint32_t)ld + c) * (uint32_t)sizeof(T) : kNowhere;
 }
+constexpr int kOnce = 2;  // cache policy: non-temporal
+template <int POLICY = 0>
 __device__ __forceinline__ u32x4 buf_ld16(Buf b, uint32_t off) {
-  return __builtin_amdgcn_raw_buffer_load_b128(b, off, 0, 0);
+  return __builtin_amdgcn_raw_buffer_load_b128(b, off, 0, POLICY);
 }
-__device__ __forceinline__ void buf_ld8(Vec8<bf16>& v, Buf b, uint32_t off) { v.r = buf_ld16(b, off); }
+template <int POLICY = 0>
+__device__ __forceinline__ void buf_ld8(Vec8<bf16>& v, Buf b, uint32_t off) {
+  v.r = buf_ld16<POLICY>(b, off);
+}
+template <int POLICY = 0>
 __device__ __forceinline__ void buf_ld8(Vec8<float>& v, Buf b, uint32_t off) {
-  v.r0 = buf_ld16(b, off);
-  v.r1 = buf_ld16(b, off + 16);
+  v.r0 = buf_ld16<POLICY>(b, off);
+  v.r1 = buf_ld16<POLICY>(b, off + 16);
 }
 __device__ __forceinline__ void buf_st8(const Vec8<bf16>& v, Buf b, uint32_t off) {
   __builtin_amdgcn_raw_buffer_store_b128(v.r, b, off, 0, 0);
@@ -104,6 +111,12 @@ __device__ __forceinline__ void buf_st8(const Vec8<bf16>& v, Buf b, uint32_t off
 __device__ __forceinline__ void buf_st8(const Vec8<float>& v, Buf b, uint32_t off) {
   __builtin_amdgcn_raw_buffer_store_b128(v.r0, b, off, 0, 0);
   __builtin_amdgcn_raw_buffer_store_b128(v.r1, b, off + 16, 0, 0);
+}
+__device__ __forceinline__ bf16 buf_ld1(Buf b, uint32_t off, bf16*) {
+  return __builtin_bit_cast(bf16, __builtin_amdgcn_raw_buffer_load_b16(b, off, 0, 0));
+}
+__device__ __forceinline__ float buf_ld1(Buf b, uint32_t off, float*) {
+  return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, off, 0, 0));
 }
 __device__ __forceinline__ float buf_ldf(Buf b, uint32_t off) {
   return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, off, 0, 0));
@@ -146,15 +159,19 @@ __device__ __forceinline__ int up_col(int q, int mm) { return 32 * (q >> 1) + 8 
 // Forward
 // ---------------------------------------------------------------------------
 
-// v (or a part of its reduction, part[split][T][r]) of one 64-row tile.
+// v (or a part of its reduction, part[split][T][r]) of kDown rows of a
+// 64-row tile.
 template <typename T, int RT>
 __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long ldx, const T* a, int r, int in,
                                                         float* v, long total_rows) {
   constexpr int RP = 16 * RT;
-  __shared__ float sh[kWaves][kTile][RP + 1];
-  const int seg = find(t.step0, t.count, blockIdx.x);
-  const int first = (blockIdx.x - t.step0[seg]) * kTile;
-  const int rows = uniform(min(kTile, t.rows[seg] - first)), slot = uniform(t.slot[seg]);
+  constexpr int NI = kDown / 16;
+  __shared__ float sh[kWaves][kDown][RP + 1];
+  const int tile = blockIdx.x / (kTile / kDown);
+  const int seg = find(t.step0, t.count, tile);
+  const int first = (blockIdx.x - t.step0[seg] * (kTile / kDown)) * kDown;
+  const int rows = uniform(min(kDown, t.rows[seg] - first)), slot = uniform(t.slot[seg]);
+  if (rows <= 0) return;
   const long row0 = uniform(t.row0[seg] + first);
   float* out = v + ((long)blockIdx.y * total_rows + row0) * r;
   if (slot < 0) {
@@ -164,9 +181,9 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
   const int tiles = (rows + 15) / 16;
   const Buf xb = rows_of(x, row0, ldx, rows, in), ab = rows_of(a, (long)slot * r, in, r, in);
-  f32x4 acc[4][RT];
+  f32x4 acc[NI][RT];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < NI; ++i)
 #pragma unroll
     for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   // 64-column steps, dealt to the splits and then to the waves in turn; a lane
@@ -175,7 +192,7 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
   const int nk = (in + 63) / 64, stride = gridDim.y * kWaves;
   const uint32_t xrow = (uint32_t)ldx * 16 * sizeof(T), arow = (uint32_t)in * 16 * sizeof(T);
   struct Step {
-    Vec8<T> av[2][RT], xv[2][4];
+    Vec8<T> av[2][RT], xv[2][NI];
   };
   auto load = [&](Step& s, int k, int count) {
 #pragma unroll
@@ -183,7 +200,7 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
       const int c = 64 * k + 16 * g + 8 * h;
       const uint32_t xo = col_off<T>(m, ldx, c, in), ao = col_off<T>(m, in, c, in);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < NI; ++i)
         if (i < count) buf_ld8(s.xv[h][i], xb, xo + i * xrow);
 #pragma unroll
       for (int j = 0; j < RT; ++j) buf_ld8(s.av[h][j], ab, ao + j * arow);
@@ -193,22 +210,26 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < NI; ++i)
         if (i < count) {
 #pragma unroll
           for (int j = 0; j < RT; ++j) acc[i][j] = mma16(s.xv[h][i].frag(), s.av[h][j].frag(), acc[i][j]);
         }
   };
   int k = blockIdx.y * kWaves + w;
-  if (tiles == 4) {
+  if (tiles == NI) {
     // two steps in flight in turn (past the last they read zero)
     Step s0, s1;
-    load(s0, k, 4);
+    load(s0, k, NI);
     for (; k < nk; k += 2 * stride) {
-      load(s1, k + stride, 4);
-      multiply(s0, 4);
-      load(s0, k + 2 * stride, 4);
-      multiply(s1, 4);
+      load(s1, k + stride, NI);
+      __builtin_amdgcn_sched_barrier(0);  // or the loads sink to their uses
+      multiply(s0, NI);
+      __builtin_amdgcn_sched_barrier(0);
+      load(s0, k + 2 * stride, NI);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(s1, NI);
+      __builtin_amdgcn_sched_barrier(0);
     }
   } else {
     Step s0;
@@ -218,7 +239,7 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
     }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < NI; ++i)
 #pragma unroll
     for (int j = 0; j < RT; ++j)
 #pragma unroll
@@ -249,13 +270,28 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
   const long row0 = uniform(t.row0[seg] + first);
   if (slot < 0 && base == y) return;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  // a wave's 64 columns: column tile q, first-operand row mm is column
+  // 32 (q / 2) + 8 (mm / 4) + 4 (q % 2) + mm % 4, so that tiles 2h and 2h + 1
+  // give a lane eight neighbours, and its row's four lanes 32
+  const int c0 = cb * kUpCols + 64 * w;
+  const Buf wb = rows_of(slot >= 0 ? b : nullptr, (long)slot * out_features + c0, r, min(64, out_features - c0), r);
+  frag_t<T> wf[4][U::weights];
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int s = 0; s < U::weights; ++s) {
+      Vec8<T> f;
+      buf_ld8(f, wb, col_off<T>(up_col(q, m), r, U::rank(s, g), r));
+      wf[q][s] = f.frag();
+    }
   if (slot >= 0) {
-    for (int i = threadIdx.x; i < kTile * RP; i += kThreads) {
+    for (int i = threadIdx.x; i < (rows + 15) / 16 * 16 * RP; i += kThreads) {
       const int row = i / RP, c = i - row * RP;
       float s = 0.f;
       if (row < rows && c < r) {
         const float* p = v + (row0 + row) * r + c;
         s = p[0];
+#pragma unroll 4
         for (int q = 1; q < parts; ++q) s += p[(long)q * total_rows * r];
         if (parts > 1 && cb == 0) v_out[(row0 + row) * r + c] = s;
       }
@@ -266,24 +302,7 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
     for (int i = threadIdx.x; i < rows * r; i += kThreads) v_out[row0 * r + i] = 0.f;
   }
   __syncthreads();
-  // a wave's 64 columns: column tile q, first-operand row mm is column
-  // 32 (q / 2) + 8 (mm / 4) + 4 (q % 2) + mm % 4, so that tiles 2h and 2h + 1
-  // give a lane eight neighbours, and its row's four lanes 32
-  const int c0 = cb * kUpCols + 64 * w;
   if (c0 >= out_features) return;
-  frag_t<T> wf[4][U::weights];
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int col = c0 + up_col(q, m);
-#pragma unroll
-    for (int s = 0; s < U::weights; ++s) {
-      const int rk = U::rank(s, g);
-      Vec8<T> f;
-      if (slot >= 0 && col < out_features && rk < r) f.load(b + ((long)slot * out_features + col) * r + rk);
-      else f.zero();
-      wf[q][s] = f.frag();
-    }
-  }
   const Buf bb = rows_of(base, row0, ldb, rows, out_features), yb = rows_of(y, row0, ldy, rows, out_features);
   uint32_t bo[2], yo[2];
 #pragma unroll
@@ -383,13 +402,14 @@ constexpr int kTokStride = kStep + 8;
 
 // One 32-row x 128-column tile of X in a wave's registers: lane (m, g) holds
 // rows 8g .. 8g + 7 at columns 8m .. 8m + 7.
+// The tile is read once: non-temporal, or it pushes dv out of the L2.
 template <typename T>
 __device__ __forceinline__ void load_tile(Vec8<T> (&xr)[8], const T* x, long ld, int row0, int rows, int c0, int width,
                                           int m, int g) {
   const Buf b = rows_of(x, row0, ld, rows, width);
   const uint32_t off = col_off<T>(8 * g, ld, c0 + 8 * m, width), row = (uint32_t)ld * sizeof(T);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) buf_ld8(xr[i], b, off + i * row);
+  for (int i = 0; i < 8; ++i) buf_ld8<kOnce>(xr[i], b, off + i * row);
 }
 
 // acc[j][q] += X^T W over the tile's 32 rows (xt: the tile turned): columns
@@ -483,19 +503,15 @@ __global__ void __launch_bounds__((64 * OutWaves<T>::n))
     }
   };
   // B as the second operand of dv = dy B: rank 16 q + m, columns 32 k + 8 g ..
-  const T* bs = b + (long)slot * out_features * stride;
+  const Buf bs = rows_of(b, (long)slot * out_features + c0, stride, min(128, out_features - c0), r);
   frag_t<T> bf[4][RT];
 #pragma unroll
   for (int k = 0; k < 4; ++k)
 #pragma unroll
     for (int q = 0; q < RT; ++q) {
-      float f[8];
+      const uint32_t off = col_off<T>(32 * k + 8 * g, stride, 16 * q + m, r);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = c0 + 32 * k + 8 * g + e;
-        f[e] = (c < out_features && 16 * q + m < r) ? to_f32(bs[(long)c * stride + 16 * q + m]) : 0.f;
-      }
-      bf[k][q] = pack8(f, (T*)nullptr);
+      for (int e = 0; e < 8; ++e) bf[k][q][e] = buf_ld1(bs, off + e * (uint32_t)(stride * sizeof(T)), (T*)nullptr);
     }
   f32x4 acc[8][RT];
 #pragma unroll
@@ -558,22 +574,25 @@ __global__ void __launch_bounds__((64 * OutWaves<T>::n))
 #pragma unroll
     for (int i = 0; i < 8; ++i) xr[i] = xn[i];
   }
+  // all of the old gradient is read before any is written: one latency
   const bool add = part < 0;
-  float* dst = (add ? db + (long)slot * out_features * stride : db_part + (long)part * out_features * stride);
+  const Buf dst = rows_of(add ? db + (long)slot * out_features * stride : db_part + (long)part * out_features * stride, c0,
+                          stride, min(128, out_features - c0), r);
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
+  for (int q = 0; q < RT; ++q) {
+    const uint32_t off = col_off<float>(32 * g, stride, 16 * q + m, r);
+    float old[8][4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int c = c0 + 8 * (4 * g + e) + j;
-      if (c >= out_features) continue;
+    for (int j = 0; j < 8; ++j)
 #pragma unroll
-      for (int q = 0; q < RT; ++q) {
-        const int k = 16 * q + m;
-        if (k >= r) continue;
-        float* p = dst + (long)c * stride + k;
-        *p = (add ? *p : 0.f) + scale * acc[j][q][e];
-      }
-    }
+      for (int e = 0; e < 4; ++e) old[j][e] = add ? buf_ldf(dst, off + (8 * e + j) * 4 * (uint32_t)stride) : 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(old[j][e] + scale * acc[j][q][e]), dst,
+                                              off + (8 * e + j) * 4 * (uint32_t)stride, 0, 0);
+  }
   });
 }
 
@@ -632,6 +651,7 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
   // fp32, in registers (it would not fit LDS)
   frag_t<T> wf[kTurned ? 1 : 2][4][U::weights];
   if constexpr (!kTurned) {
+    const Buf ab = rows_of(live ? a : nullptr, (long)slot * r, in, r, in);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -639,13 +659,9 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
         const int col = c0 + 64 * h + up_col(q, m);
 #pragma unroll
         for (int s = 0; s < U::weights; ++s) {
-          float f[8];
+          const uint32_t off = col_off<T>(U::rank(s, g), in, col, in);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int rk = U::rank(s, g) + e;
-            f[e] = live && dx && col < in && rk < r ? to_f32(a[((long)slot * r + rk) * in + col]) : 0.f;
-          }
-          wf[h][q][s] = pack8(f, (T*)nullptr);
+          for (int e = 0; e < 8; ++e) wf[h][q][s][e] = buf_ld1(ab, off + e * (uint32_t)(in * sizeof(T)), (T*)nullptr);
         }
       }
   }
@@ -752,24 +768,24 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
   }
   if (!live) return;
   const bool add = part < 0;
-  float* dst = add ? da + (long)slot * r * in : da_part + (long)part * r * in;
+  const Buf dst = rows_of(add ? da + (long)slot * r * in : da_part + (long)part * r * in, 0, in, r, in);
 #pragma unroll
   for (int q = 0; q < RT; ++q) {
-    const int k = 16 * q + m;
-    if (k >= r) continue;
+    Vec8<float> o[4];
+    uint32_t off[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int c = c0 + 8 * (4 * g + e);
-      if (c >= in) continue;
-      Vec8<float> o;
-      float s[8];
-      float* p = dst + (long)k * in + c;
-      if (add) o.load(p);
-      else o.zero();
+      off[e] = 16 * q + m < r ? col_off<float>(16 * q + m, in, c0 + 8 * (4 * g + e), in) : kNowhere;
+      if (add) buf_ld8(o[e], dst, off[e]);
+      else o[e].zero();
+    }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] = o.get(j) + acc[j][q][e];
-      o.set(s);
-      o.store(p);
+    for (int e = 0; e < 4; ++e) {
+      float s[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] = o[e].get(j) + acc[j][q][e];
+      o[e].set(s);
+      buf_st8(o[e], dst, off[e]);
     }
   }
   });
@@ -1013,7 +1029,7 @@ int adapter_forward(const fl_adapter_desc* d, const fl_batch_desc* batch, const 
     const int rc = dispatch(d, [&](auto* type, auto rt) {
       using E = std::remove_pointer_t<decltype(type)>;
       constexpr int RT = decltype(rt)::value;
-      hipLaunchKernelGGL((down_kernel<E, RT>), dim3(t.step0[t.count], splits), dim3(kThreads), 0, s, t, (const E*)x,
+      hipLaunchKernelGGL((down_kernel<E, RT>), dim3(t.step0[t.count] * (kTile / kDown), splits), dim3(kThreads), 0, s, t, (const E*)x,
                          ldx, (const E*)a, d->rank, d->in_features, splits > 1 ? w.v_part : v, T);
       if (int e = launch_status()) return e;
       hipLaunchKernelGGL((up_kernel<E, 16 * RT>), dim3((unsigned)(t.step0[t.count] * cols)), dim3(kThreads), 0, s, t,
