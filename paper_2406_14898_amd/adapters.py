@@ -20,6 +20,7 @@ class ClientAdapters:
         self.desc = F.fl_adapter_desc(num_adapters, rank, in_features, out_features, scale,
                                       F.FL_BF16 if dtype == "bf16" else F.FL_F32)
         self.dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.f32 = torch.float32
         self.shape_a = (num_adapters, rank, in_features)
         self.shape_b = (num_adapters, out_features, rank)
 
@@ -32,12 +33,13 @@ class ClientAdapters:
         """client_adapter: each client's slot or -1 (host).  x [T, in], base [T,
         out] (None: 0; may be y) and y [T, out] may have rows apart in memory; v
         fp32 [T, rank] is what backward() reads."""
-        import torch
-        T, (_, r, inn), out = batch.total_tokens, self.shape_a, self.shape_b[1]
-        x, ldx = F.matrix(x, T, inn, self.dtype, "x")
-        base, ld_base = F.matrix(base, T, out, self.dtype, "base")
-        y, ldy = F.matrix(y, T, out, self.dtype, "y")
-        F.tensors(("a", a, self.shape_a, self.dtype), ("b", b, self.shape_b, self.dtype), ("v", v, (T, r), torch.float32))
+        T, (_, r, inn), out, dt = batch.total_tokens, self.shape_a, self.shape_b[1], self.dtype
+        dev = F.current_device()
+        x, ldx = F.matrix("x", x, dev, (T, inn), dt)
+        base, ld_base = F.matrix("base", base, dev, (T, out), dt)
+        y, ldy = F.matrix("y", y, dev, (T, out), dt)
+        a, b = F.address("a", a, dev, self.shape_a, dt), F.address("b", b, dev, self.shape_b, dt)
+        v = F.address("v", v, dev, (T, r), self.f32)
         F.fl_adapter_forward(self.desc, batch, client_adapter, x, ldx, a, b, base, ld_base, y, ldy, v, workspace,
                              workspace.numel(), stream)
 
@@ -45,14 +47,15 @@ class ClientAdapters:
                  stream=None) -> None:
         """dx = dres + dv A (dres None: 0, may be dx; dx None: not formed); da, db
         fp32, accumulated (+=)."""
-        import torch
-        T, (_, r, inn), out = batch.total_tokens, self.shape_a, self.shape_b[1]
-        dy, ld_dy = F.matrix(dy, T, out, self.dtype, "dy")
-        x, ldx = F.matrix(x, T, inn, self.dtype, "x")
-        dres, ld_dres = F.matrix(dres, T, inn, self.dtype, "dres")
-        dx, ld_dx = F.matrix(dx, T, inn, self.dtype, "dx")
-        F.tensors(("a", a, self.shape_a, self.dtype), ("b", b, self.shape_b, self.dtype), ("v", v, (T, r), torch.float32),
-                  ("da", da, self.shape_a, torch.float32), ("db", db, self.shape_b, torch.float32))
+        T, (_, r, inn), out, dt = batch.total_tokens, self.shape_a, self.shape_b[1], self.dtype
+        dev = F.current_device()
+        dy, ld_dy = F.matrix("dy", dy, dev, (T, out), dt)
+        x, ldx = F.matrix("x", x, dev, (T, inn), dt)
+        dres, ld_dres = F.matrix("dres", dres, dev, (T, inn), dt)
+        dx, ld_dx = F.matrix("dx", dx, dev, (T, inn), dt)
+        a, b = F.address("a", a, dev, self.shape_a, dt), F.address("b", b, dev, self.shape_b, dt)
+        v = F.address("v", v, dev, (T, r), self.f32)
+        da, db = F.address("da", da, dev, self.shape_a, self.f32), F.address("db", db, dev, self.shape_b, self.f32)
         F.fl_adapter_backward(self.desc, batch, client_adapter, dy, ld_dy, x, ldx, a, b, v, dres, ld_dres, dx, ld_dx, da,
                               db, workspace, workspace.numel(), stream)
 
@@ -70,10 +73,11 @@ class StackAdapters:
         if len(layers) != stack.num_layers or (grads is not None and len(grads) != stack.num_layers):
             raise F.FlglmError(F.FL_ERR_ARG, f"adapters of {len(layers)} blocks for a stack of {stack.num_layers}")
         n, r, _ = layers[0]["a"].shape
+        dev = F.current_device()
         for what, rows, t in (("adapter", layers, dt), ("adapter gradient", grads or (), torch.float32)):
             for l, d in enumerate(rows):
-                F.tensors((f"{what} a of block {l}", d["a"], (n, r, stack.hidden), t),
-                          (f"{what} b of block {l}", d["b"], (n, 3 * stack.hidden, r), t))
+                F.address(f"{what} a of block {l}", d["a"], dev, (n, r, stack.hidden), t)
+                F.address(f"{what} b of block {l}", d["b"], dev, (n, 3 * stack.hidden, r), t)
         self.layers, self.grads = layers, grads
         self.record = F.stack_adapters(n, r, scale, batch, client_adapter, layers, grads)
         self.workspace = torch.empty(F.fl_stack_adapter_bytes(stack.handle, batch, self.record), dtype=torch.uint8,

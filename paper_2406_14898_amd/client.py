@@ -51,7 +51,7 @@ class ClientHead:
                            stream=None, ln_g=None, ln_b=None) -> None:
         """head_forward with the PreferenceLoss `pref` in the cross-entropy's
         place; labels host [T] (negative: none), outputs as pref.forward's."""
-        pref._outputs(batch, ref_logp, logp, loss, loss_sum)
+        pref.check_outputs(batch, F.current_device(), ref_logp, logp, loss, loss_sum)
         F.fl_lm_head_preference_forward(self.handle, pref.desc, batch, h, w, labels, ref_logp, logp, loss, loss_sum, ws,
                                         pref_ws, stream, ln_g, ln_b)
 

@@ -226,28 +226,42 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
-def matrix(t, rows: int, width: int, dtype, name: str):
-    """(tensor, row stride) of a [rows, width] argument whose rows may lie apart
-    in memory; refused where the library would read something else."""
+def _refuse(name: str, t, device: int, shape, dtype) -> None:
+    if t.get_device() != device:
+        raise FlglmError(FL_ERR_ARG, f"{name} is on {t.device}, not on the current device")
+    if t.shape != tuple(shape) or t.dtype != dtype:
+        raise FlglmError(FL_ERR_ARG, f"{name} is {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
+    raise FlglmError(FL_ERR_ARG, f"{name} is not contiguous")
+
+
+def address(name: str, t, device: int, shape, dtype) -> Optional[int]:
+    """Address of a contiguous device tensor of this shape and type on the
+    current device (None passes through); anything else is refused."""
+    if t is None:
+        return None
+    if t.get_device() != device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(name, t, device, shape, dtype)
+    return t.data_ptr()
+
+
+def matrix(name: str, t, device: int, shape, dtype):
+    """(address, row stride) of a [rows, width] device tensor whose rows may lie
+    apart in memory; refused where the library would read something else."""
     if t is None:
         return None, 0
-    tensors((name, t, (rows, width), dtype), rows_apart=True)
-    return t, (t.stride(0) if rows > 1 else width)
+    if t.get_device() != device or t.dtype != dtype or t.shape != shape:
+        _refuse(name, t, device, shape, dtype)
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
+        _refuse(name, t, device, shape, dtype)
+    return t.data_ptr(), ld if shape[0] > 1 else shape[1]
 
 
-def tensors(*args, rows_apart: bool = False) -> None:
-    """Checks (name, tensor or None, shape, dtype) arguments: on the current
-    device, of that shape and type, contiguous (rows_apart: each row is)."""
+def current_device() -> int:
     import torch
-    for name, t, shape, dtype in args:
-        if t is None:
-            continue
-        if not t.is_cuda or t.device.index != torch.cuda.current_device():
-            raise FlglmError(FL_ERR_ARG, f"{name} is on {t.device}, not on the current device")
-        if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-            raise FlglmError(FL_ERR_ARG, f"{name} is {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
-        if not (t.is_contiguous() or (rows_apart and t.stride(1) == 1)):
-            raise FlglmError(FL_ERR_ARG, f"{name} is not contiguous")
+    if not torch.cuda.is_available():
+        raise FlglmError(FL_ERR_ARG, "no GPU: the library takes device memory")
+    return torch.cuda.current_device()
 
 
 def _stream(s) -> Optional[int]:
@@ -397,7 +411,6 @@ def fl_average_replicas(params, params_bf16, n: int, stream=None) -> None:
 
 
 def _host_i32(a):
-    import numpy as np
     arr = np.ascontiguousarray(np.asarray(a, dtype=np.int32))
     return arr, arr.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
 
@@ -559,10 +572,13 @@ def fl_server_stack_backward_adapters(handle: int, batch: BatchDesc, layers: Seq
 
 
 def _sizes(sizes):
-    return (ctypes.c_int64 * len(sizes))(*sizes)
+    return sizes if isinstance(sizes, ctypes.Array) else (ctypes.c_int64 * len(sizes))(*sizes)
 
 
-def _pointers(tensors):
+def pointers(tensors):
+    """Host array of the tensors' (or the integers') device addresses."""
+    if isinstance(tensors, ctypes.Array):
+        return tensors
     return (ctypes.c_void_p * len(tensors))(*[_ptr(t) for t in tensors])
 
 
@@ -574,15 +590,15 @@ def fl_grad_norm_workspace_bytes(sizes) -> int:
 
 def fl_grad_norm(dtype: int, grads, sizes, max_norm: float, norm_coef, workspace, workspace_bytes: int,
                  stream=None) -> None:
-    """grads: device tensors (or addresses); sizes: their element counts."""
-    _check(load().fl_grad_norm(dtype, len(grads), _pointers(grads), _sizes(sizes), max_norm, _ptr(norm_coef),
+    """grads: device tensors (or addresses, or pointers() of them); sizes: their element counts."""
+    _check(load().fl_grad_norm(dtype, len(sizes), pointers(grads), _sizes(sizes), max_norm, _ptr(norm_coef),
                                _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def fl_clip_grads(dtype: int, grads, out, sizes, norm_coef, stream=None) -> None:
-    if len(out) != len(grads):
-        raise FlglmError(FL_ERR_ARG, f"{len(out)} outputs for {len(grads)} gradients")
-    _check(load().fl_clip_grads(dtype, len(grads), _pointers(grads), _pointers(out), _sizes(sizes), _ptr(norm_coef),
+    if len(out) != len(grads) or len(sizes) != len(grads):
+        raise FlglmError(FL_ERR_ARG, f"{len(out)} outputs and {len(sizes)} sizes for {len(grads)} gradients")
+    _check(load().fl_clip_grads(dtype, len(sizes), pointers(grads), pointers(out), _sizes(sizes), _ptr(norm_coef),
                                 _stream(stream)))
 
 

@@ -98,35 +98,42 @@ class GradNorm:
         self.dtype = self.grads[0].dtype
         if self.dtype not in (torch.float32, torch.bfloat16):
             raise F.FlglmError(F.FL_ERR_ARG, f"gradients are fp32 or bf16, not {self.dtype}")
+        dev = F.current_device()
         for i, g in enumerate(self.grads):
-            F.tensors((f"gradient {i}", g, g.shape, self.dtype))
-        self.sizes = [g.numel() for g in self.grads]
-        device = self.grads[0].device
-        self.workspace = torch.empty(F.fl_grad_norm_workspace_bytes(self.sizes), dtype=torch.uint8, device=device)
-        self.result = torch.empty(2, dtype=torch.float32, device=device)  # norm, coefficient
+            F.address(f"gradient {i}", g, dev, g.shape, self.dtype)
+        self.kind = F.FL_F32 if self.dtype == torch.float32 else F.FL_BF16
+        self.numel = [g.numel() for g in self.grads]
+        self.sizes = F._sizes(self.numel)
+        self.workspace = torch.empty(F.fl_grad_norm_workspace_bytes(self.sizes), dtype=torch.uint8, device=dev)
+        self.result = torch.empty(2, dtype=torch.float32, device=dev)  # norm, coefficient
 
     def norm(self, max_norm: float = float("inf"), stream=None):
         """Device fp32 [1]: the norm of the gradients' present values.  The
         coefficient min(1, max_norm / (norm + 1e-6)) is left in result[1]."""
-        F.fl_grad_norm(F.FL_F32 if self._f32 else F.FL_BF16, self.grads, self.sizes, max_norm, self.result,
-                       self.workspace, self.workspace.numel(), stream)
+        self._norm(F.pointers(self.grads), max_norm, stream)
         return self.result[:1]
 
     def clip(self, max_norm: float, out: Optional[Sequence] = None, stream=None):
         """Gradients times the coefficient, into `out` (tensors like the
         gradients; None: in place); returns the norm before."""
-        norm = self.norm(max_norm, stream)
+        grads = F.pointers(self.grads)
+        to = grads
         if out is not None:
-            for i, (o, g) in enumerate(zip(out, self.grads)):
-                F.tensors((f"output {i}", o, g.shape, self.dtype))
-        F.fl_clip_grads(F.FL_F32 if self._f32 else F.FL_BF16, self.grads, self.grads if out is None else out, self.sizes,
-                        self.result, stream)
-        return norm
+            dev = F.current_device()
+            if len(out) != len(self.numel):
+                raise F.FlglmError(F.FL_ERR_ARG, f"{len(out)} outputs for {len(self.numel)} gradients")
+            for o, n in zip(out, self.numel):
+                if o.get_device() != dev or o.dtype != self.dtype or o.numel() != n or not o.is_contiguous():
+                    raise F.FlglmError(F.FL_ERR_ARG, f"an output is {tuple(o.shape)} {o.dtype} on {o.device}, expected "
+                                                     f"{n} contiguous elements like its gradient")
+            to = F.pointers(out)
+        self._norm(grads, max_norm, stream)
+        F.fl_clip_grads(self.kind, grads, to, self.sizes, self.result, stream)
+        return self.result[:1]
 
-    @property
-    def _f32(self) -> bool:
-        import torch
-        return self.dtype == torch.float32
+    def _norm(self, grads, max_norm, stream) -> None:
+        F.fl_grad_norm(self.kind, grads, self.sizes, max_norm, self.result, self.workspace, self.workspace.numel(),
+                       stream)
 
 
 def average(arenas: Sequence[ParamArena], stream=None) -> None:
