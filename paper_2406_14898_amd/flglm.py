@@ -217,8 +217,8 @@ def _ptr(t) -> Optional[int]:
     """Device address of a tensor (None and integer addresses pass through).
     Every tensor argument of the library is device memory: a host tensor is
     refused here instead of handing its address to a kernel."""
-    if t is None:
-        return None
+    if t is None or type(t) is int:
+        return t
     if isinstance(t, int):
         return t
     if getattr(t, "is_cuda", True) is False:
@@ -258,21 +258,31 @@ def matrix(name: str, t, device: int, shape, dtype):
 
 
 def current_device() -> int:
-    import torch
-    if not torch.cuda.is_available():
+    if _gpu is None and _find_gpu() is None:
         raise FlglmError(FL_ERR_ARG, "no GPU: the library takes device memory")
-    return torch.cuda.current_device()
+    return _gpu[0]()
+
+
+#: (current device, its current stream) as functions, once torch has a GPU
+_gpu = None
+
+
+def _find_gpu():
+    global _gpu
+    try:
+        import torch
+        if torch.cuda.is_available():
+            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # without a Stream object around it
+            device = torch.cuda.current_device
+            _gpu = (device, (lambda: raw(device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream))
+    except Exception:  # pragma: no cover
+        pass
+    return _gpu
 
 
 def _stream(s) -> Optional[int]:
     if s is None:
-        try:
-            import torch
-            if torch.cuda.is_available():
-                return torch.cuda.current_stream().cuda_stream
-        except Exception:  # pragma: no cover
-            pass
-        return None
+        return _gpu[1]() if _gpu is not None or _find_gpu() is not None else None
     if isinstance(s, int):
         return s
     return s.cuda_stream
@@ -304,6 +314,7 @@ class BatchDesc:
             self.cu.ctypes.data_as(P), self.csp.ctypes.data_as(P),
             FL_MASK_PREFIX if self.prefix is not None else FL_MASK_CAUSAL,
             self.prefix.ctypes.data_as(P) if self.prefix is not None else None)
+        self.ref = ctypes.byref(self.desc)
 
     @property
     def total_tokens(self) -> int:
@@ -515,7 +526,7 @@ def _client_adapter(client_adapter, batch: BatchDesc):
 def fl_adapter_forward(desc: fl_adapter_desc, batch: BatchDesc, client_adapter, x, ldx: int, a, b, base, ld_base: int, y,
                        ldy: int, v, workspace, workspace_bytes: int, stream=None) -> None:
     arr, p = _client_adapter(client_adapter, batch)
-    _check(load().fl_adapter_forward(ctypes.byref(desc), ctypes.byref(batch.desc), p, _ptr(x), ldx, _ptr(a), _ptr(b),
+    _check(load().fl_adapter_forward(ctypes.byref(desc), batch.ref, p, _ptr(x), ldx, _ptr(a), _ptr(b),
                                      _ptr(base), ld_base, _ptr(y), ldy, _ptr(v), _ptr(workspace), workspace_bytes,
                                      _stream(stream)))
 
@@ -524,7 +535,7 @@ def fl_adapter_backward(desc: fl_adapter_desc, batch: BatchDesc, client_adapter,
                         dres, ld_dres: int, dx, ld_dx: int, da, db, workspace, workspace_bytes: int,
                         stream=None) -> None:
     arr, p = _client_adapter(client_adapter, batch)
-    _check(load().fl_adapter_backward(ctypes.byref(desc), ctypes.byref(batch.desc), p, _ptr(dy), ld_dy, _ptr(x), ldx,
+    _check(load().fl_adapter_backward(ctypes.byref(desc), batch.ref, p, _ptr(dy), ld_dy, _ptr(x), ldx,
                                       _ptr(a), _ptr(b), _ptr(v), _ptr(dres), ld_dres, _ptr(dx), ld_dx, _ptr(da),
                                       _ptr(db), _ptr(workspace), workspace_bytes, _stream(stream)))
 
