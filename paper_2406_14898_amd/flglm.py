@@ -590,7 +590,9 @@ def pointers(tensors):
     """Host array of the tensors' (or the integers') device addresses."""
     if isinstance(tensors, ctypes.Array):
         return tensors
-    return (ctypes.c_void_p * len(tensors))(*[_ptr(t) for t in tensors])
+    if not all(type(t) is int for t in tensors):
+        tensors = [_ptr(t) for t in tensors]
+    return (ctypes.c_void_p * len(tensors))(*tensors)
 
 
 def fl_grad_norm_workspace_bytes(sizes) -> int:

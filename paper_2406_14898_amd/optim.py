@@ -110,23 +110,24 @@ class GradNorm:
     def norm(self, max_norm: float = float("inf"), stream=None):
         """Device fp32 [1]: the norm of the gradients' present values.  The
         coefficient min(1, max_norm / (norm + 1e-6)) is left in result[1]."""
-        self._norm(F.pointers(self.grads), max_norm, stream)
+        self._norm(F.pointers([g.data_ptr() for g in self.grads]), max_norm, stream)
         return self.result[:1]
 
     def clip(self, max_norm: float, out: Optional[Sequence] = None, stream=None):
         """Gradients times the coefficient, into `out` (tensors like the
         gradients; None: in place); returns the norm before."""
-        grads = F.pointers(self.grads)
+        grads = F.pointers([g.data_ptr() for g in self.grads])
         to = grads
         if out is not None:
             dev = F.current_device()
             if len(out) != len(self.numel):
                 raise F.FlglmError(F.FL_ERR_ARG, f"{len(out)} outputs for {len(self.numel)} gradients")
+            dt = self.dtype
             for o, n in zip(out, self.numel):
-                if o.get_device() != dev or o.dtype != self.dtype or o.numel() != n or not o.is_contiguous():
+                if o.dtype is not dt or o.numel() != n or o.get_device() != dev or not o.is_contiguous():
                     raise F.FlglmError(F.FL_ERR_ARG, f"an output is {tuple(o.shape)} {o.dtype} on {o.device}, expected "
                                                      f"{n} contiguous elements like its gradient")
-            to = F.pointers(out)
+            to = F.pointers([o.data_ptr() for o in out])
         self._norm(grads, max_norm, stream)
         F.fl_clip_grads(self.kind, grads, to, self.sizes, self.result, stream)
         return self.result[:1]
