@@ -38,9 +38,16 @@ using namespace flglm;
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kRowThreads = 512;
 constexpr int kPairsArg = 128;       // pairs whose bounds travel in one launch's kernel arguments
 constexpr int kMaxSplits = 16;
+constexpr int kBatch = 4;            // loads of a lane in flight
 constexpr long kWantGroups = 2048;   // workgroups that fill the chip
+
+// exp(x - m) as 2^(x log2 e - m log2 e), the difference in one rounding.
+__device__ __forceinline__ float exp_less(float x, float m_log2e) {
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -m_log2e));
+}
 
 // (max, sum of exp(x - max)) pairs; an empty part is (-inf, 0).
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
@@ -50,14 +57,40 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
     s = s2;
     return;
   }
-  const float mx = fmaxf(m, m2);
-  s = s * __expf(m - mx) + s2 * __expf(m2 - mx);
+  const float mx = fmaxf(m, m2), ml = mx * kLog2e;
+  s = s * exp_less(m, ml) + s2 * exp_less(m2, ml);
+  m = mx;
+}
+
+// Takes 8 N columns into the running (max, sum): one new maximum and one
+// rescaling for all of them.
+template <typename T, int N>
+__device__ __forceinline__ void take(float& m, float& s, const Vec8<T> (&v)[N]) {
+  float mx = m;
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) mx = fmaxf(mx, v[u].get(k));
+  if (mx == -INFINITY) {  // masked columns only so far, or NaN, which a maximum passes over
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) m = v[u].get(k) != v[u].get(k) ? v[u].get(k) : m;
+    return;
+  }
+  const float ml = mx * kLog2e;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k & 3] += exp_less(v[u].get(k), ml);
+  s = s * (m == -INFINITY ? 0.f : exp_less(m, ml)) + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
   m = mx;
 }
 
 // Columns [c0, c1) of each labelled row: part[row][split] = (max, sum).
 template <typename T>
-__global__ void __launch_bounds__(kThreads) pref_row_kernel(const T* logits, long ld, int V, int cols,
+__global__ void __launch_bounds__(kRowThreads) pref_row_kernel(const T* logits, long ld, int V, int cols,
                                                             const int32_t* labels, float2* part, uint32_t* done) {
   const long t = blockIdx.x;
   const int sp = blockIdx.y;
@@ -67,37 +100,31 @@ __global__ void __launch_bounds__(kThreads) pref_row_kernel(const T* logits, lon
   const T* row = logits + t * ld;
   const int c0 = sp * cols, c1 = min(V, c0 + cols);
   float m = -INFINITY, s = 0.f;
-  for (int j0 = c0 + threadIdx.x * 8; j0 < c1; j0 += kThreads * 8) {
-    Vec8<T> v;
-    v.load(row + j0);
-    float x[8], mx = -INFINITY;
+  int j0 = c0 + threadIdx.x * 8;
+  for (; j0 + (kBatch - 1) * kRowThreads * 8 < c1; j0 += kBatch * kRowThreads * 8) {
+    Vec8<T> v[kBatch];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      x[k] = v.get(k);
-      mx = fmaxf(mx, x[k]);
-    }
-    if (mx == -INFINITY) {  // masked columns only, or NaN, which a maximum passes over
-#pragma unroll
-      for (int k = 0; k < 8; ++k) mx = x[k] != x[k] ? x[k] : mx;
-    }
-    float sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) sum += __expf(x[k] - mx);
-    join(m, s, mx, sum);
+    for (int u = 0; u < kBatch; ++u) v[u].load(row + j0 + u * kRowThreads * 8);
+    take(m, s, v);
+  }
+  for (; j0 < c1; j0 += kRowThreads * 8) {
+    Vec8<T> v[1];
+    v[0].load(row + j0);
+    take(m, s, v);
   }
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
     const float m2 = __shfl_xor(m, o), s2 = __shfl_xor(s, o);
     join(m, s, m2, s2);
   }
-  __shared__ float sm[kThreads / 64], ss[kThreads / 64];
+  __shared__ float sm[kRowThreads / 64], ss[kRowThreads / 64];
   if ((threadIdx.x & 63) == 0) {
     sm[threadIdx.x >> 6] = m;
     ss[threadIdx.x >> 6] = s;
   }
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kThreads / 64; ++w) join(m, s, sm[w], ss[w]);
+    for (int w = 1; w < kRowThreads / 64; ++w) join(m, s, sm[w], ss[w]);
     part[t * gridDim.y + sp] = make_float2(m, s);
   }
 }
@@ -132,46 +159,43 @@ __global__ void __launch_bounds__(kThreads) pref_pair_kernel(PairArgs a, const T
   __shared__ double sh[kThreads / 64];
   __shared__ bool last;
   const int p = a.first + blockIdx.x;
-  double lp[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r0 = a.cu[2 * blockIdx.x + h], r1 = a.cu[2 * blockIdx.x + h + 1];
-    double sum = 0;
-    for (int t = r0 + threadIdx.x; t < r1; t += kThreads) {
-      const int lab = labels[t];
-      f32x4 f = {0.f, 0.f, 0.f, 0.f};
-      if (lab >= 0 && lab < V) {
-        float m = -INFINITY, s = 0.f;
-        for (int k = 0; k < splits; ++k) {
-          const float2 q = part[(long)t * splits + k];
-          join(m, s, q.x, q.y);
-        }
-        sum += ((double)to_f32(logits[(long)t * ld + lab]) - (double)m) - log((double)s);
-        f[0] = m;
-        f[1] = s;
-        f[2] = 1.f;
+  const int r0 = a.cu[2 * blockIdx.x], r1 = a.cu[2 * blockIdx.x + 1], r2 = a.cu[2 * blockIdx.x + 2];
+  double lp[2] = {0, 0};
+  for (int t = r0 + threadIdx.x; t < r2; t += kThreads) {
+    const int lab = labels[t];
+    f32x4 f = {0.f, 0.f, 0.f, 0.f};
+    if (lab >= 0 && lab < V) {
+      const float x = to_f32(logits[(long)t * ld + lab]);
+      float m = -INFINITY, s = 0.f;
+#pragma unroll 4
+      for (int k = 0; k < splits; ++k) {
+        const float2 q = part[(long)t * splits + k];
+        join(m, s, q.x, q.y);
       }
-      factors[t] = f;
+      const double l = ((double)x - (double)m) - log((double)s);
+      lp[0] += t < r1 ? l : 0.0;
+      lp[1] += t < r1 ? 0.0 : l;
+      f[0] = m;
+      f[1] = s;
+      f[2] = 1.f;
     }
-    lp[h] = block_sum(sum, sh);
+    factors[t] = f;
   }
+  lp[0] = block_sum(lp[0], sh);
+  lp[1] = block_sum(lp[1], sh);
   double d = lp[0] - lp[1];
   if (ref) d = (lp[0] - (double)ref[2 * p]) - (lp[1] - (double)ref[2 * p + 1]);
   const double z = beta * d;
   // (no 0 times infinity: z is infinite where a label has no probability)
   const double L = (1.0 - eps) * softplus(-z) + (eps > 0.0 ? eps * softplus(z) : 0.0);
   const double k = beta * (eps / (1.0 + exp(-z)) - (1.0 - eps) / (1.0 + exp(z)));
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r0 = a.cu[2 * blockIdx.x + h], r1 = a.cu[2 * blockIdx.x + h + 1];
-    const double kh = h ? -k : k;
-    for (int t = r0 + threadIdx.x; t < r1; t += kThreads) {
-      f32x4 f = factors[t];  // this thread's own
-      if (f[2] != 0.f) {
-        f[1] = (float)(kh / (double)f[1]);
-        f[2] = (float)kh;
-        factors[t] = f;
-      }
+  for (int t = r0 + threadIdx.x; t < r2; t += kThreads) {
+    f32x4 f = factors[t];  // this thread's own
+    if (f[2] != 0.f) {
+      const double kh = t < r1 ? k : -k;
+      f[1] = (float)(kh / (double)f[1]);
+      f[2] = (float)kh;
+      factors[t] = f;
     }
   }
   if (threadIdx.x == 0) {
@@ -192,32 +216,35 @@ __global__ void __launch_bounds__(kThreads) pref_pair_kernel(PairArgs a, const T
 }
 
 // The first `width` columns of dlogits (past V: 0) of row t; may be the logits
-// themselves.
+// themselves.  2048 columns a workgroup, so that the chip sweeps through
+// memory in order, and from the last row to the first: what the row kernel
+// read last is in the last-level cache.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) pref_grad_kernel(const T* logits, long ld, int V, const int32_t* labels,
                                                              const f32x4* factors, float scale, T* dlogits, long ldd,
-                                                             int width) {
-  const long t = blockIdx.x;
-  const f32x4 f = factors[t];
+                                                             int width, int blocks) {
+  const uint32_t i = gridDim.x - 1 - blockIdx.x;
+  const long t = i / (uint32_t)blocks;
+  const int j0 = ((int)(i % (uint32_t)blocks) * kThreads + threadIdx.x) * 8;
+  if (j0 >= width) return;
   const int lab = labels[t];
-  const T* row = logits + t * ld;
-  T* out = dlogits + t * ldd;
-  const float m = f[0], ks = scale * f[1], k = scale * f[2];
-  const bool live = lab >= 0 && lab < V;
-  for (long j0 = ((long)blockIdx.y * kThreads + threadIdx.x) * 8; j0 < width; j0 += (long)gridDim.y * kThreads * 8) {
-    Vec8<T> v;
-    float g[8];
-    if (live && j0 < V) {
-      v.load(row + j0);
+  Vec8<T> v;
+  float g[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = (j0 + i == lab ? k : 0.f) - ks * __expf(v.get(i) - m);
-    } else {
+  for (int k = 0; k < 8; ++k) g[k] = 0.f;
+  if (lab >= 0 && lab < V && j0 < V) {
+    v.load(logits + t * ld + j0);
+    const f32x4 f = factors[t];
+    const float ml = f[0] * kLog2e, ks = -scale * f[1];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = 0.f;
+    for (int k = 0; k < 8; ++k) g[k] = ks * exp_less(v.get(k), ml);
+    if ((unsigned)(lab - j0) < 8u) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) g[k] += j0 + k == lab ? scale * f[2] : 0.f;
     }
-    v.set(g);
-    v.store(out + j0);
   }
+  v.set(g);
+  v.store(dlogits + t * ldd + j0);
 }
 
 bool al16(const void* p) { return ((uintptr_t)p & 15) == 0; }
@@ -239,7 +266,7 @@ struct PrefWs {
 };
 // Parts a row is split into: one when the rows alone fill the chip.
 int splits_of(long T, long V) {
-  const long most = std::max(1L, V / (8 * kThreads));
+  const long most = std::max(1L, V / (8 * kRowThreads));
   return (int)std::min<long>({(kWantGroups + T - 1) / T, most, (long)kMaxSplits});
 }
 PrefWs carve(long T, long V, char* base) {
@@ -294,7 +321,7 @@ int forward(const fl_preference_desc* d, const fl_batch_desc* b, const T* logits
   const long tokens = b->total_tokens;
   const int V = (int)d->vocab, splits = splits_of(tokens, V);
   const int cols = (int)(((V + splits - 1) / splits + 7) / 8 * 8);
-  hipLaunchKernelGGL(pref_row_kernel<T>, dim3((unsigned)tokens, splits), dim3(kThreads), 0, s, logits, ld, V, cols,
+  hipLaunchKernelGGL(pref_row_kernel<T>, dim3((unsigned)tokens, splits), dim3(kRowThreads), 0, s, logits, ld, V, cols,
                      labels, w.part, w.done);
   if (int rc = launch_status()) return rc;
   PairArgs a;
@@ -313,10 +340,19 @@ int forward(const fl_preference_desc* d, const fl_batch_desc* b, const T* logits
 template <typename T>
 int gradient(const fl_preference_desc* d, long tokens, const T* logits, long ld, const int32_t* labels,
              float grad_scale, T* dlogits, long ldd, int width, const PrefWs& w, hipStream_t s) {
-  const int V = (int)d->vocab, splits = splits_of(tokens, V);
-  hipLaunchKernelGGL(pref_grad_kernel<T>, dim3((unsigned)tokens, splits), dim3(kThreads), 0, s, logits, ld, V, labels,
-                     w.factors, grad_scale, dlogits, ldd, width);
-  return launch_status();
+  const int V = (int)d->vocab;
+  const long blocks = (width + 8 * kThreads - 1) / (8 * kThreads);
+  // (rows x blocks would pass a launch's 2^31 workgroups from 2^26 rows on)
+  const long most = std::max(1L, (1L << 30) / blocks);
+  for (long t1 = tokens; t1 > 0;) {
+    const long t0 = std::max(0L, t1 - most);
+    hipLaunchKernelGGL(pref_grad_kernel<T>, dim3((unsigned)((t1 - t0) * blocks)), dim3(kThreads), 0, s,
+                       logits + t0 * ld, ld, V, labels + t0, w.factors + t0, grad_scale, dlogits + t0 * ldd, ldd, width,
+                       (int)blocks);
+    if (int rc = launch_status()) return rc;
+    t1 = t0;
+  }
+  return FL_OK;
 }
 
 }  // namespace
