@@ -13,7 +13,7 @@
 // on whole sequences, so no row's gradient is known before the last row of
 // its pair has been read.  Rows without a label are read in neither.
 //
-//  * row kernel: the running (maximum, sum of exponentials) of a row's
+//  * row kernel: the running maximum and sum of exponentials of a row's
 //    columns; a row is split over several workgroups when rows are few.
 //  * pair kernel: one workgroup a pair joins the parts of its rows, forms the
 //    sequence sums, the loss and each row's factors.  The last pair to finish
@@ -39,17 +39,21 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kRowThreads = 512;
+constexpr double kLn2 = 0.69314718055994530942;
 constexpr int kPairsArg = 128;       // pairs whose bounds travel in one launch's kernel arguments
 constexpr int kMaxSplits = 16;
 constexpr int kBatch = 4;            // loads of a lane in flight
 constexpr long kWantGroups = 2048;   // workgroups that fill the chip
 
-// exp(x - m) as 2^(x log2 e - m log2 e), the difference in one rounding.
-__device__ __forceinline__ float exp_less(float x, float m_log2e) {
-  return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -m_log2e));
+// Exponentials are powers of two: with M the running maximum of x log2 e,
+// rounded to fp32 and then taken as it is, s = sum of 2^(x log2 e - M), the
+// difference in one rounding, and logsumexp = M ln 2 + ln s.  (A maximum m that
+// is rounded again in m log2 e would put an error of its own on every row.)
+__device__ __forceinline__ float exp2_less(float x, float M) {
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -M));
 }
 
-// (max, sum of exp(x - max)) pairs; an empty part is (-inf, 0).
+// (M, s) pairs; an empty part is (-inf, 0).
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
   if (m2 == -INFINITY) return;
   if (m == -INFINITY) {
@@ -57,20 +61,21 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
     s = s2;
     return;
   }
-  const float mx = fmaxf(m, m2), ml = mx * kLog2e;
-  s = s * exp_less(m, ml) + s2 * exp_less(m2, ml);
+  const float mx = fmaxf(m, m2);
+  s = s * __builtin_amdgcn_exp2f(m - mx) + s2 * __builtin_amdgcn_exp2f(m2 - mx);
   m = mx;
 }
 
-// Takes 8 N columns into the running (max, sum): one new maximum and one
-// rescaling for all of them.
+// Takes 8 N columns into the running (M, s): one new maximum and one rescaling
+// for all of them.
 template <typename T, int N>
 __device__ __forceinline__ void take(float& m, float& s, const Vec8<T> (&v)[N]) {
-  float mx = m;
+  float top = -INFINITY;
 #pragma unroll
   for (int u = 0; u < N; ++u)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) mx = fmaxf(mx, v[u].get(k));
+    for (int k = 0; k < 8; ++k) top = fmaxf(top, v[u].get(k));
+  const float mx = fmaxf(m, top * kLog2e);
   if (mx == -INFINITY) {  // masked columns only so far, or NaN, which a maximum passes over
 #pragma unroll
     for (int u = 0; u < N; ++u)
@@ -78,17 +83,16 @@ __device__ __forceinline__ void take(float& m, float& s, const Vec8<T> (&v)[N]) 
       for (int k = 0; k < 8; ++k) m = v[u].get(k) != v[u].get(k) ? v[u].get(k) : m;
     return;
   }
-  const float ml = mx * kLog2e;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int u = 0; u < N; ++u)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum[k & 3] += exp_less(v[u].get(k), ml);
-  s = s * (m == -INFINITY ? 0.f : exp_less(m, ml)) + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+    for (int k = 0; k < 8; ++k) sum[k & 3] += exp2_less(v[u].get(k), mx);
+  s = s * (m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx)) + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
   m = mx;
 }
 
-// Columns [c0, c1) of each labelled row: part[row][split] = (max, sum).
+// Columns [c0, c1) of each labelled row: part[row][split] = (M, s).
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) pref_row_kernel(const T* logits, long ld, int V, int cols,
                                                             const int32_t* labels, float2* part, uint32_t* done) {
@@ -148,8 +152,8 @@ __device__ __forceinline__ double block_sum(double v, double* sh) {
 
 __device__ __forceinline__ double softplus(double u) { return fmax(u, 0.0) + log1p(exp(-fabs(u))); }
 
-// factors[t] = (max, k / sum of exponentials, k, 0): the gradient of row t is
-// k onehot - (k / sum) exp(x - max); k = 0 for a row without a label.
+// factors[t] = (M, k / s, k, 0): the gradient of row t is k onehot - (k / s)
+// 2^(x log2 e - M); k = 0 for a row without a label.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) pref_pair_kernel(PairArgs a, const T* logits, long ld, int V, int splits,
                                                              const int32_t* labels, const float2* part,
@@ -172,7 +176,7 @@ __global__ void __launch_bounds__(kThreads) pref_pair_kernel(PairArgs a, const T
         const float2 q = part[(long)t * splits + k];
         join(m, s, q.x, q.y);
       }
-      const double l = ((double)x - (double)m) - log((double)s);
+      const double l = (double)x - ((double)m * kLn2 + log((double)s));
       lp[0] += t < r1 ? l : 0.0;
       lp[1] += t < r1 ? 0.0 : l;
       f[0] = m;
@@ -235,9 +239,9 @@ __global__ void __launch_bounds__(kThreads) pref_grad_kernel(const T* logits, lo
   if (lab >= 0 && lab < V && j0 < V) {
     v.load(logits + t * ld + j0);
     const f32x4 f = factors[t];
-    const float ml = f[0] * kLog2e, ks = -scale * f[1];
+    const float ks = -scale * f[1];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) g[k] = ks * exp_less(v.get(k), ml);
+    for (int k = 0; k < 8; ++k) g[k] = ks * exp2_less(v.get(k), f[0]);
     if ((unsigned)(lab - j0) < 8u) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) g[k] += j0 + k == lab ? scale * f[2] : 0.f;
