@@ -674,14 +674,21 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
   if (live) {
     stage(wt[0], wr[0]);
     if constexpr (kTurned) {
-      for (int i = tid; i < RP * (kInCols / 8); i += kThreads) {
-        const int rk = i / (kInCols / 8), c = 8 * (i - rk * (kInCols / 8));
-        Vec8<T> f;
-        if (rk < r && cb * kInCols + c < in) f.load(a + ((long)slot * r + rk) * in + cb * kInCols + c);
-        else f.zero();
-        const auto e = f.frag();
+      // lanes along the ranks: along the columns their writes would meet in two banks
+      const Buf ar = rows_of(a, (long)slot * r, in, r, in);
+      constexpr int kAt = kThreads / RP;  // groups of eight columns a pass
 #pragma unroll
-        for (int j = 0; j < 8; ++j) aw[(c + j) * kTurnedRow + rk] = e[j];
+      for (int i = 0; i < kInCols / 8; i += 4 * kAt) {
+        Vec8<T> f[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          buf_ld8(f[u], ar, col_off<T>(tid % RP, in, cb * kInCols + 8 * (i + u * kAt + tid / RP), in));
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const auto e = f[u].frag();
+#pragma unroll
+          for (int j = 0; j < 8; ++j) aw[(8 * (i + u * kAt + tid / RP) + j) * kTurnedRow + tid % RP] = e[j];
+        }
       }
     }
   }
