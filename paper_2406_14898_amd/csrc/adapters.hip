@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
     for (int i = threadIdx.x; i < rows * r; i += kThreads) out[i] = 0.f;
     return;
   }
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   const int tiles = (rows + 15) / 16;
   const Buf xb = rows_of(x, row0, ldx, rows, in), ab = rows_of(a, (long)slot * r, in, r, in);
   f32x4 acc[NI][RT];
@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
   const int rows = uniform(min(kTile, t.rows[seg] - first)), slot = uniform(t.slot[seg]);
   const long row0 = uniform(t.row0[seg] + first);
   if (slot < 0 && base == y) return;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   // a wave's 64 columns: column tile q, first-operand row mm is column
   // 32 (q / 2) + 8 (mm / 4) + 4 (q % 2) + mm % 4, so that tiles 2h and 2h + 1
   // give a lane eight neighbours, and its row's four lanes 32
@@ -284,20 +284,42 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
       buf_ld8(f, wb, col_off<T>(up_col(q, m), r, U::rank(s, g), r));
       wf[q][s] = f.frag();
     }
-  if (slot >= 0) {
+  if (slot >= 0 && parts == 1) {
+    // (through the code for parts, below, 41447 rows take 497 us instead of 487)
     for (int i = threadIdx.x; i < (rows + 15) / 16 * 16 * RP; i += kThreads) {
       const int row = i / RP, c = i - row * RP;
       float s = 0.f;
-      if (row < rows && c < r) {
-        const float* p = v + (row0 + row) * r + c;
-        s = p[0];
-#pragma unroll 4
-        for (int q = 1; q < parts; ++q) s += p[(long)q * total_rows * r];
-        if (parts > 1 && cb == 0) v_out[(row0 + row) * r + c] = s;
-      }
+      if (row < rows && c < r) s = v[(row0 + row) * r + c];
 #pragma unroll
       for (int q = 0; q < U::parts; ++q) sh[row][q * RP + c] = split(s, (T*)nullptr);
     }
+  } else if (slot >= 0) {
+    // a thread's rank, and one row in kRows; 16 rows at least are staged
+    constexpr int kRows = kThreads / RP, kMany = kTile / kRows;
+    const int rank = threadIdx.x % RP, row = threadIdx.x / RP;
+    auto stage = [&](auto count) {
+      constexpr int n = decltype(count)::value;
+      float f[n] = {};
+      for (int q = 0; q < parts; ++q) {
+        const Buf vb = rows_of(v + q * total_rows * r, row0, r, rows, r);
+        const uint32_t off = col_off<float>(row, r, rank, r);
+        float part[n];
+#pragma unroll
+        for (int i = 0; i < n; ++i) part[i] = buf_ldf(vb, off + i * (kRows * 4) * (uint32_t)r);
+        __builtin_amdgcn_sched_barrier(0);  // all loads before the first sum
+#pragma unroll
+        for (int i = 0; i < n; ++i) f[i] += part[i];
+      }
+      const Buf ob = rows_of(cb == 0 ? v_out : nullptr, row0, r, rows, r);
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(f[i]), ob, col_off<float>(row + i * kRows, r, rank, r), 0, 0);
+#pragma unroll
+        for (int q = 0; q < U::parts; ++q) sh[row + i * kRows][q * RP + rank] = split(f[i], (T*)nullptr);
+      }
+    };
+    if (rows > 16) stage(std::integral_constant<int, kMany>());
+    else stage(std::integral_constant<int, 16 / kRows>());
   } else if (parts > 1 && cb == 0) {
     for (int i = threadIdx.x; i < rows * r; i += kThreads) v_out[row0 * r + i] = 0.f;
   }
@@ -485,7 +507,7 @@ __global__ void __launch_bounds__((64 * OutWaves<T>::n))
   for_slots(t, sl, worker, [&](Walk& wk, int slot, int part) {
   int tid = threadIdx.x;
   settle(tid);  // addresses are formed anew for each slot: held across slots, they would not fit the registers
-  const int lane = tid & 63, w = tid >> 6, m = lane & 15, g = lane >> 4;
+  const int lane = tid & 63, w = uniform(tid >> 6), m = lane & 15, g = lane >> 4;
   const int c0 = cb * 128 * NW + 128 * w;
   int row0, row1 = 0;
   int rows = wk.next(t, &row0), rows1 = 0;
@@ -623,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
   for_slots(t, sl, worker, [&](Walk& wk, int slot, int part) {
   int tid = threadIdx.x;
   settle(tid);  // as in bwd_out
-  const int lane = tid & 63, w = tid >> 6, m = lane & 15, g = lane >> 4;
+  const int lane = tid & 63, w = uniform(tid >> 6), m = lane & 15, g = lane >> 4;
   const int c0 = cb * kInCols + 128 * w;
   const bool live = slot >= 0;
   if (!live && (!dx || dx == dres)) return;
@@ -880,10 +902,13 @@ void fill(const std::vector<Run>& runs, size_t* i, int rows_a_step, Segs* t) {
 }
 
 // Forward: workgroups along the reduction of v, for batches whose tiles alone
-// do not fill the chip; every wave has a step at least.
+// do not fill the chip; every wave has a step at least.  `up` adds the parts in
+// every block of columns, which is why they are few (4096 -> 4096, rank 64, one
+// client of 128 rows: 8 parts 16 us, 16 parts 18; 2048 rows: 7 parts 26 us, 16
+// 33, none 44; 64 clients of one row, rank 16: 3 parts 17.7 us, none 21).
 int splits_of(const fl_adapter_desc* d, const fl_batch_desc* b) {
   const long tiles = b->total_tokens / kTile + b->num_clients;
-  return (int)std::max(1L, std::min<long>({512 / tiles, d->in_features / (64 * kWaves), 16}));
+  return (int)std::max(1L, std::min<long>({256 / tiles, d->in_features / (64 * kWaves), 8}));
 }
 // Backward: columns of a workgroup of bwd_out (OutWaves).
 long out_cols(const fl_adapter_desc* d) {
