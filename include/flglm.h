@@ -370,7 +370,7 @@ int fl_lm_head_preference_backward(fl_client* client, const fl_preference_desc* 
  * the two products, and products with it keep its digits (bf16 inputs give
  * the results of an fp32 computation rounded once).
  * Row strides are in elements, multiples of 8, at least the row's width and at
- * most 2^24. */
+ * most 2^22. */
 typedef struct fl_adapter_desc {
   int32_t num_adapters;  /* slots n, 1 .. 2^16 */
   int32_t rank;          /* r: a multiple of 8 in [8, 64] */

@@ -62,9 +62,11 @@ class ClientAdapters:
 
 class StackAdapters:
     """Adapters on the fused query / key / value projection of every block of a
-    ServerStack, for one batch: what its forward() and backward() take as
-    `adapters`.  layers / grads: one dict "a" [n, rank, H], "b" [n, 3H, rank] a
-    block (gradients fp32, accumulated; None: forward only)."""
+    ServerStack, for batches of one shape: what its forward() and backward()
+    take as `adapters`.  layers / grads: one dict "a" [n, rank, H], "b" [n, 3H,
+    rank] a block (gradients fp32, accumulated; None: forward only).  Owns the
+    workspace, in which a forward leaves what its backward reads: calls on
+    different streams, or graphs captured with it, must not overlap."""
 
     def __init__(self, stack, batch: F.BatchDesc, client_adapter, layers: Sequence[Dict],
                  grads: Optional[Sequence[Dict]] = None, scale: float = 1.0, device="cuda"):
@@ -78,7 +80,22 @@ class StackAdapters:
             for l, d in enumerate(rows):
                 F.address(f"{what} a of block {l}", d["a"], dev, (n, r, stack.hidden), t)
                 F.address(f"{what} b of block {l}", d["b"], dev, (n, 3 * stack.hidden, r), t)
-        self.layers, self.grads = layers, grads
+        # the record holds addresses: the tensors themselves, not only their dicts, live as long
+        self.tensors = [d[k] for rows in (layers, grads or ()) for d in rows for k in ("a", "b")]
+        self.stack, self.device, self.has_grads = stack, dev, grads is not None
+        self.clients, self.tokens = batch.desc.num_clients, batch.total_tokens
         self.record = F.stack_adapters(n, r, scale, batch, client_adapter, layers, grads)
         self.workspace = torch.empty(F.fl_stack_adapter_bytes(stack.handle, batch, self.record), dtype=torch.uint8,
                                      device=device)
+
+    def check(self, stack, batch: F.BatchDesc, backward: bool = False) -> None:
+        """Refuses a call that the record and the workspace were not made for."""
+        if stack is not self.stack:
+            raise F.FlglmError(F.FL_ERR_ARG, "the adapters are another stack's")
+        if batch.desc.num_clients != self.clients or batch.total_tokens != self.tokens:
+            raise F.FlglmError(F.FL_ERR_ARG, f"adapters for {self.clients} clients and {self.tokens} tokens, a batch of "
+                                             f"{batch.desc.num_clients} and {batch.total_tokens}")
+        if F.current_device() != self.device:
+            raise F.FlglmError(F.FL_ERR_ARG, f"the adapters are on device {self.device}, not on the current one")
+        if backward and not self.has_grads:
+            raise F.FlglmError(F.FL_ERR_ARG, "the adapters have no gradients")

@@ -10,9 +10,18 @@
 //  * down: v from x.  64-row tiles, the reduction over a workgroup's waves,
 //    and over workgroups too when rows are few.
 //  * up: y from base and v.  A workgroup covers 64 rows x 256 columns.
-//  * bwd_out: one pass over dy gives dv (summed over column blocks) and dB
-//    (summed over slabs of rows).
+//  * bwd_out: one pass over dy gives dv (a part for each block of columns,
+//    which dv_sum adds) and dB.
 //  * bwd_in: one pass over x and dres gives dx and dA.
+//  * join: adds the parts of dA and dB that more than one workgroup left.
+//
+// Measured on one MI355X, bf16, clients of one slot each (a plain copy of
+// 1 GiB moves 5.0 TB/s here, reads alone 6.2):
+//   forward, 41447 rows, 4096 -> 12288, rank 16, 32 clients: 2.35 GB in 480 us
+//     (down 99 us, 3.4 TB/s of reads; up 385 us, 5.3 TB/s)
+//   backward, 41447 rows, 4096 -> 12288 without dres: 2.05 GB in 456 us (out 211,
+//     dv_sum 6, in 207, join 16)
+//   one row, 4096 -> 12288: 6.4 us for both forward kernels
 //
 // v and dv are fp32.  In bf16 mode a matrix product with them runs on the bf16
 // matrix cores in parts: v = v0 + v1 (+ v2), each part the bf16 nearest to
@@ -21,7 +30,7 @@
 //
 // Rows reach their adapters through a table of segments (runs of rows with
 // one slot) in kernel arguments: nothing is uploaded, and a call can be
-// captured.  Sums over rows and slabs have a fixed order: no atomics.
+// captured.  Sums over rows and parts have a fixed order: no atomics.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -40,9 +49,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kSegs = 128;     // segments a launch (2 KB of kernel arguments, 3.5 KB with the slabs)
+constexpr int kSegs = 128;     // segments a launch (2 KB of kernel arguments, 3.6 KB with the table of slots)
 constexpr int kTile = 64;      // forward: rows of a tile
-constexpr int kDown = 64;      // forward: rows of a workgroup of `down`
 constexpr int kUpCols = 256;   // forward: columns of a workgroup of `up`
 constexpr int kStep = 32;      // backward: rows of a step
 constexpr int64_t kMaxStride = 1 << 22;  // elements between rows: 64 of them span at most 2^30 bytes
@@ -159,19 +167,16 @@ __device__ __forceinline__ int up_col(int q, int mm) { return 32 * (q >> 1) + 8 
 // Forward
 // ---------------------------------------------------------------------------
 
-// v (or a part of its reduction, part[split][T][r]) of kDown rows of a
-// 64-row tile.
+// v (or a part of its reduction, part[split][T][r]) of one 64-row tile.
 template <typename T, int RT>
 __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long ldx, const T* a, int r, int in,
                                                         float* v, long total_rows) {
   constexpr int RP = 16 * RT;
-  constexpr int NI = kDown / 16;
-  __shared__ float sh[kWaves][kDown][RP + 1];
-  const int tile = blockIdx.x / (kTile / kDown);
-  const int seg = find(t.step0, t.count, tile);
-  const int first = (blockIdx.x - t.step0[seg] * (kTile / kDown)) * kDown;
-  const int rows = uniform(min(kDown, t.rows[seg] - first)), slot = uniform(t.slot[seg]);
-  if (rows <= 0) return;
+  constexpr int NI = kTile / 16;
+  __shared__ float sh[kWaves][kTile][RP + 1];
+  const int seg = find(t.step0, t.count, blockIdx.x);
+  const int first = (blockIdx.x - t.step0[seg]) * kTile;
+  const int rows = uniform(min(kTile, t.rows[seg] - first)), slot = uniform(t.slot[seg]);
   const long row0 = uniform(t.row0[seg] + first);
   float* out = v + ((long)blockIdx.y * total_rows + row0) * r;
   if (slot < 0) {
@@ -268,7 +273,11 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
   const int first = (tile - t.step0[seg]) * kTile;
   const int rows = uniform(min(kTile, t.rows[seg] - first)), slot = uniform(t.slot[seg]);
   const long row0 = uniform(t.row0[seg] + first);
-  if (slot < 0 && base == y) return;
+  if (slot < 0) {  // no adapter: v is zero (without parts `down` wrote it), y is base
+    if (parts > 1 && cb == 0)
+      for (int i = threadIdx.x; i < rows * r; i += kThreads) v_out[row0 * r + i] = 0.f;
+    if (base == y) return;
+  }
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   // a wave's 64 columns: column tile q, first-operand row mm is column
   // 32 (q / 2) + 8 (mm / 4) + 4 (q % 2) + mm % 4, so that tiles 2h and 2h + 1
@@ -313,15 +322,14 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
       const Buf ob = rows_of(cb == 0 ? v_out : nullptr, row0, r, rows, r);
 #pragma unroll
       for (int i = 0; i < n; ++i) {
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(f[i]), ob, col_off<float>(row + i * kRows, r, rank, r), 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(f[i]), ob, col_off<float>(row + i * kRows, r, rank, r), 0,
+                                              0);
 #pragma unroll
         for (int q = 0; q < U::parts; ++q) sh[row + i * kRows][q * RP + rank] = split(f[i], (T*)nullptr);
       }
     };
     if (rows > 16) stage(std::integral_constant<int, kMany>());
     else stage(std::integral_constant<int, 16 / kRows>());
-  } else if (parts > 1 && cb == 0) {
-    for (int i = threadIdx.x; i < rows * r; i += kThreads) v_out[row0 * r + i] = 0.f;
   }
   __syncthreads();
   if (c0 >= out_features) return;
@@ -424,7 +432,8 @@ constexpr int kTokStride = kStep + 8;
 
 // One 32-row x 128-column tile of X in a wave's registers: lane (m, g) holds
 // rows 8g .. 8g + 7 at columns 8m .. 8m + 7.
-// The tile is read once: non-temporal, or it pushes dv out of the L2.
+// The tile is read once: non-temporal (dy: 484 -> 463 us a backward of 41447
+// rows; not for what is read in two halves of a line, as by `up`: 487 -> 559).
 template <typename T>
 __device__ __forceinline__ void load_tile(Vec8<T> (&xr)[8], const T* x, long ld, int row0, int rows, int c0, int width,
                                           int m, int g) {
@@ -505,116 +514,117 @@ __global__ void __launch_bounds__((64 * OutWaves<T>::n))
   const int cols = (out_features + 128 * NW - 1) / (128 * NW);
   const int worker = group / cols, cb = group - worker * cols;
   for_slots(t, sl, worker, [&](Walk& wk, int slot, int part) {
-  int tid = threadIdx.x;
-  settle(tid);  // addresses are formed anew for each slot: held across slots, they would not fit the registers
-  const int lane = tid & 63, w = uniform(tid >> 6), m = lane & 15, g = lane >> 4;
-  const int c0 = cb * 128 * NW + 128 * w;
-  int row0, row1 = 0;
-  int rows = wk.next(t, &row0), rows1 = 0;
-  Vec8<T> xr[8], xn[8], xt[8];
-  Factor<RP, NT> vn;
-  vn.load(v, row0, rows, stride, r, tid);
-  load_tile(xr, dy, lddy, row0, rows, c0, out_features, m, g);
-  auto stage = [&](T* dst) {
+    int tid = threadIdx.x;
+    settle(tid);  // addresses are formed anew for each slot: held across slots, they would not fit the registers
+    const int lane = tid & 63, w = uniform(tid >> 6), m = lane & 15, g = lane >> 4;
+    const int c0 = cb * 128 * NW + 128 * w;
+    int row0, row1 = 0;
+    int rows = wk.next(t, &row0), rows1 = 0;
+    Vec8<T> xr[8], xn[8], xt[8];
+    Factor<RP, NT> vn;
+    vn.load(v, row0, rows, stride, r, tid);
+    load_tile(xr, dy, lddy, row0, rows, c0, out_features, m, g);
+    auto stage = [&](T* dst) {
 #pragma unroll
-    for (int i = 0; i < Factor<RP, NT>::n; ++i) {
-      const int row = Factor<RP, NT>::row(tid, i), c = Factor<RP, NT>::rank(tid);
-      float f = vn.f[i];
+      for (int i = 0; i < Factor<RP, NT>::n; ++i) {
+        const int row = Factor<RP, NT>::row(tid, i), c = Factor<RP, NT>::rank(tid);
+        float f = vn.f[i];
 #pragma unroll
-      for (int p = 0; p < NP; ++p) dst[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
+        for (int p = 0; p < NP; ++p) dst[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
+      }
+    };
+    // B as the second operand of dv = dy B: rank 16 q + m, columns 32 k + 8 g ..
+    const Buf bs = rows_of(b, (long)slot * out_features + c0, stride, min(128, out_features - c0), r);
+    frag_t<T> bf[4][RT];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int q = 0; q < RT; ++q) {
+        const uint32_t off = col_off<T>(32 * k + 8 * g, stride, 16 * q + m, r);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) bf[k][q][e] = buf_ld1(bs, off + e * (uint32_t)(stride * sizeof(T)), (T*)nullptr);
+      }
+    f32x4 acc[8][RT];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int q = 0; q < RT; ++q) acc[j][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+    stage(wt[0]);
+    lds_barrier();
+    for (int buf = 0;; buf ^= 1) {
+      const bool more = wk.step < wk.end;
+      if (more) {  // in flight until the next step begins
+        rows1 = wk.next(t, &row1);
+        vn.load(v, row1, rows1, stride, r, tid);
+        load_tile(xn, dy, lddy, row1, rows1, c0, out_features, m, g);
+      }
+      T* mine = tile[buf][w];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) xr[i].store(mine + (8 * g + i) * kRow + 8 * m);
+      transpose8x8(xr, xt);
+      __builtin_amdgcn_wave_barrier();
+      outer<T, RT>(acc, xt, wt[buf], m, g);
+      f32x4 d[2][RT];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int q = 0; q < RT; ++q) d[h][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          Vec8<T> f;
+          f.load(mine + (16 * h + m) * kRow + 32 * k + 8 * g);
+#pragma unroll
+          for (int q = 0; q < RT; ++q) d[h][q] = mma16(f.frag(), bf[k][q], d[h][q]);
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+      asm volatile("" ::: "memory");  // the rows are read: dv takes their place
+      float* dvs = (float*)mine;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int q = 0; q < RT; ++q)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dvs[(16 * h + 4 * g + e) * kDv + 16 * q + m] = d[h][q][e];
+      if (more) stage(wt[buf ^ 1]);
+      lds_barrier();
+      const Buf dst = rows_of(dv_part + cb * total_rows * stride, row0, stride, rows, r);
+      const uint32_t off = col_off<float>(Factor<RP, NT>::row(tid, 0), stride, Factor<RP, NT>::rank(tid), r);
+#pragma unroll
+      for (int i = 0; i < Factor<RP, NT>::n; ++i) {
+        const int row = Factor<RP, NT>::row(tid, i), c = Factor<RP, NT>::rank(tid);
+        float s = 0.f;
+#pragma unroll
+        for (int q = 0; q < NW; ++q) s += ((const float*)tile[buf][q])[row * kDv + c];
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(scale * s), dst,
+                                              off + i * (NT / RP * 4) * (uint32_t)stride, 0, 0);
+      }
+      if (!more) break;
+      row0 = row1;
+      rows = rows1;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) xr[i] = xn[i];
     }
-  };
-  // B as the second operand of dv = dy B: rank 16 q + m, columns 32 k + 8 g ..
-  const Buf bs = rows_of(b, (long)slot * out_features + c0, stride, min(128, out_features - c0), r);
-  frag_t<T> bf[4][RT];
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
+    // all of the old gradient is read before any is written: one latency
+    const bool add = part < 0;
+    const long matrix = (long)out_features * stride;
+    const Buf dst = rows_of(add ? db + slot * matrix : db_part + part * matrix, c0, stride,
+                            min(128, out_features - c0), r);
 #pragma unroll
     for (int q = 0; q < RT; ++q) {
-      const uint32_t off = col_off<T>(32 * k + 8 * g, stride, 16 * q + m, r);
+      const uint32_t off = col_off<float>(32 * g, stride, 16 * q + m, r);
+      float old[8][4];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) bf[k][q][e] = buf_ld1(bs, off + e * (uint32_t)(stride * sizeof(T)), (T*)nullptr);
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) old[j][e] = add ? buf_ldf(dst, off + (8 * e + j) * 4 * (uint32_t)stride) : 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(old[j][e] + scale * acc[j][q][e]), dst,
+                                                off + (8 * e + j) * 4 * (uint32_t)stride, 0, 0);
     }
-  f32x4 acc[8][RT];
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-#pragma unroll
-    for (int q = 0; q < RT; ++q) acc[j][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-  stage(wt[0]);
-  lds_barrier();
-  for (int buf = 0;; buf ^= 1) {
-    const bool more = wk.step < wk.end;
-    if (more) {  // in flight until the next step begins
-      rows1 = wk.next(t, &row1);
-      vn.load(v, row1, rows1, stride, r, tid);
-      load_tile(xn, dy, lddy, row1, rows1, c0, out_features, m, g);
-    }
-    T* mine = tile[buf][w];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) xr[i].store(mine + (8 * g + i) * kRow + 8 * m);
-    transpose8x8(xr, xt);
-    __builtin_amdgcn_wave_barrier();
-    outer<T, RT>(acc, xt, wt[buf], m, g);
-    f32x4 d[2][RT];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int q = 0; q < RT; ++q) d[h][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        Vec8<T> f;
-        f.load(mine + (16 * h + m) * kRow + 32 * k + 8 * g);
-#pragma unroll
-        for (int q = 0; q < RT; ++q) d[h][q] = mma16(f.frag(), bf[k][q], d[h][q]);
-      }
-    }
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("" ::: "memory");  // the rows are read: dv takes their place
-    float* dvs = (float*)mine;
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int q = 0; q < RT; ++q)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) dvs[(16 * h + 4 * g + e) * kDv + 16 * q + m] = d[h][q][e];
-    if (more) stage(wt[buf ^ 1]);
-    lds_barrier();
-    const Buf dst = rows_of(dv_part + cb * total_rows * stride, row0, stride, rows, r);
-    const uint32_t off = col_off<float>(Factor<RP, NT>::row(tid, 0), stride, Factor<RP, NT>::rank(tid), r);
-#pragma unroll
-    for (int i = 0; i < Factor<RP, NT>::n; ++i) {
-      const int row = Factor<RP, NT>::row(tid, i), c = Factor<RP, NT>::rank(tid);
-      float s = 0.f;
-#pragma unroll
-      for (int q = 0; q < NW; ++q) s += ((const float*)tile[buf][q])[row * kDv + c];
-      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(scale * s), dst, off + i * (NT / RP * 4) * (uint32_t)stride,
-                                            0, 0);
-    }
-    if (!more) break;
-    row0 = row1;
-    rows = rows1;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) xr[i] = xn[i];
-  }
-  // all of the old gradient is read before any is written: one latency
-  const bool add = part < 0;
-  const Buf dst = rows_of(add ? db + (long)slot * out_features * stride : db_part + (long)part * out_features * stride, c0,
-                          stride, min(128, out_features - c0), r);
-#pragma unroll
-  for (int q = 0; q < RT; ++q) {
-    const uint32_t off = col_off<float>(32 * g, stride, 16 * q + m, r);
-    float old[8][4];
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) old[j][e] = add ? buf_ldf(dst, off + (8 * e + j) * 4 * (uint32_t)stride) : 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(old[j][e] + scale * acc[j][q][e]), dst,
-                                              off + (8 * e + j) * 4 * (uint32_t)stride, 0, 0);
-  }
   });
 }
 
@@ -628,11 +638,12 @@ __global__ void __launch_bounds__(kThreads) dv_sum_kernel(float* dv_part, int pa
   *reinterpret_cast<f32x4*>(dv_part + e) = s;
 }
 
-// dx and dA (or its slab's part).
+// dx and dA (or a part of it).  As bwd_out, without a sum over the waves: a
+// wave's columns are its own.
 template <typename T, int RT>
-__global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1)) bwd_in_kernel(Segs t, Slots sl, const T* x, long ldx, const T* a,
-                                                          const float* dv, int r, int in, const T* dres, long lddr,
-                                                          T* dx, long lddx, float* da, float* da_part) {
+__global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
+    bwd_in_kernel(Segs t, Slots sl, const T* x, long ldx, const T* a, const float* dv, int r, int in, const T* dres,
+                  long lddr, T* dx, long lddx, float* da, float* da_part) {
   constexpr int RP = 16 * RT, NP = Parts<T>::exact;
   using U = Up<T, RP>;
   __shared__ __align__(16) T wt[2][NP * RP * kTokStride];
@@ -643,180 +654,180 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
   const int cols = (in + kInCols - 1) / kInCols;
   const int worker = blockIdx.x / cols, cb = blockIdx.x - worker * cols;
   for_slots(t, sl, worker, [&](Walk& wk, int slot, int part) {
-  int tid = threadIdx.x;
-  settle(tid);  // as in bwd_out
-  const int lane = tid & 63, w = uniform(tid >> 6), m = lane & 15, g = lane >> 4;
-  const int c0 = cb * kInCols + 128 * w;
-  const bool live = slot >= 0;
-  if (!live && (!dx || dx == dres)) return;
-  int row0, row1 = 0;
-  int rows = wk.next(t, &row0), rows1 = 0;
-  Vec8<T> xr[8], xt[8];
-  Factor<RP, kThreads> vn;
-  auto stage = [&](T* turned, T* in_rows) {
+    int tid = threadIdx.x;
+    settle(tid);  // as in bwd_out
+    const int lane = tid & 63, w = uniform(tid >> 6), m = lane & 15, g = lane >> 4;
+    const int c0 = cb * kInCols + 128 * w;
+    const bool live = slot >= 0;
+    if (!live && (!dx || dx == dres)) return;
+    int row0, row1 = 0;
+    int rows = wk.next(t, &row0), rows1 = 0;
+    Vec8<T> xr[8], xt[8];
+    Factor<RP, kThreads> vn;
+    auto stage = [&](T* turned, T* in_rows) {
 #pragma unroll
-    for (int i = 0; i < Factor<RP, kThreads>::n; ++i) {
-      const int row = Factor<RP, kThreads>::row(tid, i), c = Factor<RP, kThreads>::rank(tid);
-      float f = vn.f[i], f2 = f;
+      for (int i = 0; i < Factor<RP, kThreads>::n; ++i) {
+        const int row = Factor<RP, kThreads>::row(tid, i), c = Factor<RP, kThreads>::rank(tid);
+        float f = vn.f[i], f2 = f;
 #pragma unroll
-      for (int p = 0; p < NP; ++p) turned[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
+        for (int p = 0; p < NP; ++p) turned[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
 #pragma unroll
-      for (int p = 0; p < U::parts; ++p) in_rows[row * U::stride + p * RP + c] = split(f2, (T*)nullptr);
-    }
-  };
-  if (live) {
-    vn.load(dv, row0, rows, r, r, tid);
-    load_tile(xr, x, ldx, row0, rows, c0, in, m, g);
-  }
-  // A as the first operand of dx = dv A, columns as in `up`: bf16, turned to
-  // [column][rank] in LDS (in registers it would cost a second wave a SIMD);
-  // fp32, in registers (it would not fit LDS)
-  frag_t<T> wf[kTurned ? 1 : 2][4][U::weights];
-  if constexpr (!kTurned) {
-    const Buf ab = rows_of(live ? a : nullptr, (long)slot * r, in, r, in);
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int col = c0 + 64 * h + up_col(q, m);
-#pragma unroll
-        for (int s = 0; s < U::weights; ++s) {
-          const uint32_t off = col_off<T>(U::rank(s, g), in, col, in);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) wf[h][q][s][e] = buf_ld1(ab, off + e * (uint32_t)(in * sizeof(T)), (T*)nullptr);
-        }
+        for (int p = 0; p < U::parts; ++p) in_rows[row * U::stride + p * RP + c] = split(f2, (T*)nullptr);
       }
-  }
-  f32x4 acc[8][RT];
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-#pragma unroll
-    for (int q = 0; q < RT; ++q) acc[j][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-  lds_barrier();  // the slot before has read what LDS holds
-  if (live) {
-    stage(wt[0], wr[0]);
-    if constexpr (kTurned) {
-      // lanes along the ranks: along the columns their writes would meet in two banks
-      const Buf ar = rows_of(a, (long)slot * r, in, r, in);
-      constexpr int kAt = kThreads / RP;  // groups of eight columns a pass
-#pragma unroll
-      for (int i = 0; i < kInCols / 8; i += 4 * kAt) {
-        Vec8<T> f[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          buf_ld8(f[u], ar, col_off<T>(tid % RP, in, cb * kInCols + 8 * (i + u * kAt + tid / RP), in));
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const auto e = f[u].frag();
-#pragma unroll
-          for (int j = 0; j < 8; ++j) aw[(8 * (i + u * kAt + tid / RP) + j) * kTurnedRow + tid % RP] = e[j];
-        }
-      }
+    };
+    if (live) {
+      vn.load(dv, row0, rows, r, r, tid);
+      load_tile(xr, x, ldx, row0, rows, c0, in, m, g);
     }
-  }
-  lds_barrier();
-  uint32_t ro[2][2], xo[2][2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      ro[h][u] = col_off<T>(m, lddr, c0 + 64 * h + 32 * u + 8 * g, in);
-      xo[h][u] = col_off<T>(m, lddx, c0 + 64 * h + 32 * u + 8 * g, in);
-    }
-  const uint32_t rrow = 16 * sizeof(T) * (uint32_t)lddr, xrow = 16 * sizeof(T) * (uint32_t)lddx;
-  for (int buf = 0;; buf ^= 1) {
-    const bool more = wk.step < wk.end;
-    // what this step adds to, then what the next one takes
-    const Buf rb = rows_of(dx ? dres : nullptr, row0, lddr, rows, in), xb = rows_of(dx, row0, lddx, rows, in);
-    Vec8<T> bs[2][2][2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
+    // A as the first operand of dx = dv A, columns as in `up`: bf16, turned to
+    // [column][rank] in LDS (in registers it would cost a second wave a SIMD);
+    // fp32, in registers (it would not fit LDS)
+    frag_t<T> wf[kTurned ? 1 : 2][4][U::weights];
+    if constexpr (!kTurned) {
+      const Buf ab = rows_of(live ? a : nullptr, (long)slot * r, in, r, in);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) buf_ld8(bs[h][i][u], rb, ro[h][u] + i * rrow);
-    if (live) transpose8x8(xr, xt);
-    if (more) {
-      rows1 = wk.next(t, &row1);
-      if (live) {
-        vn.load(dv, row1, rows1, r, r, tid);
-        load_tile(xr, x, ldx, row1, rows1, c0, in, m, g);
-      }
-    }
-    if (live) outer<T, RT>(acc, xt, wt[buf], m, g);
-    if (dx) {
+        for (int q = 0; q < 4; ++q) {
+          const int col = c0 + 64 * h + up_col(q, m);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        Vec8<T> f[U::steps];
-        if (live) {
+          for (int s = 0; s < U::weights; ++s) {
+            const uint32_t off = col_off<T>(U::rank(s, g), in, col, in);
 #pragma unroll
-          for (int s = 0; s < U::steps; ++s) {
-            if (U::live(s, g)) f[s].load(wr[buf] + (16 * i + m) * U::stride + 8 * U::chunk(s, g));
-            else f[s].zero();
+            for (int e = 0; e < 8; ++e) wf[h][q][s][e] = buf_ld1(ab, off + e * (uint32_t)(in * sizeof(T)), (T*)nullptr);
           }
         }
+    }
+    f32x4 acc[8][RT];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          f32x4 d[4];
+    for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) d[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int q = 0; q < RT; ++q) acc[j][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+    lds_barrier();  // the slot before has read what LDS holds
+    if (live) {
+      stage(wt[0], wr[0]);
+      if constexpr (kTurned) {
+        // lanes along the ranks: along the columns their writes would meet in two banks
+        const Buf ar = rows_of(a, (long)slot * r, in, r, in);
+        constexpr int kAt = kThreads / RP;  // groups of eight columns a pass
+#pragma unroll
+        for (int i = 0; i < kInCols / 8; i += 4 * kAt) {
+          Vec8<T> f[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            buf_ld8(f[u], ar, col_off<T>(tid % RP, in, cb * kInCols + 8 * (i + u * kAt + tid / RP), in));
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const auto e = f[u].frag();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) aw[(8 * (i + u * kAt + tid / RP) + j) * kTurnedRow + tid % RP] = e[j];
+          }
+        }
+      }
+    }
+    lds_barrier();
+    uint32_t ro[2][2], xo[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        ro[h][u] = col_off<T>(m, lddr, c0 + 64 * h + 32 * u + 8 * g, in);
+        xo[h][u] = col_off<T>(m, lddx, c0 + 64 * h + 32 * u + 8 * g, in);
+      }
+    const uint32_t rrow = 16 * sizeof(T) * (uint32_t)lddr, xrow = 16 * sizeof(T) * (uint32_t)lddx;
+    for (int buf = 0;; buf ^= 1) {
+      const bool more = wk.step < wk.end;
+      // what this step adds to, then what the next one takes
+      const Buf rb = rows_of(dx ? dres : nullptr, row0, lddr, rows, in), xb = rows_of(dx, row0, lddx, rows, in);
+      Vec8<T> bs[2][2][2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) buf_ld8(bs[h][i][u], rb, ro[h][u] + i * rrow);
+      if (live) transpose8x8(xr, xt);
+      if (more) {
+        rows1 = wk.next(t, &row1);
+        if (live) {
+          vn.load(dv, row1, rows1, r, r, tid);
+          load_tile(xr, x, ldx, row1, rows1, c0, in, m, g);
+        }
+      }
+      if (live) outer<T, RT>(acc, xt, wt[buf], m, g);
+      if (dx) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          Vec8<T> f[U::steps];
           if (live) {
-            if constexpr (kTurned) {
 #pragma unroll
-              for (int q = 0; q < 4; ++q)
-#pragma unroll
-                for (int s = 0; s < U::weights; ++s) {
-                  Vec8<T> wv;
-                  wv.load(aw + (128 * w + 64 * h + up_col(q, m)) * kTurnedRow + U::rank(s, g));
-#pragma unroll
-                  for (int p = s; p < U::steps; p += U::weights) d[q] = mma16(wv.frag(), f[p].frag(), d[q]);
-                }
-            } else {
-#pragma unroll
-              for (int s = 0; s < U::steps; ++s)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) d[q] = mma16(wf[h][q][s % U::weights], f[s].frag(), d[q]);
+            for (int s = 0; s < U::steps; ++s) {
+              if (U::live(s, g)) f[s].load(wr[buf] + (16 * i + m) * U::stride + 8 * U::chunk(s, g));
+              else f[s].zero();
             }
           }
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            float o[8];
+          for (int h = 0; h < 2; ++h) {
+            f32x4 d[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = bs[h][i][u].get(e) + d[2 * u + (e >> 2)][e & 3];
-            bs[h][i][u].set(o);
-            buf_st8(bs[h][i][u], xb, xo[h][u] + i * xrow);
+            for (int q = 0; q < 4; ++q) d[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (live) {
+              if constexpr (kTurned) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                  for (int s = 0; s < U::weights; ++s) {
+                    Vec8<T> wv;
+                    wv.load(aw + (128 * w + 64 * h + up_col(q, m)) * kTurnedRow + U::rank(s, g));
+#pragma unroll
+                    for (int p = s; p < U::steps; p += U::weights) d[q] = mma16(wv.frag(), f[p].frag(), d[q]);
+                  }
+              } else {
+#pragma unroll
+                for (int s = 0; s < U::steps; ++s)
+#pragma unroll
+                  for (int q = 0; q < 4; ++q) d[q] = mma16(wf[h][q][s % U::weights], f[s].frag(), d[q]);
+              }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              float o[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) o[e] = bs[h][i][u].get(e) + d[2 * u + (e >> 2)][e & 3];
+              bs[h][i][u].set(o);
+              buf_st8(bs[h][i][u], xb, xo[h][u] + i * xrow);
+            }
           }
         }
       }
+      if (!more) break;
+      if (live) stage(wt[buf ^ 1], wr[buf ^ 1]);
+      lds_barrier();
+      row0 = row1;
+      rows = rows1;
     }
-    if (!more) break;
-    if (live) stage(wt[buf ^ 1], wr[buf ^ 1]);
-    lds_barrier();
-    row0 = row1;
-    rows = rows1;
-  }
-  if (!live) return;
-  const bool add = part < 0;
-  const Buf dst = rows_of(add ? da + (long)slot * r * in : da_part + (long)part * r * in, 0, in, r, in);
+    if (!live) return;
+    const bool add = part < 0;
+    const Buf dst = rows_of(add ? da + (long)slot * r * in : da_part + (long)part * r * in, 0, in, r, in);
 #pragma unroll
-  for (int q = 0; q < RT; ++q) {
-    Vec8<float> o[4];
-    uint32_t off[4];
+    for (int q = 0; q < RT; ++q) {
+      Vec8<float> o[4];
+      uint32_t off[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      off[e] = 16 * q + m < r ? col_off<float>(16 * q + m, in, c0 + 8 * (4 * g + e), in) : kNowhere;
-      if (add) buf_ld8(o[e], dst, off[e]);
-      else o[e].zero();
+      for (int e = 0; e < 4; ++e) {
+        off[e] = 16 * q + m < r ? col_off<float>(16 * q + m, in, c0 + 8 * (4 * g + e), in) : kNowhere;
+        if (add) buf_ld8(o[e], dst, off[e]);
+        else o[e].zero();
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float s[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = o[e].get(j) + acc[j][q][e];
+        o[e].set(s);
+        buf_st8(o[e], dst, off[e]);
+      }
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float s[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] = o[e].get(j) + acc[j][q][e];
-      o[e].set(s);
-      buf_st8(o[e], dst, off[e]);
-    }
-  }
   });
 }
 
@@ -979,7 +990,8 @@ int check_desc(const fl_adapter_desc* d) {
   if (d->dtype != FL_BF16 && d->dtype != FL_F32) return set_error(FL_ERR_SHAPE, "dtype must be bf16 or fp32");
   if (d->num_adapters < 1 || d->num_adapters > (1 << 16))
     return set_error(FL_ERR_SHAPE, "num_adapters must be in [1, 2^16]");
-  if (d->rank < 8 || d->rank > 64 || d->rank % 8) return set_error(FL_ERR_SHAPE, "rank must be a multiple of 8 in [8, 64]");
+  if (d->rank < 8 || d->rank > 64 || d->rank % 8)
+    return set_error(FL_ERR_SHAPE, "rank must be a multiple of 8 in [8, 64]");
   for (int n : {d->in_features, d->out_features})
     if (n < 8 || n % 8 || n > 65536) return set_error(FL_ERR_SHAPE, "features must be multiples of 8 in [8, 65536]");
   if (!std::isfinite(d->scale)) return set_error(FL_ERR_ARG, "scale is not finite");
@@ -1005,7 +1017,7 @@ int check_mat(const Mat& m, bool required) {
   if (!m.p) return required ? set_error(FL_ERR_NULL, "a matrix argument is NULL") : FL_OK;
   if (!al16(m.p)) return set_error(FL_ERR_ALIGN, "a matrix argument is not 16-byte aligned");
   if (m.ld < m.width || m.ld % 8 || m.ld > kMaxStride)
-    return set_error(FL_ERR_SHAPE, "a row stride must be a multiple of 8, at least the row's width and at most 2^24");
+    return set_error(FL_ERR_SHAPE, "a row stride must be a multiple of 8, at least the row's width and at most 2^22");
   return FL_OK;
 }
 
@@ -1061,7 +1073,7 @@ int adapter_forward(const fl_adapter_desc* d, const fl_batch_desc* batch, const 
     const int rc = dispatch(d, [&](auto* type, auto rt) {
       using E = std::remove_pointer_t<decltype(type)>;
       constexpr int RT = decltype(rt)::value;
-      hipLaunchKernelGGL((down_kernel<E, RT>), dim3(t.step0[t.count] * (kTile / kDown), splits), dim3(kThreads), 0, s, t, (const E*)x,
+      hipLaunchKernelGGL((down_kernel<E, RT>), dim3(t.step0[t.count], splits), dim3(kThreads), 0, s, t, (const E*)x,
                          ldx, (const E*)a, d->rank, d->in_features, splits > 1 ? w.v_part : v, T);
       if (int e = launch_status()) return e;
       hipLaunchKernelGGL((up_kernel<E, 16 * RT>), dim3((unsigned)(t.step0[t.count] * cols)), dim3(kThreads), 0, s, t,
@@ -1115,8 +1127,8 @@ int adapter_backward(const fl_adapter_desc* d, const fl_batch_desc* batch, const
     if (rc) return rc;
     if (parts_out || parts_in) {
       const Join ja{si, w.da_part, da, na}, jb{so, w.db_part, db, nb};
-      hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(std::max(na, nb), 4 * kThreads), std::max(si.count, so.count), 2),
-                         dim3(kThreads), 0, s, ja, jb);
+      const dim3 grid((unsigned)cdiv(std::max(na, nb), 4 * kThreads), std::max(si.count, so.count), 2);
+      hipLaunchKernelGGL(join_kernel, grid, dim3(kThreads), 0, s, ja, jb);
       if (int e = launch_status()) return e;
     }
   }

@@ -573,8 +573,9 @@ int fl_lm_head_preference_backward(fl_client* c, const fl_preference_desc* pref,
                                    workspace_bytes))
     return rc;
   if (overlap(pref_workspace, pref_workspace_bytes, workspace, workspace_bytes) ||
-      overlap(pref_workspace, pref_workspace_bytes, dh, T * c->d.hidden * c->E))
-    return set_error(FL_ERR_ALIAS, "the loss's workspace overlaps dh or the client's workspace");
+      overlap(pref_workspace, pref_workspace_bytes, dh, T * c->d.hidden * c->E) ||
+      (dw_vocab && overlap(pref_workspace, pref_workspace_bytes, dw_vocab, 4 * c->d.vocab * c->d.hidden)))
+    return set_error(FL_ERR_ALIAS, "the loss's workspace overlaps dh, dw or the client's workspace");
   const ClientWs w = carve(c, T, (char*)workspace);
   hipStream_t s = (hipStream_t)stream;
   // in place: the logits become their own gradient (padded columns: 0)

@@ -896,8 +896,8 @@ struct StackAdapters {
 };
 
 // Checks the adapters of a call and carves their workspace.
-int carve_adapters(const fl_stack* st, const fl_batch_desc* b, const BatchInfo& bi, const fl_stack_adapters* ad,
-                   bool backward, void* ws, size_t ws_bytes, StackAdapters* out) {
+int carve_adapters(const fl_stack* st, const fl_batch_desc* b, const fl_stack_adapters* ad, bool backward, void* ws,
+                   size_t ws_bytes, StackAdapters* out) {
   const int N = st->d.num_layers;
   out->ad = ad;
   out->batch = b;
@@ -1070,7 +1070,7 @@ static int stack_forward(fl_stack* st, const fl_batch_desc* b, const fl_layer_pa
 
   StackAdapters sa;
   if (adapters) {
-    if ((rc = carve_adapters(st, b, bi, adapters, false, adapter_ws, adapter_ws_bytes, &sa))) return rc;
+    if ((rc = carve_adapters(st, b, adapters, false, adapter_ws, adapter_ws_bytes, &sa))) return rc;
     if (overlap(adapter_ws, adapter_ws_bytes, ws, ws_bytes) || overlap(adapter_ws, adapter_ws_bytes, x, act) ||
         overlap(adapter_ws, adapter_ws_bytes, y, act) || overlap(adapter_ws, adapter_ws_bytes, saved, nsaved))
       return fail(FL_ERR_ALIAS, "the adapters' workspace overlaps x / y / saved / workspace");
@@ -1176,7 +1176,7 @@ static int stack_backward(fl_stack* st, const fl_batch_desc* b, const fl_layer_p
 
   StackAdapters sa;
   if (adapters) {
-    if ((rc = carve_adapters(st, b, bi, adapters, true, adapter_ws, adapter_ws_bytes, &sa))) return rc;
+    if ((rc = carve_adapters(st, b, adapters, true, adapter_ws, adapter_ws_bytes, &sa))) return rc;
     if (overlap(adapter_ws, adapter_ws_bytes, ws, ws_bytes) || overlap(adapter_ws, adapter_ws_bytes, x, act) ||
         overlap(adapter_ws, adapter_ws_bytes, dy, act) || overlap(adapter_ws, adapter_ws_bytes, dx, act) ||
         overlap(adapter_ws, adapter_ws_bytes, saved, nsaved))

@@ -217,9 +217,7 @@ def _ptr(t) -> Optional[int]:
     """Device address of a tensor (None and integer addresses pass through).
     Every tensor argument of the library is device memory: a host tensor is
     refused here instead of handing its address to a kernel."""
-    if t is None or type(t) is int:
-        return t
-    if isinstance(t, int):
+    if t is None or isinstance(t, int):
         return t
     if getattr(t, "is_cuda", True) is False:
         raise FlglmError(FL_ERR_ARG, f"tensor on {t.device}: the library takes device memory")

@@ -106,6 +106,7 @@ class GradNorm:
         self.sizes = F._sizes(self.numel)
         self.workspace = torch.empty(F.fl_grad_norm_workspace_bytes(self.sizes), dtype=torch.uint8, device=dev)
         self.result = torch.empty(2, dtype=torch.float32, device=dev)  # norm, coefficient
+        self.device = dev
 
     def norm(self, max_norm: float = float("inf"), stream=None):
         """Device fp32 [1]: the norm of the gradients' present values.  The
@@ -133,6 +134,8 @@ class GradNorm:
         return self.result[:1]
 
     def _norm(self, grads, max_norm, stream) -> None:
+        if F.current_device() != self.device:
+            raise F.FlglmError(F.FL_ERR_ARG, f"the gradients are on device {self.device}, not on the current one")
         F.fl_grad_norm(self.kind, grads, self.sizes, max_norm, self.result, self.workspace, self.workspace.numel(),
                        stream)
 

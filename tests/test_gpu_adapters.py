@@ -172,6 +172,13 @@ def test_bases_of_every_kind(slots, base, dres, with_dx):
     _run([[40], [21], [90]], slots, 2, 16, 96, 200, "bf16", base=base, dres=dres, with_dx=with_dx)
 
 
+@pytest.mark.parametrize("slots", [[0, -1, 1], [-1, -1, -1]])
+def test_projection_in_place_with_a_divided_reduction(slots):
+    """Few rows of many columns: v is summed over workgroups, also the zeros of
+    clients without an adapter, whose rows of y stay as they are."""
+    _run([[40], [21], [90]], slots, 2, 16, 1032, 200, "bf16", base="inplace", dres="inplace")
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_rows_apart_in_memory(dt):
     """Strided x, base, y, dy, dres and dx; what lies between their rows stays."""

@@ -254,3 +254,38 @@ def test_adapters_of_another_stack_are_refused():
     with pytest.raises(FlglmError):
         StackAdapters(stack, batch, [0, 0], _adapters(1, 8, 256, 2, "bf16", 0))    # two clients' slots for one
     stack.close()
+
+
+def test_adapters_of_another_batch_are_refused():
+    """What the record and the workspace were not made for reaches no kernel."""
+    stack, other = (ServerStack(2, 256, 4, 512, 32, "bf16") for _ in range(2))
+    batch = BatchDesc([0, 8, 20], [0, 1, 2])
+    ad = _adapters(1, 8, 256, 2, "bf16", 0)
+    adapters = StackAdapters(stack, batch, [0, -1], ad)
+    adapters.check(stack, batch)
+    for s, b, backward in ((other, batch, False),                              # its workspace is another size
+                           (stack, BatchDesc([0, 8, 14, 20], [0, 1, 2, 3]), False),  # three clients, two slots
+                           (stack, BatchDesc([0, 8, 21], [0, 1, 2]), False),   # v of 20 rows
+                           (stack, batch, True)):                              # forward only
+        with pytest.raises(FlglmError):
+            adapters.check(s, b, backward)
+    x = torch.zeros((20, 256), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(FlglmError):
+        stack.forward(BatchDesc([0, 8, 14, 20], [0, 1, 2, 3]), [{}, {}], x, torch.empty_like(x), None, x, adapters=adapters)
+    with pytest.raises(FlglmError):
+        stack.backward(batch, [{}, {}], [{}, {}], x, x, x, torch.empty_like(x), x, adapters=adapters)
+    other.close()
+    stack.close()
+
+
+def test_adapters_keep_their_tensors():
+    """The record holds addresses: a tensor replaced in its dict stays alive."""
+    stack = ServerStack(2, 256, 4, 512, 32, "bf16")
+    ad = _adapters(1, 8, 256, 2, "bf16", 0)
+    adapters = StackAdapters(stack, BatchDesc([0, 8], [0, 1]), [0], ad, _zeros(ad))
+    held = [t.data_ptr() for t in adapters.tensors]
+    for d in ad:
+        d["a"] = d["b"] = None
+    assert [p for la in adapters.record.layers[:2] for p in (la.a, la.b)] == held[:4]
+    assert [p for la in adapters.record.grads[:2] for p in (la.a, la.b)] == held[4:]
+    stack.close()
