@@ -76,6 +76,7 @@ __device__ __forceinline__ double block_sum(double v) {
 // fp32: one 305 us, four 262 us, 6.1 TB/s).
 constexpr int kBatch = 4;
 
+// Sums of squares, one partial a workgroup; bound by the reads.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) square_kernel(NormTable t, int chunk, double* part) {
   const int k = find(t, blockIdx.x);
@@ -117,6 +118,8 @@ __global__ void __launch_bounds__(kThreads) square_kernel(NormTable t, int chunk
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
+// One workgroup adds the partials (4096 at most from one tensor of 0.4 G: 4 us,
+// of which most is the launch).
 constexpr int kFinish = 1024;
 __global__ void __launch_bounds__(kFinish) finish_kernel(const double* part, int64_t n, double max_norm, float* out) {
   double a = 0;
@@ -136,9 +139,10 @@ __global__ void __launch_bounds__(kFinish) finish_kernel(const double* part, int
 
 // Eight elements a lane and done: the chip then sweeps through memory in order,
 // which reads and writes faster than as many workgroups each in a stretch of
-// its own (0.4 G fp32: 585 us; 128 K elements a workgroup 640, with
+// its own (0.4 G fp32: 540 us, 6.0 TB/s; 128 K elements a workgroup 640, with
 // non-temporal stores 690).  From the last element to the first: what the norm
-// read last is in the last-level cache.
+// read last is in the last-level cache (norm and clipping of 300 MB 153 us,
+// of 400 MB 243; from the first on 180 and 260; past 1 GB within 1 %).
 template <typename T>
 __global__ void __launch_bounds__(kThreads) scale_kernel(Table t, const float* norm_coef) {
   const float c = norm_coef[1];

@@ -20,6 +20,11 @@
 //    adds the losses in pair order.
 //  * gradient kernel: one pass over the logits.
 //
+// Measured on one MI355X, 8 pairs, 4910 rows of which 3671 carry a label, 130528
+// bf16 columns: row 205 us (0.96 GB, 4.7 TB/s; bound by the reads), pair 12 us
+// (8 workgroups' latency of a few dependent loads), gradient 414 us (0.96 GB
+// read, 1.28 GB written, 5.4 TB/s).
+//
 // Sums of exponentials are fp32 (values in [0, 1], at most 2^24 of them, added
 // in parts); log-probabilities and their sums over a sequence are 64 bits,
 // because z is a difference of sums of hundreds of rows.
@@ -39,11 +44,11 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kRowThreads = 512;
-constexpr double kLn2 = 0.69314718055994530942;
+constexpr double kLn2 = 1.0 / (double)kLog2e;  // of the fp32 factor, so that M kLn2 gives a row's maximum back
 constexpr int kPairsArg = 128;       // pairs whose bounds travel in one launch's kernel arguments
 constexpr int kMaxSplits = 16;
 constexpr int kBatch = 4;            // loads of a lane in flight
-constexpr long kWantGroups = 2048;   // workgroups that fill the chip
+constexpr long kWantGroups = 2048;   // workgroups that fill the chip, four a CU, twice
 
 // Exponentials are powers of two: with M the running maximum of x log2 e,
 // rounded to fp32 and then taken as it is, s = sum of 2^(x log2 e - M), the
@@ -51,6 +56,17 @@ constexpr long kWantGroups = 2048;   // workgroups that fill the chip
 // is rounded again in m log2 e would put an error of its own on every row.)
 __device__ __forceinline__ float exp2_less(float x, float M) {
   return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -M));
+}
+// The larger M, the more its rounding moves s: by 2^64 where |M| reaches 2^31,
+// and x log2 e overflows for the type's lowest values, with which logits are
+// masked.  So in a row whose maximum is past +-kFar, a logit past it counts as
+// +-kFar (a power of two: its M is exact), and a row of nothing but lowest
+// values is uniform.  Below an ordinary maximum such a logit gives 2^-infinity
+// = 0 as it is.
+constexpr float kFar = 0x1p30f;
+__device__ __forceinline__ bool far_row(float M) { return fabsf(M) >= kFar * kLog2e; }
+__device__ __forceinline__ float saturate(float x) {  // infinities and NaN stay
+  return fabsf(x) < INFINITY && fabsf(x) > kFar ? copysignf(kFar, x) : x;
 }
 
 // (M, s) pairs; an empty part is (-inf, 0).
@@ -75,12 +91,20 @@ __device__ __forceinline__ void take(float& m, float& s, const Vec8<T> (&v)[N]) 
   for (int u = 0; u < N; ++u)
 #pragma unroll
     for (int k = 0; k < 8; ++k) top = fmaxf(top, v[u].get(k));
-  const float mx = fmaxf(m, top * kLog2e);
-  if (mx == -INFINITY) {  // masked columns only so far, or NaN, which a maximum passes over
-#pragma unroll
+  float mx = fmaxf(m, top * kLog2e);
+  if (far_row(mx)) {  // nothing but masked columns so far, infinities, or NaN, which a maximum passes over
+    mx = fmaxf(m, saturate(top) * kLog2e);
+    float sum = 0.f;
     for (int u = 0; u < N; ++u)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) m = v[u].get(k) != v[u].get(k) ? v[u].get(k) : m;
+      for (int k = 0; k < 8; ++k) {
+        const float x = saturate(v[u].get(k));
+        if (mx > -INFINITY) sum += exp2_less(x, mx);
+        else m = x != x ? x : m;
+      }
+    if (mx > -INFINITY) {
+      s = s * (m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx)) + sum;
+      m = mx;
+    }
     return;
   }
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
@@ -95,7 +119,7 @@ __device__ __forceinline__ void take(float& m, float& s, const Vec8<T> (&v)[N]) 
 // Columns [c0, c1) of each labelled row: part[row][split] = (M, s).
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) pref_row_kernel(const T* logits, long ld, int V, int cols,
-                                                            const int32_t* labels, float2* part, uint32_t* done) {
+                                                               const int32_t* labels, float2* part, uint32_t* done) {
   const long t = blockIdx.x;
   const int sp = blockIdx.y;
   if (t == 0 && sp == 0 && threadIdx.x == 0) *done = 0;  // the pair kernel's count, of the launch behind this one
@@ -169,13 +193,13 @@ __global__ void __launch_bounds__(kThreads) pref_pair_kernel(PairArgs a, const T
     const int lab = labels[t];
     f32x4 f = {0.f, 0.f, 0.f, 0.f};
     if (lab >= 0 && lab < V) {
-      const float x = to_f32(logits[(long)t * ld + lab]);
-      float m = -INFINITY, s = 0.f;
+      float x = to_f32(logits[(long)t * ld + lab]), m = -INFINITY, s = 0.f;
 #pragma unroll 4
       for (int k = 0; k < splits; ++k) {
         const float2 q = part[(long)t * splits + k];
         join(m, s, q.x, q.y);
       }
+      if (far_row(m)) x = saturate(x);
       const double l = (double)x - ((double)m * kLn2 + log((double)s));
       lp[0] += t < r1 ? l : 0.0;
       lp[1] += t < r1 ? 0.0 : l;
@@ -214,7 +238,8 @@ __global__ void __launch_bounds__(kThreads) pref_pair_kernel(PairArgs a, const T
   // every pair's loss is written: added in pair order, whichever came last
   __threadfence();
   double sum = 0;
-  for (int i = threadIdx.x; i < a.pairs; i += kThreads) sum += (double)__hip_atomic_load(loss + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  for (int i = threadIdx.x; i < a.pairs; i += kThreads)
+    sum += (double)__hip_atomic_load(loss + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   sum = block_sum(sum, sh);
   if (threadIdx.x == 0) *loss_sum = (float)sum;
 }
@@ -242,6 +267,9 @@ __global__ void __launch_bounds__(kThreads) pref_grad_kernel(const T* logits, lo
     const float ks = -scale * f[1];
 #pragma unroll
     for (int k = 0; k < 8; ++k) g[k] = ks * exp2_less(v.get(k), f[0]);
+    if (far_row(f[0])) {
+      for (int k = 0; k < 8; ++k) g[k] = ks * exp2_less(saturate(v.get(k)), f[0]);
+    }
     if ((unsigned)(lab - j0) < 8u) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) g[k] += j0 + k == lab ? scale * f[2] : 0.f;

@@ -185,6 +185,32 @@ def test_a_label_without_probability():
             assert (dl == 0).all()
 
 
+@pytest.mark.parametrize("V", [64, 1000, 33000])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_columns_masked_by_the_lowest_value(V, dt):
+    """The type's lowest value in some columns is -infinity there."""
+    x, labels, cu, ref, batch = _case([4, 5, 2, 7], V, dt, masked=V // 3)
+    y = x.clone()
+    y[:, V - V // 3:] = torch.finfo(DT[dt]).min
+    got = _run(y, labels, cu, ref, batch, V, dt, eps=0.1)[1:]
+    _check(x, V, labels, cu, ref, 0.2, 0.1, 0.5, dt, *got)
+
+
+@pytest.mark.parametrize("V", [8, 1000, 33000])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("value", ["min", "max"])
+def test_rows_of_nothing_but_the_extreme_value(value, V, dt):
+    """All columns at the type's lowest (or highest) value: a uniform row, its log
+    probability -ln V and its gradient that of 1 / V; bounds as for any row."""
+    x, labels, cu, ref, batch = _case([3, 4], V, dt, unlabelled=0.0)
+    y = x.clone()
+    y[1] = y[5] = getattr(torch.finfo(DT[dt]), value)
+    flat = x.clone()
+    flat[1] = flat[5] = 0
+    _, logp, loss, total, dl = _run(y, labels, cu, ref, batch, V, dt)
+    _check(flat, V, labels, cu, ref, 0.2, 0.0, 0.5, dt, logp, loss, total, dl)
+
+
 def test_nan_reaches_its_own_pair_only():
     x, labels, cu, ref, batch = _case([4, 5, 6, 3], 1000, "f32", unlabelled=0.0)
     _, logp, loss, _, dl = _run(x, labels, cu, ref, batch, 1000, "f32")
