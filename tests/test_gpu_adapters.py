@@ -234,6 +234,39 @@ def test_infinities_and_nan_stay_in_their_rows():
     assert not torch.isfinite(v2[3]).any() and torch.isnan(y2[44].float()).all()
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("r", [8, 40])
+def test_nan_in_a_gradient_stays_with_its_slot(r, dt):
+    """NaN and infinities in dy and x: a client without an adapter passes none on,
+    a client with one spoils its slot's gradients and its own row of dx only."""
+    batch, rows = _batch([[20], [20], [20], [7]])
+    slots = [0, -1, 1, 0]
+    d = _inputs(67, 2, r, 64, 96, dt, 8)
+    op = ClientAdapters(2, r, 64, 96, dt, 1.0)
+    ws = op.workspace(batch)
+
+    def run(x, dy):
+        y, v = torch.empty((67, 96), dtype=DT[dt], device="cuda"), torch.empty((67, r), device="cuda")
+        op.forward(batch, slots, x, d["a"], d["b"], None, y, v, ws)
+        dx = torch.empty_like(x)
+        da, db = torch.zeros((2, r, 64), device="cuda"), torch.zeros((2, 96, r), device="cuda")
+        op.backward(batch, slots, dy, x, d["a"], d["b"], v, d["dres"], dx, da, db, ws)
+        return dx, da, db
+
+    dx, da, db = run(d["x"], d["dy"])
+    x, dy = d["x"].clone(), d["dy"].clone()
+    x[25, 7], dy[26, 3], dy[39] = float("nan"), float("inf"), float("nan")  # no adapter
+    for p, q in zip((dx, da, db), run(x, dy)):
+        assert torch.equal(p, q)
+    x[3, 5], dy[64, 2] = float("inf"), float("nan")  # slot 0
+    dx2, da2, db2 = run(x, dy)
+    assert torch.equal(da[1], da2[1]) and torch.equal(db[1], db2[1])
+    keep = torch.ones(67, dtype=torch.bool)
+    keep[64] = False
+    assert torch.equal(dx[keep], dx2[keep]) and torch.isnan(dx2[64].float()).all()
+    assert not torch.isfinite(da2[0]).all() and not torch.isfinite(db2[0]).all()
+
+
 def test_results_repeat_bit_for_bit():
     d, batch, rows, op, ws, y, v, dx, da, db = _run([[300], [150], [333]], [0, 1, 0], 2, 16, 512, 768, "bf16")
     first = None
