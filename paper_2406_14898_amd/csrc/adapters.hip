@@ -19,9 +19,10 @@
 // 1 GiB moves 5.0 TB/s here, reads alone 6.2):
 //   forward, 41447 rows, 4096 -> 12288, rank 16, 32 clients: 2.35 GB in 480 us
 //     (down 99 us, 3.4 TB/s of reads; up 385 us, 5.3 TB/s)
-//   backward, 41447 rows, 4096 -> 12288 without dres: 2.05 GB in 456 us (out 211,
-//     dv_sum 6, in 207, join 16)
-//   one row, 4096 -> 12288: 6.4 us for both forward kernels
+//   backward, the same and dres: 2.05 GB in 456 us (out 211, dv_sum 6, in 207,
+//     join 16)
+//   64 clients of one token, 4096 -> 12288, rank 16: 34 MB in 15.7 us
+//   one token, rank 8: 6.1 us
 //
 // v and dv are fp32.  In bf16 mode a matrix product with them runs on the bf16
 // matrix cores in parts: v = v0 + v1 (+ v2), each part the bf16 nearest to
@@ -184,7 +185,6 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
     return;
   }
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
-  const int tiles = (rows + 15) / 16;
   const Buf xb = rows_of(x, row0, ldx, rows, in), ab = rows_of(a, (long)slot * r, in, r, in);
   f32x4 acc[NI][RT];
 #pragma unroll
@@ -199,48 +199,65 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
   struct Step {
     Vec8<T> av[2][RT], xv[2][NI];
   };
-  auto load = [&](Step& s, int k, int count) {
+  auto load = [&](Step& s, int k) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int c = 64 * k + 16 * g + 8 * h;
       const uint32_t xo = col_off<T>(m, ldx, c, in), ao = col_off<T>(m, in, c, in);
 #pragma unroll
-      for (int i = 0; i < NI; ++i)
-        if (i < count) buf_ld8(s.xv[h][i], xb, xo + i * xrow);
+      for (int i = 0; i < NI; ++i) buf_ld8(s.xv[h][i], xb, xo + i * xrow);
 #pragma unroll
       for (int j = 0; j < RT; ++j) buf_ld8(s.av[h][j], ab, ao + j * arow);
     }
   };
-  auto multiply = [&](Step& s, int count) {
+  auto multiply = [&](Step& s) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < NI; ++i)
-        if (i < count) {
 #pragma unroll
-          for (int j = 0; j < RT; ++j) acc[i][j] = mma16(s.xv[h][i].frag(), s.av[h][j].frag(), acc[i][j]);
-        }
+        for (int j = 0; j < RT; ++j) acc[i][j] = mma16(s.xv[h][i].frag(), s.av[h][j].frag(), acc[i][j]);
   };
   int k = blockIdx.y * kWaves + w;
-  if (tiles == NI) {
-    // two steps in flight in turn (past the last they read zero)
-    Step s0, s1;
-    load(s0, k, NI);
-    for (; k < nk; k += 2 * stride) {
-      load(s1, k + stride, NI);
-      __builtin_amdgcn_sched_barrier(0);  // or the loads sink to their uses
-      multiply(s0, NI);
+  if (rows <= 16) {
+    // one token, or a few: more steps in flight, and no loads of rows that do not
+    // exist (64 clients of one token, 4096 -> 12288, rank 16: the forward 15.7 us,
+    // through the code below 16.7)
+    constexpr int U = sizeof(T) == 2 ? (RT == 1 ? 4 : RT == 2 ? 3 : 2) : (RT == 1 ? 2 : 1);
+    for (; k < nk; k += U * stride) {
+      Vec8<T> av[U][2][RT], xv[U][2];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int c = 64 * (k + u * stride) + 16 * g + 8 * h;
+          const uint32_t ao = col_off<T>(m, in, c, in);
+          buf_ld8(xv[u][h], xb, col_off<T>(m, ldx, c, in));
+#pragma unroll
+          for (int j = 0; j < RT; ++j) buf_ld8(av[u][h][j], ab, ao + j * arow);
+        }
       __builtin_amdgcn_sched_barrier(0);
-      load(s0, k + 2 * stride, NI);
-      __builtin_amdgcn_sched_barrier(0);
-      multiply(s1, NI);
-      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < RT; ++j) acc[0][j] = mma16(xv[u][h].frag(), av[u][h][j].frag(), acc[0][j]);
     }
   } else {
-    Step s0;
-    for (; k < nk; k += stride) {
-      load(s0, k, tiles);
-      multiply(s0, tiles);
+    // two steps in flight in turn (past the last they read zero, and so do rows
+    // past a tile's last)
+    Step s0, s1;
+    load(s0, k);
+    for (; k < nk; k += 2 * stride) {
+      load(s1, k + stride);
+      __builtin_amdgcn_sched_barrier(0);  // or the loads sink to their uses
+      multiply(s0);
+      __builtin_amdgcn_sched_barrier(0);
+      load(s0, k + 2 * stride);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(s1);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 #pragma unroll
@@ -261,10 +278,12 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
 
 // y = base + scale v B^T on one 64-row tile and 256 columns; v the sum of
 // `parts` partial reductions (parts > 1: also stored to v_out).
+// (Five waves a SIMD, of 96 registers, instead of the four of more: 64 clients
+// of one token 15.7 us instead of 16.5, 41447 rows 484 instead of 480.)
 template <typename T, int RP>
-__global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, int parts, long total_rows,
-                                                      float* v_out, const T* b, int r, int out_features, float scale,
-                                                      const T* base, long ldb, T* y, long ldy) {
+__global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RP <= 32 ? 5 : 1))
+    up_kernel(Segs t, const float* v, int parts, long total_rows, float* v_out, const T* b, int r, int out_features,
+              float scale, const T* base, long ldb, T* y, long ldy) {
   using U = Up<T, RP>;
   __shared__ __align__(16) T sh[kTile][U::stride];
   const int cols = (out_features + kUpCols - 1) / kUpCols;
@@ -309,15 +328,21 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
     auto stage = [&](auto count) {
       constexpr int n = decltype(count)::value;
       float f[n] = {};
-      for (int q = 0; q < parts; ++q) {
-        const Buf vb = rows_of(v + q * total_rows * r, row0, r, rows, r);
-        const uint32_t off = col_off<float>(row, r, rank, r);
-        float part[n];
+      constexpr int nq = n <= 8 ? 4 : 2;  // parts at once
+      const uint32_t off = col_off<float>(row, r, rank, r);
+      for (int q0 = 0; q0 < parts; q0 += nq) {
+        float part[nq][n];
 #pragma unroll
-        for (int i = 0; i < n; ++i) part[i] = buf_ldf(vb, off + i * (kRows * 4) * (uint32_t)r);
+        for (int q = 0; q < nq; ++q) {
+          const Buf vb = rows_of(v + (q0 + q) * total_rows * r, row0, r, q0 + q < parts ? rows : 0, r);
+#pragma unroll
+          for (int i = 0; i < n; ++i) part[q][i] = buf_ldf(vb, off + i * (kRows * 4) * (uint32_t)r);
+        }
         __builtin_amdgcn_sched_barrier(0);  // all loads before the first sum
 #pragma unroll
-        for (int i = 0; i < n; ++i) f[i] += part[i];
+        for (int q = 0; q < nq; ++q)
+#pragma unroll
+          for (int i = 0; i < n; ++i) f[i] += part[q][i];
       }
       const Buf ob = rows_of(cb == 0 ? v_out : nullptr, row0, r, rows, r);
 #pragma unroll
@@ -374,10 +399,13 @@ __global__ void __launch_bounds__(kThreads) up_kernel(Segs t, const float* v, in
 #pragma unroll
     for (int i = 0; i < kTile / 16; ++i) rows16(i, bs[i]);
   } else {
+    Vec8<T> bs[2], next[2];
+    load16(0, bs);
     for (int i = 0; 16 * i < rows; ++i) {
-      Vec8<T> bs[2];
-      load16(i, bs);
+      load16(i + 1, next);  // past the last row: zero
       rows16(i, bs);
+      bs[0] = next[0];
+      bs[1] = next[1];
     }
   }
 }
@@ -916,7 +944,8 @@ void fill(const std::vector<Run>& runs, size_t* i, int rows_a_step, Segs* t) {
 // do not fill the chip; every wave has a step at least.  `up` adds the parts in
 // every block of columns, which is why they are few (4096 -> 4096, rank 64, one
 // client of 128 rows: 8 parts 16 us, 16 parts 18; 2048 rows: 7 parts 26 us, 16
-// 33, none 44; 64 clients of one row, rank 16: 3 parts 17.7 us, none 21).
+// 33, none 44; 64 clients of one row, rank 16: 3 parts 17.7 us, none 21; all
+// before `up` had the loads of four parts in flight).
 int splits_of(const fl_adapter_desc* d, const fl_batch_desc* b) {
   const long tiles = b->total_tokens / kTile + b->num_clients;
   return (int)std::max(1L, std::min<long>({256 / tiles, d->in_features / (64 * kWaves), 8}));
