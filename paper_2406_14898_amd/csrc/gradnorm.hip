@@ -177,10 +177,11 @@ int launch_status() {
 }
 
 // Elements of a chunk: enough chunks to fill the chip, few enough that the
-// partials stay small.
+// partials stay small, and a whole batch of loads at least (norm and clipping of
+// 52 tensors, 6.8 M fp32 elements: 19.7 us; one step a chunk 21.2).
 int chunk_of(int64_t total) {
   const int64_t want = (total / 4096 + kStep - 1) / kStep * kStep;
-  return (int)std::min<int64_t>(std::max<int64_t>(want, kStep), 64 * kStep);
+  return (int)std::min<int64_t>(std::max<int64_t>(want, kBatch * kStep), 64 * kStep);
 }
 
 // The tensors' count and sizes; total elements and chunks.
