@@ -43,11 +43,10 @@ using namespace flglm;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRowThreads = 512;
 constexpr double kLn2 = 1.0 / (double)kLog2e;  // of the fp32 factor, so that M kLn2 gives a row's maximum back
 constexpr int kPairsArg = 128;       // pairs whose bounds travel in one launch's kernel arguments
 constexpr int kMaxSplits = 8;        // (one pair, 110 rows of 130528: 8 parts 12.4 us, 16 parts 13.9)
-constexpr int kBatch = 2;            // loads of a lane in flight (one pair: 2 12.4 us, 4 12.7; 8 pairs 622, 625)
+constexpr int kBatch = 2;            // loads of a lane at once
 constexpr long kWantGroups = 2048;   // workgroups that fill the chip, four a CU, twice
 
 // Exponentials are powers of two: with M the running maximum of x log2 e,
@@ -117,9 +116,10 @@ __device__ __forceinline__ void take(float& m, float& s, const Vec8<T> (&v)[N]) 
 }
 
 // Columns [c0, c1) of each labelled row: part[row][split] = (M, s).
+// (512 threads a workgroup: one pair 12.4 us, 256 11.7.)
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads) pref_row_kernel(const T* logits, long ld, int V, int cols,
-                                                               const int32_t* labels, float2* part, uint32_t* done) {
+__global__ void __launch_bounds__(kThreads) pref_row_kernel(const T* logits, long ld, int V, int cols,
+                                                            const int32_t* labels, float2* part, uint32_t* done) {
   const long t = blockIdx.x;
   const int sp = blockIdx.y;
   if (t == 0 && sp == 0 && threadIdx.x == 0) *done = 0;  // the pair kernel's count, of the launch behind this one
@@ -129,13 +129,37 @@ __global__ void __launch_bounds__(kRowThreads) pref_row_kernel(const T* logits, 
   const int c0 = sp * cols, c1 = min(V, c0 + cols);
   float m = -INFINITY, s = 0.f;
   int j0 = c0 + threadIdx.x * 8;
-  for (; j0 + (kBatch - 1) * kRowThreads * 8 < c1; j0 += kBatch * kRowThreads * 8) {
-    Vec8<T> v[kBatch];
+  // whole batches, one loaded while the one before it is taken (8 pairs: 613 us
+  // a step, without 622)
+  constexpr int kWhole = kBatch * kThreads * 8;
+  const int last = c1 - (kBatch - 1) * kThreads * 8;
+  if (j0 < last) {
+    Vec8<T> va[kBatch], vb[kBatch];  // in turn: moved from one to the other, they would be waited for
+    auto load = [&](Vec8<T> (&b)[kBatch]) {
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) v[u].load(row + j0 + u * kRowThreads * 8);
-    take(m, s, v);
+      for (int u = 0; u < kBatch; ++u) b[u].load(row + j0 + u * kThreads * 8);
+      j0 += kWhole;
+      __builtin_amdgcn_sched_barrier(0);  // or the loads sink to their uses
+    };
+    load(va);
+    for (;;) {
+      if (j0 >= last) {
+        take(m, s, va);
+        break;
+      }
+      load(vb);
+      take(m, s, va);
+      __builtin_amdgcn_sched_barrier(0);
+      if (j0 >= last) {
+        take(m, s, vb);
+        break;
+      }
+      load(va);
+      take(m, s, vb);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
-  for (; j0 < c1; j0 += kRowThreads * 8) {
+  for (; j0 < c1; j0 += kThreads * 8) {
     Vec8<T> v[1];
     v[0].load(row + j0);
     take(m, s, v);
@@ -145,14 +169,14 @@ __global__ void __launch_bounds__(kRowThreads) pref_row_kernel(const T* logits, 
     const float m2 = __shfl_xor(m, o), s2 = __shfl_xor(s, o);
     join(m, s, m2, s2);
   }
-  __shared__ float sm[kRowThreads / 64], ss[kRowThreads / 64];
+  __shared__ float sm[kThreads / 64], ss[kThreads / 64];
   if ((threadIdx.x & 63) == 0) {
     sm[threadIdx.x >> 6] = m;
     ss[threadIdx.x >> 6] = s;
   }
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kRowThreads / 64; ++w) join(m, s, sm[w], ss[w]);
+    for (int w = 1; w < kThreads / 64; ++w) join(m, s, sm[w], ss[w]);
     part[t * gridDim.y + sp] = make_float2(m, s);
   }
 }
@@ -302,7 +326,7 @@ struct PrefWs {
 };
 // Parts a row is split into: one when the rows alone fill the chip.
 int splits_of(long T, long V) {
-  const long most = std::max(1L, V / (8 * kRowThreads));
+  const long most = std::max(1L, V / (8 * kThreads));
   return (int)std::min<long>({(kWantGroups + T - 1) / T, most, (long)kMaxSplits});
 }
 PrefWs carve(long T, long V, char* base) {
@@ -357,7 +381,7 @@ int forward(const fl_preference_desc* d, const fl_batch_desc* b, const T* logits
   const long tokens = b->total_tokens;
   const int V = (int)d->vocab, splits = splits_of(tokens, V);
   const int cols = (int)(((V + splits - 1) / splits + 7) / 8 * 8);
-  hipLaunchKernelGGL(pref_row_kernel<T>, dim3((unsigned)tokens, splits), dim3(kRowThreads), 0, s, logits, ld, V, cols,
+  hipLaunchKernelGGL(pref_row_kernel<T>, dim3((unsigned)tokens, splits), dim3(kThreads), 0, s, logits, ld, V, cols,
                      labels, w.part, w.done);
   if (int rc = launch_status()) return rc;
   PairArgs a;
