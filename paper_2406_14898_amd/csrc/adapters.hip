@@ -472,14 +472,16 @@ __device__ __forceinline__ void load_tile(Vec8<T> (&xr)[8], const T* x, long ld,
 }
 
 // acc[j][q] += X^T W over the tile's 32 rows (xt: the tile turned): columns
-// 8 m + j, ranks 16 q + n.
-template <typename T, int RT>
-__device__ __forceinline__ void outer(f32x4 (&acc)[8][RT], const Vec8<T> (&xt)[8], const T* wt, int m, int g) {
+// 8 m + j, ranks 16 q + n.  between() runs before each eight products.
+template <typename T, int RT, typename F>
+__device__ __forceinline__ void outer(f32x4 (&acc)[8][RT], const Vec8<T> (&xt)[8], const T* wt, int m, int g,
+                                      F&& between) {
   constexpr int NP = Parts<T>::exact;
 #pragma unroll
   for (int p = 0; p < NP; ++p)
 #pragma unroll
     for (int q = 0; q < RT; ++q) {
+      between();
       Vec8<T> f;
       f.load(wt + ((long)p * 16 * RT + 16 * q + m) * kTokStride + 8 * g);
 #pragma unroll
@@ -516,10 +518,12 @@ template <int RP, int NT> struct Factor {
 // [r0, r0 + 16 RT): ranks past 32 are two slices, each with workgroups of its
 // own, because the sums of 64 would leave no registers to overlap anything in.
 // The slices of a tile run eight workgroups apart, so on one XCD and its L2.
-// A step: the tile (loaded during the step before) goes to the wave's own LDS
-// in rows, and through registers, turned, into dB; dv reads the rows back and
-// leaves its result in their place; one barrier, and the waves' results are
-// added.
+// A step: the tile (loaded two steps before) goes to the wave's own LDS in rows,
+// and through registers, turned, into dB; dv reads the rows back and leaves its
+// result in their place; one barrier, and the waves' results are added.  Reading
+// dy alone in this order takes 150 us for 1.02 GB; with a store of dv's size a
+// step beside it 182, whatever its order or place; this kernel 200 (with one
+// tile ahead 211).
 template <typename T, int RT>
 __global__ void __launch_bounds__((64 * OutWaves<T>::n))
     bwd_out_kernel(Segs t, Slots sl, const T* dy, long lddy, const T* b, const float* v, int stride, int out_features,
@@ -546,21 +550,12 @@ __global__ void __launch_bounds__((64 * OutWaves<T>::n))
     settle(tid);  // addresses are formed anew for each slot: held across slots, they would not fit the registers
     const int lane = tid & 63, w = uniform(tid >> 6), m = lane & 15, g = lane >> 4;
     const int c0 = cb * 128 * NW + 128 * w;
+    // this step's rows and the next one's (none: 0)
     int row0, row1 = 0;
     int rows = wk.next(t, &row0), rows1 = 0;
-    Vec8<T> xr[8], xn[8], xt[8];
-    Factor<RP, NT> vn;
-    vn.load(v, row0, rows, stride, r, tid);
-    load_tile(xr, dy, lddy, row0, rows, c0, out_features, m, g);
-    auto stage = [&](T* dst) {
-#pragma unroll
-      for (int i = 0; i < Factor<RP, NT>::n; ++i) {
-        const int row = Factor<RP, NT>::row(tid, i), c = Factor<RP, NT>::rank(tid);
-        float f = vn.f[i];
-#pragma unroll
-        for (int p = 0; p < NP; ++p) dst[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
-      }
-    };
+    Vec8<T> xa[8], xb[8], xt[8];
+    Factor<RP, NT> va, vb;
+    va.load(v, row0, rows, stride, r, tid);
     // B as the second operand of dv = dy B: rank 16 q + m, columns 32 k + 8 g ..
     const Buf bs = rows_of(b, (long)slot * out_features + c0, stride, min(128, out_features - c0), r);
     frag_t<T> bf[4][RT];
@@ -572,26 +567,50 @@ __global__ void __launch_bounds__((64 * OutWaves<T>::n))
 #pragma unroll
         for (int e = 0; e < 8; ++e) bf[k][q][e] = buf_ld1(bs, off + e * (uint32_t)(stride * sizeof(T)), (T*)nullptr);
       }
+    load_tile(xa, dy, lddy, row0, rows, c0, out_features, m, g);
+    if (wk.step < wk.end) rows1 = wk.next(t, &row1);
+    vb.load(v, row1, rows1, stride, r, tid);
+    load_tile(xb, dy, lddy, row1, rows1, c0, out_features, m, g);
+    auto stage = [&](T* dst, const Factor<RP, NT>& vn) {
+#pragma unroll
+      for (int i = 0; i < Factor<RP, NT>::n; ++i) {
+        const int row = Factor<RP, NT>::row(tid, i), c = Factor<RP, NT>::rank(tid);
+        float f = vn.f[i];
+#pragma unroll
+        for (int p = 0; p < NP; ++p) dst[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
+      }
+    };
     f32x4 acc[8][RT];
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
       for (int q = 0; q < RT; ++q) acc[j][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-    stage(wt[0]);
+    stage(wt[0], va);
     lds_barrier();
-    for (int buf = 0;; buf ^= 1) {
-      const bool more = wk.step < wk.end;
-      if (more) {  // in flight until the next step begins
-        rows1 = wk.next(t, &row1);
-        vn.load(v, row1, rows1, stride, r, tid);
-        load_tile(xn, dy, lddy, row1, rows1, c0, out_features, m, g);
-      }
+    // One step: its tile xr, its factor's registers vc (staged already) and the
+    // next step's factor vn.  xr and vc are loaded anew for the step after the
+    // next, between the products: eight loads at once would hold the wave up.
+    auto step = [&](int buf, Vec8<T> (&xr)[8], Factor<RP, NT>& vc, const Factor<RP, NT>& vn) {
       T* mine = tile[buf][w];
 #pragma unroll
       for (int i = 0; i < 8; ++i) xr[i].store(mine + (8 * g + i) * kRow + 8 * m);
       transpose8x8(xr, xt);
+      int row2 = 0, rows2 = 0;
+      if (wk.step < wk.end) rows2 = wk.next(t, &row2);
+      __builtin_amdgcn_sched_barrier(0);
+      vc.load(v, row2, rows2, stride, r, tid);
+      __builtin_amdgcn_sched_barrier(0);
+      const Buf from = rows_of(dy, row2, lddy, rows2, out_features);
+      const uint32_t off2 = col_off<T>(8 * g, lddy, c0 + 8 * m, out_features), row_bytes = (uint32_t)lddy * sizeof(T);
+      int fetched = 0;
+      auto fetch = [&] {
+        if (fetched == 8) return;
+        buf_ld8<kOnce>(xr[fetched], from, off2 + fetched * row_bytes);
+        ++fetched;
+        __builtin_amdgcn_sched_barrier(0x387);  // products and global memory stay in order, all else may pass
+      };
       __builtin_amdgcn_wave_barrier();
-      outer<T, RT>(acc, xt, wt[buf], m, g);
+      outer<T, RT>(acc, xt, wt[buf], m, g, fetch);
       f32x4 d[2][RT];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -599,6 +618,7 @@ __global__ void __launch_bounds__((64 * OutWaves<T>::n))
         for (int q = 0; q < RT; ++q) d[h][q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
+          fetch();
           Vec8<T> f;
           f.load(mine + (16 * h + m) * kRow + 32 * k + 8 * g);
 #pragma unroll
@@ -614,7 +634,7 @@ __global__ void __launch_bounds__((64 * OutWaves<T>::n))
         for (int q = 0; q < RT; ++q)
 #pragma unroll
           for (int e = 0; e < 4; ++e) dvs[(16 * h + 4 * g + e) * kDv + 16 * q + m] = d[h][q][e];
-      if (more) stage(wt[buf ^ 1]);
+      stage(wt[buf ^ 1], vn);
       lds_barrier();
       const Buf dst = rows_of(dv_part + cb * total_rows * stride, row0, stride, rows, r);
       const uint32_t off = col_off<float>(Factor<RP, NT>::row(tid, 0), stride, Factor<RP, NT>::rank(tid), r);
@@ -627,17 +647,24 @@ __global__ void __launch_bounds__((64 * OutWaves<T>::n))
         __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(scale * s), dst,
                                               off + i * (NT / RP * 4) * (uint32_t)stride, 0, 0);
       }
-      if (!more) break;
       row0 = row1;
       rows = rows1;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) xr[i] = xn[i];
+      row1 = row2;
+      rows1 = rows2;
+    };
+    // by twos: left in the middle, the loop would wait for all loads at its head
+    while (rows1 > 0) {
+      step(0, xa, va, vb);
+      step(1, xb, vb, va);
     }
-    // all of the old gradient is read before any is written: one latency
+    if (rows > 0) step(0, xa, va, vb);
+    // all of the old gradient (a part has none: zeros) is read before any is
+    // written: one latency
     const bool add = part < 0;
     const long matrix = (long)out_features * stride;
-    const Buf dst = rows_of(add ? db + slot * matrix : db_part + part * matrix, c0, stride,
-                            min(128, out_features - c0), r);
+    float* sums = add ? db + slot * matrix : db_part + part * matrix;
+    const int cols_left = min(128, out_features - c0);
+    const Buf dst = rows_of(sums, c0, stride, cols_left, r), src = rows_of(sums, c0, stride, add ? cols_left : 0, r);
 #pragma unroll
     for (int q = 0; q < RT; ++q) {
       const uint32_t off = col_off<float>(32 * g, stride, 16 * q + m, r);
@@ -645,7 +672,7 @@ __global__ void __launch_bounds__((64 * OutWaves<T>::n))
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) old[j][e] = add ? buf_ldf(dst, off + (8 * e + j) * 4 * (uint32_t)stride) : 0.f;
+        for (int e = 0; e < 4; ++e) old[j][e] = buf_ldf(src, off + (8 * e + j) * 4 * (uint32_t)stride);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -782,7 +809,7 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
           load_tile(xr, x, ldx, row1, rows1, c0, in, m, g);
         }
       }
-      if (live) outer<T, RT>(acc, xt, wt[buf], m, g);
+      if (live) outer<T, RT>(acc, xt, wt[buf], m, g, [] {});
       if (dx) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -836,7 +863,8 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
     }
     if (!live) return;
     const bool add = part < 0;
-    const Buf dst = rows_of(add ? da + (long)slot * r * in : da_part + (long)part * r * in, 0, in, r, in);
+    float* sums = add ? da + (long)slot * r * in : da_part + (long)part * r * in;
+    const Buf dst = rows_of(sums, 0, in, r, in), src = rows_of(sums, 0, in, add ? r : 0, in);
 #pragma unroll
     for (int q = 0; q < RT; ++q) {
       Vec8<float> o[4];
@@ -844,8 +872,7 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         off[e] = 16 * q + m < r ? col_off<float>(16 * q + m, in, c0 + 8 * (4 * g + e), in) : kNowhere;
-        if (add) buf_ld8(o[e], dst, off[e]);
-        else o[e].zero();
+        buf_ld8(o[e], src, off[e]);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
