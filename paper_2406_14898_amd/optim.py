@@ -10,6 +10,7 @@ accumulates into (the gradient views), so one launch updates every tensor.
 
 from __future__ import annotations
 
+import ctypes
 from typing import Dict, Iterable, List, Optional, Sequence, Tuple
 
 from . import flglm as F
@@ -104,6 +105,7 @@ class GradNorm:
         self.kind = F.FL_F32 if self.dtype == torch.float32 else F.FL_BF16
         self.numel = [g.numel() for g in self.grads]
         self.sizes = F._sizes(self.numel)
+        self.array = ctypes.c_void_p * len(self.grads)
         self.workspace = torch.empty(F.fl_grad_norm_workspace_bytes(self.sizes), dtype=torch.uint8, device=dev)
         self.result = torch.empty(2, dtype=torch.float32, device=dev)  # norm, coefficient
         self.device = dev
@@ -111,27 +113,28 @@ class GradNorm:
     def norm(self, max_norm: float = float("inf"), stream=None):
         """Device fp32 [1]: the norm of the gradients' present values.  The
         coefficient min(1, max_norm / (norm + 1e-6)) is left in result[1]."""
-        self._norm(F.pointers([g.data_ptr() for g in self.grads]), max_norm, stream)
+        self._norm(self._addresses(self.grads), max_norm, stream)
         return self.result[:1]
 
     def clip(self, max_norm: float, out: Optional[Sequence] = None, stream=None):
         """Gradients times the coefficient, into `out` (tensors like the
         gradients; None: in place); returns the norm before."""
-        grads = F.pointers([g.data_ptr() for g in self.grads])
-        to = grads
+        grads = to = self._addresses(self.grads)
         if out is not None:
-            dev = F.current_device()
             if len(out) != len(self.numel):
                 raise F.FlglmError(F.FL_ERR_ARG, f"{len(out)} outputs for {len(self.numel)} gradients")
-            dt = self.dtype
-            for o, n in zip(out, self.numel):
-                if o.dtype is not dt or o.numel() != n or o.get_device() != dev or not o.is_contiguous():
-                    raise F.FlglmError(F.FL_ERR_ARG, f"an output is {tuple(o.shape)} {o.dtype} on {o.device}, expected "
-                                                     f"{n} contiguous elements like its gradient")
-            to = F.pointers([o.data_ptr() for o in out])
+            t = type(self.result)  # the checks one by one over all tensors: 52 of them 8 us, tensor by tensor 22
+            if not (list(map(t.numel, out)) == self.numel and {o.dtype for o in out} == {self.dtype} and
+                    set(map(t.get_device, out)) == {self.device} and all(map(t.is_contiguous, out))):
+                raise F.FlglmError(F.FL_ERR_ARG, f"an output is not as many contiguous elements as its gradient, in "
+                                                 f"{self.dtype} on device {self.device}")
+            to = self._addresses(out)
         self._norm(grads, max_norm, stream)
         F.fl_clip_grads(self.kind, grads, to, self.sizes, self.result, stream)
         return self.result[:1]
+
+    def _addresses(self, tensors):
+        return self.array(*map(type(self.result).data_ptr, tensors))
 
     def _norm(self, grads, max_norm, stream) -> None:
         if F.current_device() != self.device:

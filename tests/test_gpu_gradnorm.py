@@ -138,3 +138,19 @@ def test_the_workspace_is_only_as_large_as_asked():
     F.fl_grad_norm(F.FL_F32, grads, sizes, 1.0, res, ws, n)
     torch.cuda.synchronize()
     assert (ws[n:] == 77).all() and abs(float(res[0]) - _norm64(grads)) < 1e-4
+
+
+def test_outputs_unlike_the_gradients_are_refused():
+    """Nothing is launched: the gradients and outputs keep their values."""
+    grads = [torch.ones(40, device="cuda"), torch.ones((4, 8), device="cuda")]
+    op = GradNorm(grads)
+    good = [torch.zeros(40, device="cuda"), torch.zeros((4, 8), device="cuda")]
+    for bad in (good[:1], [good[0], good[1][:3]], [good[0], good[1].bfloat16()], [good[0], good[1].cpu()],
+                [good[0], torch.zeros((8, 8), device="cuda")[:, ::2].t()], [good[0], good[0][:32]],
+                [grads[1].new_zeros(40), grads[0][:32]]):
+        with pytest.raises(F.FlglmError):
+            op.clip(1.0, out=bad)
+    torch.cuda.synchronize()
+    assert all((g == 1).all() for g in grads) and all((o == 0).all() for o in good)
+    op.clip(1.0, out=good)
+    assert all((g == 1).all() for g in grads) and all(abs(float(o.max()) - 72 ** -0.5) < 1e-5 for o in good)
