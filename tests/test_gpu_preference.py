@@ -167,6 +167,17 @@ def test_full_vocabulary():
     _check(x, 130528, labels, cu, ref, 0.2, 0.0, 0.5, "bf16", *_run(x, labels, cu, ref, batch, 130528, "bf16")[1:])
 
 
+@pytest.mark.parametrize("dt,V", [("bf16", 16400), ("f32", 8200)])
+def test_a_gradient_larger_than_the_cache(dt, V):
+    """Two pairs at once, 203 MB of gradient, and each alone: the same bits."""
+    x, labels, cu, ref, batch = _case([1500, 1600, 1700, 1400], V, dt)
+    _, logp, loss, total, dl = _run(x, labels, cu, ref, batch, V, dt)
+    for p, (a, b) in enumerate(((0, 3100), (3100, 6200))):
+        one = BatchDesc([0, cu[2 * p + 1] - a, b - a], [0, 2])
+        _, l1, s1, _, d1 = _run(x[a:b], labels[a:b], one.cu, ref[2 * p:2 * p + 2], one, V, dt)
+        assert torch.equal(l1, logp[2 * p:2 * p + 2]) and torch.equal(s1, loss[p:p + 1]) and torch.equal(d1, dl[a:b])
+
+
 def test_a_label_without_probability():
     """A preferred label at a masked id: l = -inf, the loss infinite, the slope
     -beta, every gradient finite; on the rejected side the loss is 0."""
