@@ -17,10 +17,10 @@
 //
 // Measured on one MI355X, bf16, clients of one slot each (a plain copy of
 // 1 GiB moves 5.0 TB/s here, reads alone 6.2):
-//   forward, 41447 rows, 4096 -> 12288, rank 16, 32 clients: 2.35 GB in 480 us
-//     (down 99 us, 3.4 TB/s of reads; up 385 us, 5.3 TB/s)
-//   backward, the same and dres: 2.05 GB in 456 us (out 211, dv_sum 6, in 207,
-//     join 16)
+//   forward, 41447 rows, 4096 -> 12288, rank 16, 32 clients: 2.35 GB in 433 us
+//     (down 82 us, 4.1 TB/s of reads; up 355 us, 5.8 TB/s)
+//   backward, the same and dres: 2.05 GB in 412 us (out 194, dv_sum 6, in 190,
+//     join 13, the gradients' clearing)
 //   64 clients of one token, 4096 -> 12288, rank 16: 34 MB in 15.7 us
 //   one token, rank 8: 6.1 us
 //
@@ -114,12 +114,41 @@ __device__ __forceinline__ void buf_ld8(Vec8<float>& v, Buf b, uint32_t off) {
   v.r0 = buf_ld16<POLICY>(b, off);
   v.r1 = buf_ld16<POLICY>(b, off + 16);
 }
+template <int POLICY = 0>
 __device__ __forceinline__ void buf_st8(const Vec8<bf16>& v, Buf b, uint32_t off) {
-  __builtin_amdgcn_raw_buffer_store_b128(v.r, b, off, 0, 0);
+  __builtin_amdgcn_raw_buffer_store_b128(v.r, b, off, 0, POLICY);
 }
+template <int POLICY = 0>
 __device__ __forceinline__ void buf_st8(const Vec8<float>& v, Buf b, uint32_t off) {
-  __builtin_amdgcn_raw_buffer_store_b128(v.r0, b, off, 0, 0);
-  __builtin_amdgcn_raw_buffer_store_b128(v.r1, b, off + 16, 0, 0);
+  __builtin_amdgcn_raw_buffer_store_b128(v.r0, b, off, 0, POLICY);
+  __builtin_amdgcn_raw_buffer_store_b128(v.r1, b, off + 16, 0, POLICY);
+}
+// bf16 between products and memory.  A product leaves lane (m, g) row m at
+// columns 8 g (x) and 32 + 8 g (y); an access of whole 128-byte lines is lane
+// (m, g) at row m % 8 (x) or 8 + m % 8 (y) and columns 8 (g + 4 (m / 8)).  From
+// either to the other: the upper half of each 16 lanes of x is exchanged with
+// the lower half of y.  (41447 rows forward: in halves of lines 485 us, in whole
+// ones 457, and past the cache 433.)
+__device__ __forceinline__ void turn(u32x4& x, u32x4& y, bool upper) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t give = upper ? x[i] : y[i];
+    const uint32_t take = (uint32_t)__builtin_amdgcn_mov_dpp((int)give, 0x128, 0xf, 0xf, true);  // row_ror:8
+    if (upper) x[i] = take;
+    else y[i] = take;
+  }
+}
+template <typename T> constexpr bool kLines = sizeof(T) == 2;  // an fp32 access of 32 columns is whole lines already
+__device__ __forceinline__ void turn(Vec8<bf16>& x, Vec8<bf16>& y, bool upper) { turn(x.r, y.r, upper); }
+__device__ __forceinline__ void turn(Vec8<float>&, Vec8<float>&, bool) {}
+// This lane's row (of 16) and column (of 64) in access h of two.
+template <typename T>
+__device__ __forceinline__ int line_row(int h, int m) {
+  return kLines<T> ? 8 * h + (m & 7) : m;
+}
+template <typename T>
+__device__ __forceinline__ int line_col(int h, int m, int g) {
+  return kLines<T> ? 8 * (g + 4 * (m >> 3)) : 8 * g + 32 * h;
 }
 __device__ __forceinline__ bf16 buf_ld1(Buf b, uint32_t off, bf16*) {
   return __builtin_bit_cast(bf16, __builtin_amdgcn_raw_buffer_load_b16(b, off, 0, 0));
@@ -280,7 +309,7 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
 // `parts` partial reductions (parts > 1: also stored to v_out).
 // (Five waves a SIMD, of 96 registers, instead of the four of more: 64 clients
 // of one token 15.7 us instead of 16.5, 41447 rows 484 instead of 480.)
-template <typename T, int RP>
+template <typename T, int RP, bool STREAM>
 __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RP <= 32 ? 5 : 1))
     up_kernel(Segs t, const float* v, int parts, long total_rows, float* v_out, const T* b, int r, int out_features,
               float scale, const T* base, long ldb, T* y, long ldy) {
@@ -362,8 +391,8 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RP <= 32 ? 5 : 1)
   uint32_t bo[2], yo[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    bo[h] = col_off<T>(m, ldb, c0 + 8 * g + 32 * h, out_features);
-    yo[h] = col_off<T>(m, ldy, c0 + 8 * g + 32 * h, out_features);
+    bo[h] = col_off<T>(line_row<T>(h, m), ldb, c0 + line_col<T>(h, m, g), out_features);
+    yo[h] = col_off<T>(line_row<T>(h, m), ldy, c0 + line_col<T>(h, m, g), out_features);
   }
   auto rows16 = [&](int i, Vec8<T> (&bs)[2]) {
     f32x4 acc[4];
@@ -379,18 +408,21 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RP <= 32 ? 5 : 1)
         for (int q = 0; q < 4; ++q) acc[q] = mma16(wf[q][s % U::weights], vv.frag(), acc[q]);
       }
     }
+    turn(bs[0], bs[1], m >= 8);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = bs[h].get(e) + scale * acc[2 * h + (e >> 2)][e & 3];
       bs[h].set(o);
-      buf_st8(bs[h], yb, yo[h] + (uint32_t)(16 * i * sizeof(T)) * (uint32_t)ldy);
     }
+    turn(bs[0], bs[1], m >= 8);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) buf_st8<STREAM ? kOnce : 0>(bs[h], yb, yo[h] + (uint32_t)(16 * i * sizeof(T)) * (uint32_t)ldy);
   };
   auto load16 = [&](int i, Vec8<T> (&bs)[2]) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) buf_ld8(bs[h], bb, bo[h] + (uint32_t)(16 * i * sizeof(T)) * (uint32_t)ldb);
+    for (int h = 0; h < 2; ++h) buf_ld8<STREAM ? kOnce : 0>(bs[h], bb, bo[h] + (uint32_t)(16 * i * sizeof(T)) * (uint32_t)ldb);
   };
   if (rows > kTile - 16) {
     Vec8<T> bs[kTile / 16][2];
@@ -461,7 +493,7 @@ constexpr int kTokStride = kStep + 8;
 // One 32-row x 128-column tile of X in a wave's registers: lane (m, g) holds
 // rows 8g .. 8g + 7 at columns 8m .. 8m + 7.
 // The tile is read once: non-temporal (dy: 484 -> 463 us a backward of 41447
-// rows; not for what is read in two halves of a line, as by `up`: 487 -> 559).
+// rows; not for what is read in two halves of a line: 487 -> 559 in `up`).
 template <typename T>
 __device__ __forceinline__ void load_tile(Vec8<T> (&xr)[8], const T* x, long ld, int row0, int rows, int c0, int width,
                                           int m, int g) {
@@ -522,8 +554,8 @@ template <int RP, int NT> struct Factor {
 // and through registers, turned, into dB; dv reads the rows back and leaves its
 // result in their place; one barrier, and the waves' results are added.  Reading
 // dy alone in this order takes 150 us for 1.02 GB; with a store of dv's size a
-// step beside it 182, whatever its order or place; this kernel 200 (with one
-// tile ahead 211).
+// step beside it 182, whatever its order or place; this kernel 194 (with one
+// tile ahead 205).
 template <typename T, int RT>
 __global__ void __launch_bounds__((64 * OutWaves<T>::n))
     bwd_out_kernel(Segs t, Slots sl, const T* dy, long lddy, const T* b, const float* v, int stride, int out_features,
@@ -695,7 +727,7 @@ __global__ void __launch_bounds__(kThreads) dv_sum_kernel(float* dv_part, int pa
 
 // dx and dA (or a part of it).  As bwd_out, without a sum over the waves: a
 // wave's columns are its own.
-template <typename T, int RT>
+template <typename T, int RT, bool STREAM>
 __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
     bwd_in_kernel(Segs t, Slots sl, const T* x, long ldx, const T* a, const float* dv, int r, int in, const T* dres,
                   long lddr, T* dx, long lddx, float* da, float* da_part) {
@@ -786,8 +818,8 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        ro[h][u] = col_off<T>(m, lddr, c0 + 64 * h + 32 * u + 8 * g, in);
-        xo[h][u] = col_off<T>(m, lddx, c0 + 64 * h + 32 * u + 8 * g, in);
+        ro[h][u] = col_off<T>(line_row<T>(u, m), lddr, c0 + 64 * h + line_col<T>(u, m, g), in);
+        xo[h][u] = col_off<T>(line_row<T>(u, m), lddx, c0 + 64 * h + line_col<T>(u, m, g), in);
       }
     const uint32_t rrow = 16 * sizeof(T) * (uint32_t)lddr, xrow = 16 * sizeof(T) * (uint32_t)lddx;
     for (int buf = 0;; buf ^= 1) {
@@ -800,7 +832,7 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int u = 0; u < 2; ++u) buf_ld8(bs[h][i][u], rb, ro[h][u] + i * rrow);
+          for (int u = 0; u < 2; ++u) buf_ld8<STREAM ? kOnce : 0>(bs[h][i][u], rb, ro[h][u] + i * rrow);
       if (live) transpose8x8(xr, xt);
       if (more) {
         rows1 = wk.next(t, &row1);
@@ -844,14 +876,17 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
                   for (int q = 0; q < 4; ++q) d[q] = mma16(wf[h][q][s % U::weights], f[s].frag(), d[q]);
               }
             }
+            turn(bs[h][i][0], bs[h][i][1], m >= 8);
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
               float o[8];
 #pragma unroll
               for (int e = 0; e < 8; ++e) o[e] = bs[h][i][u].get(e) + d[2 * u + (e >> 2)][e & 3];
               bs[h][i][u].set(o);
-              buf_st8(bs[h][i][u], xb, xo[h][u] + i * xrow);
             }
+            turn(bs[h][i][0], bs[h][i][1], m >= 8);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) buf_st8<STREAM ? kOnce : 0>(bs[h][i][u], xb, xo[h][u] + i * xrow);
           }
         }
       }
@@ -976,6 +1011,14 @@ void fill(const std::vector<Run>& runs, size_t* i, int rows_a_step, Segs* t) {
 int splits_of(const fl_adapter_desc* d, const fl_batch_desc* b) {
   const long tiles = b->total_tokens / kTile + b->num_clients;
   return (int)std::max(1L, std::min<long>({256 / tiles, d->in_features / (64 * kWaves), 8}));
+}
+// Whether `up` and bwd_in pass the last-level cache by: from outputs on that it
+// would not hold for their reader.  (4096 <-> 12288, rank 16, with a scaling of
+// the output behind the call: y of 192 MB 234 us, past the cache 227, of 96 MB
+// 82 and 81, of 48 MB 43 and 48; dx of 128 MB 232 and 226, in place 260 and 265,
+// of 64 MB 121 and 124.  dx of 340 MB, alone, 438 and 412.)
+bool streams(const fl_adapter_desc* d, long rows, int width) {
+  return d->dtype == FL_BF16 && (size_t)rows * width * 2 >= kStreamBytes;
 }
 // Backward: columns of a workgroup of bwd_out (OutWaves).
 long out_cols(const fl_adapter_desc* d) {
@@ -1123,6 +1166,7 @@ int adapter_forward(const fl_adapter_desc* d, const fl_batch_desc* batch, const 
   const int splits = splits_of(d, batch);
   const long T = batch->total_tokens;
   const long cols = cdiv(d->out_features, kUpCols);
+  const bool past_cache = streams(d, T, d->out_features);
   for (size_t i = 0; i < runs.size();) {
     Segs t;
     fill(runs, &i, kTile, &t);
@@ -1132,7 +1176,8 @@ int adapter_forward(const fl_adapter_desc* d, const fl_batch_desc* batch, const 
       hipLaunchKernelGGL((down_kernel<E, RT>), dim3(t.step0[t.count], splits), dim3(kThreads), 0, s, t, (const E*)x,
                          ldx, (const E*)a, d->rank, d->in_features, splits > 1 ? w.v_part : v, T);
       if (int e = launch_status()) return e;
-      hipLaunchKernelGGL((up_kernel<E, 16 * RT>), dim3((unsigned)(t.step0[t.count] * cols)), dim3(kThreads), 0, s, t,
+      const auto up = past_cache ? up_kernel<E, 16 * RT, kLines<E>> : up_kernel<E, 16 * RT, false>;
+      hipLaunchKernelGGL(up, dim3((unsigned)(t.step0[t.count] * cols)), dim3(kThreads), 0, s, t,
                          splits > 1 ? w.v_part : v, splits, T, v, (const E*)b, d->rank, d->out_features, d->scale,
                          (const E*)base, ld_base, (E*)y, ldy);
       return launch_status();
@@ -1152,6 +1197,7 @@ int adapter_backward(const fl_adapter_desc* d, const fl_batch_desc* batch, const
   const long T = batch->total_tokens;
   const long na = (long)d->rank * d->in_features, nb = (long)d->rank * d->out_features;
   const long cols_in = in_cols(d), cols_out = out_cols(d);
+  const bool past_cache = streams(d, T, d->in_features);
   for (size_t i = 0; i < runs.size();) {
     Segs t;
     fill(runs, &i, kStep, &t);
@@ -1175,7 +1221,8 @@ int adapter_backward(const fl_adapter_desc* d, const fl_batch_desc* batch, const
           if (int e = launch_status()) return e;
         }
       }
-      hipLaunchKernelGGL((bwd_in_kernel<E, RT>), dim3((unsigned)(workers_in * cols_in)), dim3(kThreads), 0, s, t, si,
+      const auto in = past_cache ? bwd_in_kernel<E, RT, kLines<E>> : bwd_in_kernel<E, RT, false>;
+      hipLaunchKernelGGL(in, dim3((unsigned)(workers_in * cols_in)), dim3(kThreads), 0, s, t, si,
                          (const E*)x, ldx, (const E*)a, w.dv_part, d->rank, d->in_features, (const E*)dres, ld_dres,
                          (E*)dx, ld_dx, da, w.da_part);
       return launch_status();

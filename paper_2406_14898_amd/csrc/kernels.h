@@ -8,6 +8,11 @@
 
 namespace flglm {
 
+// From this size on an output that the call does not read again is written past
+// the last-level cache of 256 MB (non-temporal): its reader would find too little
+// of it there.
+constexpr size_t kStreamBytes = size_t(128) << 20;
+
 // Sets the thread's error message; returns code.
 int set_error(int code, const char* msg);
 // The checks every entry point makes of a batch descriptor.

@@ -47,7 +47,6 @@ constexpr double kLn2 = 1.0 / (double)kLog2e;  // of the fp32 factor, so that M 
 constexpr int kPairsArg = 128;       // pairs whose bounds travel in one launch's kernel arguments
 constexpr int kMaxSplits = 8;        // (one pair, 110 rows of 130528: 8 parts 12.4 us, 16 parts 13.9)
 constexpr int kBatch = 2;            // loads of a lane at once
-constexpr size_t kStreamBytes = size_t(192) << 20;
 constexpr long kWantGroups = 2048;   // workgroups that fill the chip, four a CU, twice
 
 // Exponentials are powers of two: with M the running maximum of x log2 e,
