@@ -17,8 +17,8 @@
 //
 // Measured on one MI355X, bf16, clients of one slot each (a plain copy of
 // 1 GiB moves 5.0 TB/s here, reads alone 6.2):
-//   forward, 41447 rows, 4096 -> 12288, rank 16, 32 clients: 2.35 GB in 433 us
-//     (down 82 us, 4.1 TB/s of reads; up 355 us, 5.8 TB/s)
+//   forward, 41447 rows, 4096 -> 12288, rank 16, 32 clients: 2.35 GB in 418 us
+//     (down 70 us, 4.9 TB/s of reads; up 350 us, 5.8 TB/s)
 //   backward, the same and dres: 2.05 GB in 412 us (out 194, dv_sum 6, in 190,
 //     join 13, the gradients' clearing)
 //   64 clients of one token, 4096 -> 12288, rank 16: 34 MB in 15.7 us
@@ -127,8 +127,8 @@ __device__ __forceinline__ void buf_st8(const Vec8<float>& v, Buf b, uint32_t of
 // columns 8 g (x) and 32 + 8 g (y); an access of whole 128-byte lines is lane
 // (m, g) at row m % 8 (x) or 8 + m % 8 (y) and columns 8 (g + 4 (m / 8)).  From
 // either to the other: the upper half of each 16 lanes of x is exchanged with
-// the lower half of y.  (41447 rows forward: in halves of lines 485 us, in whole
-// ones 457, and past the cache 433.)
+// the lower half of y.  (41447 rows forward, base and y: in halves of lines
+// 485 us, in whole ones 457, and past the cache 433.)
 __device__ __forceinline__ void turn(u32x4& x, u32x4& y, bool upper) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -198,7 +198,7 @@ __device__ __forceinline__ int up_col(int q, int mm) { return 32 * (q >> 1) + 8 
 // ---------------------------------------------------------------------------
 
 // v (or a part of its reduction, part[split][T][r]) of one 64-row tile.
-template <typename T, int RT>
+template <typename T, int RT, bool STREAM>
 __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long ldx, const T* a, int r, int in,
                                                         float* v, long total_rows) {
   constexpr int RP = 16 * RT;
@@ -220,9 +220,9 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
   for (int i = 0; i < NI; ++i)
 #pragma unroll
     for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // 64-column steps, dealt to the splits and then to the waves in turn; a lane
-  // takes columns 16 g .. 16 g + 15 of a step (a wave whole 128-byte lines), as
-  // two products of 32 slots
+  // 64-column steps, dealt to the splits and then to the waves in turn: two
+  // products over 32 columns each, x loaded in whole lines (41447 rows forward:
+  // 424 us instead of 433)
   const int nk = (in + 63) / 64, stride = gridDim.y * kWaves;
   const uint32_t xrow = (uint32_t)ldx * 16 * sizeof(T), arow = (uint32_t)in * 16 * sizeof(T);
   struct Step {
@@ -231,15 +231,17 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
   auto load = [&](Step& s, int k) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int c = 64 * k + 16 * g + 8 * h;
-      const uint32_t xo = col_off<T>(m, ldx, c, in), ao = col_off<T>(m, in, c, in);
+      const uint32_t xo = col_off<T>(line_row<T>(h, m), ldx, 64 * k + line_col<T>(h, m, g), in),
+                     ao = col_off<T>(m, in, 64 * k + 8 * g + 32 * h, in);
 #pragma unroll
-      for (int i = 0; i < NI; ++i) buf_ld8(s.xv[h][i], xb, xo + i * xrow);
+      for (int i = 0; i < NI; ++i) buf_ld8<STREAM ? kOnce : 0>(s.xv[h][i], xb, xo + i * xrow);
 #pragma unroll
       for (int j = 0; j < RT; ++j) buf_ld8(s.av[h][j], ab, ao + j * arow);
     }
   };
   auto multiply = [&](Step& s) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) turn(s.xv[0][i], s.xv[1][i], m >= 8);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -1012,11 +1014,12 @@ int splits_of(const fl_adapter_desc* d, const fl_batch_desc* b) {
   const long tiles = b->total_tokens / kTile + b->num_clients;
   return (int)std::max(1L, std::min<long>({256 / tiles, d->in_features / (64 * kWaves), 8}));
 }
-// Whether `up` and bwd_in pass the last-level cache by: from outputs on that it
-// would not hold for their reader.  (4096 <-> 12288, rank 16, with a scaling of
+// Whether operands of this width pass the last-level cache by: from a size on
+// that it would not hold for an output's reader, or for the backward.  (4096 <-> 12288, rank 16, with a scaling of
 // the output behind the call: y of 192 MB 234 us, past the cache 227, of 96 MB
 // 82 and 81, of 48 MB 43 and 48; dx of 128 MB 232 and 226, in place 260 and 265,
-// of 64 MB 121 and 124.  dx of 340 MB, alone, 438 and 412.)
+// of 64 MB 121 and 124.  dx of 340 MB, alone, 438 and 412; x of 340 MB, the
+// forward alone, 424 and 418.)
 bool streams(const fl_adapter_desc* d, long rows, int width) {
   return d->dtype == FL_BF16 && (size_t)rows * width * 2 >= kStreamBytes;
 }
@@ -1173,7 +1176,8 @@ int adapter_forward(const fl_adapter_desc* d, const fl_batch_desc* batch, const 
     const int rc = dispatch(d, [&](auto* type, auto rt) {
       using E = std::remove_pointer_t<decltype(type)>;
       constexpr int RT = decltype(rt)::value;
-      hipLaunchKernelGGL((down_kernel<E, RT>), dim3(t.step0[t.count], splits), dim3(kThreads), 0, s, t, (const E*)x,
+      const auto down = streams(d, T, d->in_features) ? down_kernel<E, RT, kLines<E>> : down_kernel<E, RT, false>;
+      hipLaunchKernelGGL(down, dim3(t.step0[t.count], splits), dim3(kThreads), 0, s, t, (const E*)x,
                          ldx, (const E*)a, d->rank, d->in_features, splits > 1 ? w.v_part : v, T);
       if (int e = launch_status()) return e;
       const auto up = past_cache ? up_kernel<E, 16 * RT, kLines<E>> : up_kernel<E, 16 * RT, false>;
