@@ -31,6 +31,10 @@ constexpr int kTensors = 128;                 // tensors a launch (2.6 KB of ker
 constexpr int kStep = 8 * kThreads;           // elements a workgroup takes at a time
 constexpr int64_t kMaxTensors = 1 << 20;
 constexpr int64_t kMaxElements = int64_t(1) << 40;
+// Bytes from which clipping passes the last-level cache by (1.6 GB into other
+// tensors 779 us instead of 834 and 1 GB in place 575 either way, but in place
+// 600 MB 366 instead of 360, 300 MB 176 instead of 151).
+constexpr size_t kPastCache = size_t(1) << 30;
 constexpr double kEps = 1e-6;                 // keeps the quotient finite for a zero norm
 
 struct Table {
@@ -72,41 +76,51 @@ __device__ __forceinline__ double block_sum(double v) {
   return t;
 }
 
-// Eight elements a lane and step, kBatch steps' loads in flight at once (0.4 G
-// fp32: one 305 us, four 262 us, 6.1 TB/s).
+// 16 bytes a lane and access, so that an access of a wave is whole lines, and
+// 2048 elements a step: fp32 two accesses, bf16 one.  (Eight fp32 elements a lane
+// in two halves of lines: norm and clipping of 52 tensors, 6.8 M elements, 19.7
+// us instead of 18.5; 0.4 G 817 instead of 779.)
+template <typename T>
+struct Access {
+  using V = std::conditional_t<sizeof(T) == 2, Vec8<T>, Vec4<T>>;
+  static constexpr int n = 16 / sizeof(T), step = kStep / (n * kThreads);
+  // First element of the thread's access u behind element b.
+  __device__ static __forceinline__ int64_t at(int64_t b, int u) { return b + (u * kThreads + (int)threadIdx.x) * n; }
+};
+
+// Sums of squares, one partial a workgroup, kBatch steps' loads in flight at once
+// (0.4 G fp32: one 305 us, four 262 us, 6.1 TB/s; bound by the reads).
 constexpr int kBatch = 4;
 
-// Sums of squares, one partial a workgroup; bound by the reads.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) square_kernel(NormTable t, int chunk, double* part) {
+  using A = Access<T>;
   const int k = find(t, blockIdx.x);
   const T* g = (const T*)t.g[k];
   const int64_t n = t.size[k];
   const int64_t b0 = (int64_t)(blockIdx.x - t.first[k]) * chunk;
   const int64_t b1 = min(n, b0 + chunk);
   double acc[4] = {0, 0, 0, 0};
-  int64_t e = b0 + threadIdx.x * 8;
-  for (; e + (kBatch - 1) * kStep + 8 <= b1; e += kBatch * kStep) {
-    Vec8<T> v[kBatch];
+  auto add = [&](const typename A::V& v) {
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) v[u].load(g + e + u * kStep);
+    for (int i = 0; i < A::n; ++i) {
+      const double x = v.get(i);
+      acc[i & 3] = fma(x, x, acc[i & 3]);
+    }
+  };
+  int64_t b = b0;
+  for (; b + kBatch * kStep <= b1; b += kBatch * kStep) {
+    typename A::V v[kBatch * A::step];
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u)
+    for (int u = 0; u < kBatch * A::step; ++u) v[u].load(g + A::at(b, u));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const double x = v[u].get(i);
-        acc[i & 3] = fma(x, x, acc[i & 3]);
-      }
+    for (int u = 0; u < kBatch * A::step; ++u) add(v[u]);
   }
-  for (; e < b1; e += kStep) {
-    if (e + 8 <= b1) {
-      Vec8<T> v;
+  for (int64_t e = A::at(b, 0); e < b1; e += A::n * kThreads) {
+    if (e + A::n <= b1) {
+      typename A::V v;
       v.load(g + e);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const double x = v.get(i);
-        acc[i & 3] = fma(x, x, acc[i & 3]);
-      }
+      add(v);
     } else {
       for (int64_t j = e; j < b1; ++j) {
         const double x = to_f32(g[j]);
@@ -137,14 +151,15 @@ __global__ void __launch_bounds__(kFinish) finish_kernel(const double* part, int
   }
 }
 
-// Eight elements a lane and done: the chip then sweeps through memory in order,
+// A step a workgroup and done: the chip then sweeps through memory in order,
 // which reads and writes faster than as many workgroups each in a stretch of
-// its own (0.4 G fp32: 540 us, 6.0 TB/s; 128 K elements a workgroup 640, with
-// non-temporal stores 690).  From the last element to the first: what the norm
-// read last is in the last-level cache (norm and clipping of 300 MB 153 us,
-// of 400 MB 243; from the first on 180 and 260; past 1 GB within 1 %).
-template <typename T>
+// its own (0.4 G fp32 in place: 128 K elements a workgroup 640 us, so 540).  From the last
+// element to the first: what the norm read last is in the last-level cache (norm
+// and clipping of 300 MB in place 151 us, of 400 MB 240; from the first on 180
+// and 260; past 1 GB within 1 %).  STREAM: past that cache.
+template <typename T, bool STREAM>
 __global__ void __launch_bounds__(kThreads) scale_kernel(Table t, const float* norm_coef) {
+  using A = Access<T>;
   const float c = norm_coef[1];
   const int block = gridDim.x - 1 - blockIdx.x;
   const int k = find(t, block);
@@ -152,17 +167,37 @@ __global__ void __launch_bounds__(kThreads) scale_kernel(Table t, const float* n
   T* out = (T*)t.out[k];
   if (c == 1.f && g == out) return;
   const int64_t n = t.size[k];
-  const int64_t e = (int64_t)(block - t.first[k]) * kStep + threadIdx.x * 8;
-  if (e + 8 <= n) {
-    Vec8<T> v;
-    v.load(g + e);
-    float x[8];
+  const int64_t b = (int64_t)(block - t.first[k]) * kStep;
+  auto scaled = [&](typename A::V& v) {
+    float x[A::n];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = v.get(i) * c;
+    for (int i = 0; i < A::n; ++i) x[i] = v.get(i) * c;
     v.set(x);
-    v.store(out + e);
-  } else {
-    for (int64_t j = e; j < n; ++j) out[j] = from_f32<T>(to_f32(g[j]) * c);
+  };
+  if (b + kStep <= n) {
+    typename A::V v[A::step];
+#pragma unroll
+    for (int u = 0; u < A::step; ++u) {
+      if constexpr (STREAM) v[u].r = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(g + A::at(b, u)));
+      else v[u].load(g + A::at(b, u));
+    }
+#pragma unroll
+    for (int u = 0; u < A::step; ++u) {
+      scaled(v[u]);
+      if constexpr (STREAM) __builtin_nontemporal_store(v[u].r, reinterpret_cast<u32x4*>(out + A::at(b, u)));
+      else v[u].store(out + A::at(b, u));
+    }
+    return;
+  }
+  for (int64_t e = A::at(b, 0); e < n; e += A::n * kThreads) {
+    if (e + A::n <= n) {
+      typename A::V v;
+      v.load(g + e);
+      scaled(v);
+      v.store(out + e);
+    } else {
+      for (int64_t j = e; j < n; ++j) out[j] = from_f32<T>(to_f32(g[j]) * c);
+    }
   }
 }
 
@@ -178,7 +213,7 @@ int launch_status() {
 
 // Elements of a chunk: enough chunks to fill the chip, few enough that the
 // partials stay small, and a whole batch of loads at least (norm and clipping of
-// 52 tensors, 6.8 M fp32 elements: 19.7 us; one step a chunk 21.2).
+// 52 tensors, 6.8 M fp32 elements: 18.5 us; one step a chunk 20).
 int chunk_of(int64_t total) {
   const int64_t want = (total / 4096 + kStep - 1) / kStep * kStep;
   return (int)std::min<int64_t>(std::max<int64_t>(want, kBatch * kStep), 64 * kStep);
@@ -306,6 +341,7 @@ int fl_clip_grads(int32_t dtype, int32_t num_tensors, const void* const* grads, 
   }
   if (int rc = check_outputs(num_tensors, grads, out, sizes, E)) return rc;
   hipStream_t s = (hipStream_t)stream;
+  const bool past_cache = (size_t)total * E >= kPastCache;
   for (int i = 0; i < num_tensors;) {
     Table t;
     t.count = 0;
@@ -321,10 +357,9 @@ int fl_clip_grads(int32_t dtype, int32_t num_tensors, const void* const* grads, 
       blocks += nb;
     }
     if (!t.count) continue;
-    if (dtype == FL_BF16)
-      hipLaunchKernelGGL(scale_kernel<bf16>, dim3((unsigned)blocks), dim3(kThreads), 0, s, t, norm_coef);
-    else
-      hipLaunchKernelGGL(scale_kernel<float>, dim3((unsigned)blocks), dim3(kThreads), 0, s, t, norm_coef);
+    const auto bf = past_cache ? scale_kernel<bf16, true> : scale_kernel<bf16, false>;
+    const auto f32 = past_cache ? scale_kernel<float, true> : scale_kernel<float, false>;
+    hipLaunchKernelGGL(dtype == FL_BF16 ? bf : f32, dim3((unsigned)blocks), dim3(kThreads), 0, s, t, norm_coef);
     if (int rc = launch_status()) return rc;
   }
   return FL_OK;

@@ -154,3 +154,19 @@ def test_outputs_unlike_the_gradients_are_refused():
     assert all((g == 1).all() for g in grads) and all((o == 0).all() for o in good)
     op.clip(1.0, out=good)
     assert all((g == 1).all() for g in grads) and all(abs(float(o.max()) - 72 ** -0.5) < 1e-5 for o in good)
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_more_bytes_than_the_cache_holds(dt):
+    """Past 1 GB, ragged sizes, into other tensors: each element the product
+    rounded once."""
+    unit = 4 // dt.itemsize << 20
+    sizes = [200 * unit + 3, 1, 61 * unit - 2047, 2049, 8 * unit]
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    grads = [torch.randn(n, generator=gen, device="cuda", dtype=torch.float32).to(dt) for n in sizes]
+    out = [torch.full_like(g, 7.0) for g in grads]
+    op = GradNorm(grads)
+    op.clip(2.0, out=out)
+    coef = op.result[1]
+    for g, o in zip(grads, out):
+        assert torch.equal(o, (g.float() * coef).to(dt))
