@@ -401,7 +401,8 @@ int fl_adapter_backward(const fl_adapter_desc* desc, const fl_batch_desc* batch,
 /* The server stack with adapters on every block's fused query / key / value
  * projection (in = H, out = 3H; rotary follows, as for the projection
  * itself).  The block weights may be trained or frozen, the P-tuning prefix
- * present or not, as without adapters. */
+ * present or not, as without adapters.  Launch timing does not include the
+ * adapters' kernels. */
 typedef struct fl_layer_adapters {
   const void *a, *b; /* device [n, r, H] and [n, 3H, r], handle dtype */
 } fl_layer_adapters;
