@@ -420,11 +420,13 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RP <= 32 ? 5 : 1)
     }
     turn(bs[0], bs[1], m >= 8);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) buf_st8<STREAM ? kOnce : 0>(bs[h], yb, yo[h] + (uint32_t)(16 * i * sizeof(T)) * (uint32_t)ldy);
+    for (int h = 0; h < 2; ++h)
+      buf_st8<STREAM ? kOnce : 0>(bs[h], yb, yo[h] + (uint32_t)(16 * i * sizeof(T)) * (uint32_t)ldy);
   };
   auto load16 = [&](int i, Vec8<T> (&bs)[2]) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) buf_ld8<STREAM ? kOnce : 0>(bs[h], bb, bo[h] + (uint32_t)(16 * i * sizeof(T)) * (uint32_t)ldb);
+    for (int h = 0; h < 2; ++h)
+      buf_ld8<STREAM ? kOnce : 0>(bs[h], bb, bo[h] + (uint32_t)(16 * i * sizeof(T)) * (uint32_t)ldb);
   };
   if (rows > kTile - 16) {
     Vec8<T> bs[kTile / 16][2];

@@ -285,11 +285,13 @@ int fl_grad_norm(int32_t dtype, int32_t num_tensors, const void* const* grads, c
   if (int rc = check_sizes(num_tensors, sizes, &total, &chunks)) return rc;
   if (!grads || !norm_coef || !workspace) return set_error(FL_ERR_NULL, "grads / norm_coef / workspace is NULL");
   if (!(max_norm >= 0.0)) return set_error(FL_ERR_ARG, "max_norm must be >= 0 (infinity: never clip)");
-  if (!al16(workspace) || ((uintptr_t)norm_coef & 7)) return set_error(FL_ERR_ALIGN, "workspace / norm_coef misaligned");
+  if (!al16(workspace) || ((uintptr_t)norm_coef & 7))
+    return set_error(FL_ERR_ALIGN, "workspace / norm_coef misaligned");
   if (workspace_bytes < (size_t)std::max<int64_t>(chunks, 1) * sizeof(double))
     return set_error(FL_ERR_WORKSPACE, "workspace too small");
   const size_t E = dtype == FL_BF16 ? 2 : 4;
-  if (overlap(norm_coef, 8, workspace, workspace_bytes)) return set_error(FL_ERR_ALIAS, "norm_coef overlaps the workspace");
+  if (overlap(norm_coef, 8, workspace, workspace_bytes))
+    return set_error(FL_ERR_ALIAS, "norm_coef overlaps the workspace");
   for (int i = 0; i < num_tensors; ++i) {
     if (sizes[i] == 0) continue;
     if (!grads[i]) return set_error(FL_ERR_NULL, "a gradient is NULL");
@@ -321,7 +323,8 @@ int fl_grad_norm(int32_t dtype, int32_t num_tensors, const void* const* grads, c
     if (int rc = launch_status()) return rc;
     part += blocks;
   }
-  hipLaunchKernelGGL(finish_kernel, dim3(1), dim3(kFinish), 0, s, (const double*)workspace, chunks, max_norm, norm_coef);
+  hipLaunchKernelGGL(finish_kernel, dim3(1), dim3(kFinish), 0, s, (const double*)workspace, chunks, max_norm,
+                     norm_coef);
   return launch_status();
 }
 
@@ -336,7 +339,8 @@ int fl_clip_grads(int32_t dtype, int32_t num_tensors, const void* const* grads, 
   for (int i = 0; i < num_tensors; ++i) {
     if (sizes[i] == 0) continue;
     if (!grads[i] || !out[i]) return set_error(FL_ERR_NULL, "a gradient or output is NULL");
-    if (!al16(grads[i]) || !al16(out[i])) return set_error(FL_ERR_ALIGN, "gradients and outputs must be 16-byte aligned");
+    if (!al16(grads[i]) || !al16(out[i]))
+      return set_error(FL_ERR_ALIGN, "gradients and outputs must be 16-byte aligned");
     if (overlap(out[i], sizes[i] * E, norm_coef, 8)) return set_error(FL_ERR_ALIAS, "an output overlaps norm_coef");
   }
   if (int rc = check_outputs(num_tensors, grads, out, sizes, E)) return rc;

@@ -374,7 +374,8 @@ int check_pairs(const fl_batch_desc* b) {
 int check_ws(const fl_preference_desc* d, const fl_batch_desc* b, void* ws, size_t bytes) {
   if (!ws) return set_error(FL_ERR_NULL, "workspace is NULL");
   if (!al16(ws)) return set_error(FL_ERR_ALIGN, "workspace is not 16-byte aligned");
-  if (bytes < carve(b->total_tokens, d->vocab, nullptr).total) return set_error(FL_ERR_WORKSPACE, "workspace too small");
+  if (bytes < carve(b->total_tokens, d->vocab, nullptr).total)
+    return set_error(FL_ERR_WORKSPACE, "workspace too small");
   return FL_OK;
 }
 int check_logits(const fl_preference_desc* d, const void* logits, int64_t ld, const int32_t* labels) {

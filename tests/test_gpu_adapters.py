@@ -215,6 +215,49 @@ def test_long_clients_wide():
     _run([[1100], [257], [33]], [1, 0, 1], 2, 32, 4096, 4096, "bf16", seed=6)
 
 
+@pytest.mark.parametrize("r", [16, 24, 64])
+def test_batches_larger_than_the_cache(r):
+    """Two clients at once, 139 MB a matrix, and each alone: y, v and dx of the same
+    bits; dA and dB apart by their sums over the rows."""
+    lens, inn, n = [8600, 8400], 4096, 2
+    both, rows = _batch([[k] for k in lens])
+    d = _inputs(17000, n, r, inn, inn, "bf16", 21)
+    op = ClientAdapters(n, r, inn, inn, "bf16", 0.5)
+
+    def run(batch, slots, t):
+        T = batch.total_tokens
+        ws, y, v = op.workspace(batch), torch.empty_like(d["base"][t]), torch.empty((T, r), device="cuda")
+        op.forward(batch, slots, d["x"][t], d["a"], d["b"], d["base"][t], y, v, ws)
+        da, db = torch.zeros((n, r, inn), device="cuda"), torch.zeros((n, inn, r), device="cuda")
+        dx = torch.empty_like(d["dres"][t])
+        op.backward(batch, slots, d["dy"][t], d["x"][t], d["a"], d["b"], v, d["dres"][t], dx, da, db, ws)
+        return y, v, dx, da, db
+
+    got = run(both, [1, 0], slice(0, 17000))
+    for c, k in ((0, 1), (1, 0)):
+        t, T = slice(rows[c], rows[c + 1]), lens[c]
+        one = run(_batch([[T]])[0], [k], t)
+        for p, q in zip(got[:3], one[:3]):
+            assert torch.equal(p[t], q)
+        x, dy, v = d["x"][t].double(), d["dy"][t].double(), got[1][t].double()
+        dv = 0.5 * dy @ d["b"][k].double()
+        # two sums of T products, each as in the module's bounds
+        for p, q, size in ((got[3][k], one[3][k], dv.abs().t() @ x.abs()),
+                           (got[4][k], one[4][k], 0.5 * dy.abs().t() @ v.abs())):
+            assert ((p.double() - q.double()).abs() <= 2 * (3 * T + 64) * u * size).all()
+    # and against the formula, on a sample of rows
+    t = torch.arange(0, 17000, 331, device="cuda")
+    k = (t < 8600).long()
+    x, dy = d["x"][t].double(), d["dy"][t].double()
+    v = torch.stack([d["a"][j].double() @ x[i] for i, j in enumerate(k)])
+    y = d["base"][t].double() + 0.5 * torch.stack([d["b"][j].double() @ v[i] for i, j in enumerate(k)])
+    dv = 0.5 * torch.stack([d["b"][j].double().t() @ dy[i] for i, j in enumerate(k)])
+    dx = d["dres"][t].double() + torch.stack([d["a"][j].double().t() @ dv[i] for i, j in enumerate(k)])
+    for p, q, e in ((got[0][t], y, y.abs() + 1), (got[2][t], dx, dx.abs() + 1)):
+        # half a step of bf16, and fp32 sums of 4096 terms below it
+        assert ((p.double() - q).abs() <= 2.0 ** -8 * q.abs() + 2.0 ** -12 * e).all()
+
+
 def test_infinities_and_nan_stay_in_their_rows():
     """A row with an infinity or NaN spoils its own outputs and no other row's,
     a client's without an adapter none."""
