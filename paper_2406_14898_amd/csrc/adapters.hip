@@ -343,16 +343,7 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RP <= 32 ? 5 : 1)
       buf_ld8(f, wb, col_off<T>(up_col(q, m), r, U::rank(s, g), r));
       wf[q][s] = f.frag();
     }
-  if (slot >= 0 && parts == 1) {
-    // (through the code for parts, below, 41447 rows take 497 us instead of 487)
-    for (int i = threadIdx.x; i < (rows + 15) / 16 * 16 * RP; i += kThreads) {
-      const int row = i / RP, c = i - row * RP;
-      float s = 0.f;
-      if (row < rows && c < r) s = v[(row0 + row) * r + c];
-#pragma unroll
-      for (int q = 0; q < U::parts; ++q) sh[row][q * RP + c] = split(s, (T*)nullptr);
-    }
-  } else if (slot >= 0) {
+  if (slot >= 0) {
     // a thread's rank, and one row in kRows; 16 rows at least are staged
     constexpr int kRows = kThreads / RP, kMany = kTile / kRows;
     const int rank = threadIdx.x % RP, row = threadIdx.x / RP;
@@ -375,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RP <= 32 ? 5 : 1)
 #pragma unroll
           for (int i = 0; i < n; ++i) f[i] += part[q][i];
       }
-      const Buf ob = rows_of(cb == 0 ? v_out : nullptr, row0, r, rows, r);
+      const Buf ob = rows_of(parts > 1 && cb == 0 ? v_out : nullptr, row0, r, rows, r);
 #pragma unroll
       for (int i = 0; i < n; ++i) {
         __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(f[i]), ob, col_off<float>(row + i * kRows, r, rank, r), 0,
