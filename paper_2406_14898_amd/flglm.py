@@ -515,10 +515,13 @@ def fl_adapter_workspace_bytes(desc: fl_adapter_desc, batch: BatchDesc) -> int:
 
 
 def _client_adapter(client_adapter, batch: BatchDesc):
-    arr, p = _host_i32(client_adapter)
-    if arr.shape != (batch.desc.num_clients,):
-        raise FlglmError(FL_ERR_ARG, f"{arr.size} adapter slots for {batch.desc.num_clients} clients")
-    return arr, p
+    n = batch.desc.num_clients
+    arr = np.ascontiguousarray(client_adapter, dtype=np.int32)
+    if arr.shape != (n,):
+        raise FlglmError(FL_ERR_ARG, f"{arr.size} adapter slots for {n} clients")
+    if not arr.flags.writeable:
+        arr = arr.copy()
+    return arr, (ctypes.c_int32 * n).from_buffer(arr)  # (a third of the time of arr.ctypes.data_as)
 
 
 def fl_adapter_forward(desc: fl_adapter_desc, batch: BatchDesc, client_adapter, x, ldx: int, a, b, base, ld_base: int, y,
