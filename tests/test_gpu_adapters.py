@@ -11,7 +11,7 @@ import pytest
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
-from paper_2406_14898_amd import BatchDesc, ClientAdapters  # noqa: E402
+from paper_2406_14898_amd import BatchDesc, ClientAdapters, FlglmError  # noqa: E402
 
 u = 2.0 ** -23
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
@@ -308,6 +308,24 @@ def test_nan_in_a_gradient_stays_with_its_slot(r, dt):
     keep[64] = False
     assert torch.equal(dx[keep], dx2[keep]) and torch.isnan(dx2[64].float()).all()
     assert not torch.isfinite(da2[0]).all() and not torch.isfinite(db2[0]).all()
+
+
+def test_slots_of_any_sequence():
+    """A list, a tuple, and arrays that are read-only, strided or of 64 bits."""
+    batch, rows = _batch([[5], [3], [4]])
+    d = _inputs(12, 3, 8, 64, 96, "bf16", 2)
+    op = ClientAdapters(3, 8, 64, 96, "bf16", 1.0)
+    ws, outs = op.workspace(batch), []
+    fixed = np.array([2, -1, 0], np.int32)
+    fixed.setflags(write=False)
+    for slots in ([2, -1, 0], (2, -1, 0), fixed, np.array([2, 9, -1, 9, 0, 9], np.int32)[::2], np.array([2, -1, 0])):
+        y, v = torch.empty((12, 96), dtype=torch.bfloat16, device="cuda"), torch.empty((12, 8), device="cuda")
+        op.forward(batch, slots, d["x"], d["a"], d["b"], d["base"], y, v, ws)
+        outs.append((y, v))
+    assert all(torch.equal(p, q) for o in outs[1:] for p, q in zip(outs[0], o))
+    for slots in ([2, -1], [2, -1, 3], [2, -2, 0], [[2, -1, 0]], [2, -1, 2 ** 32]):
+        with pytest.raises((FlglmError, OverflowError)):
+            op.forward(batch, slots, d["x"], d["a"], d["b"], d["base"], y, v, ws)
 
 
 def test_results_repeat_bit_for_bit():
