@@ -309,7 +309,7 @@ int fl_grad_norm(int32_t dtype, int32_t num_tensors, const void* const* grads, c
     for (; i < num_tensors && t.count < kTensors; ++i) {
       const int64_t nb = (sizes[i] + chunk - 1) / chunk;
       if (nb == 0) continue;
-      if (t.count && blocks + nb > (1 << 30)) break;
+      if (t.count && blocks + nb > kMaxGroups) break;  // (one tensor has 2^23 chunks at most)
       t.g[t.count] = grads[i];
       t.size[t.count] = sizes[i];
       t.first[t.count++] = (int32_t)blocks;
@@ -346,19 +346,24 @@ int fl_clip_grads(int32_t dtype, int32_t num_tensors, const void* const* grads, 
   if (int rc = check_outputs(num_tensors, grads, out, sizes, E)) return rc;
   hipStream_t s = (hipStream_t)stream;
   const bool past_cache = (size_t)total * E >= kPastCache;
+  int64_t done = 0;  // elements of tensor i in the launches before
   for (int i = 0; i < num_tensors;) {
     Table t;
     t.count = 0;
     int64_t blocks = 0;
-    for (; i < num_tensors && t.count < kTensors; ++i) {
-      const int64_t nb = (sizes[i] + kStep - 1) / kStep;
-      if (nb == 0) continue;
-      if (t.count && blocks + nb > (1 << 30)) break;
-      t.g[t.count] = grads[i];
-      t.out[t.count] = out[i];
-      t.size[t.count] = sizes[i];
-      t.first[t.count++] = (int32_t)blocks;
-      blocks += nb;
+    while (i < num_tensors && t.count < kTensors && blocks < kMaxGroups) {
+      const int64_t n = std::min(sizes[i] - done, (kMaxGroups - blocks) * kStep);  // what still fits this launch
+      if (n > 0) {
+        t.g[t.count] = (const char*)grads[i] + done * E;
+        t.out[t.count] = (char*)out[i] + done * E;
+        t.size[t.count] = n;
+        t.first[t.count++] = (int32_t)blocks;
+        blocks += (n + kStep - 1) / kStep;
+        done += n;
+      }
+      if (done < sizes[i]) break;  // the launch is full
+      done = 0;
+      ++i;
     }
     if (!t.count) continue;
     const auto bf = past_cache ? scale_kernel<bf16, true> : scale_kernel<bf16, false>;

@@ -13,6 +13,9 @@ namespace flglm {
 // of it there.
 constexpr size_t kStreamBytes = size_t(128) << 20;
 
+// Workgroups (of 256) a launch: one takes fewer than 2^32 threads.
+constexpr long kMaxGroups = 1L << 23;
+
 // Sets the thread's error message; returns code.
 int set_error(int code, const char* msg);
 // The checks every entry point makes of a batch descriptor.

@@ -392,9 +392,12 @@ int forward(const fl_preference_desc* d, const fl_batch_desc* b, const T* logits
   const long tokens = b->total_tokens;
   const int V = (int)d->vocab, splits = splits_of(tokens, V);
   const int cols = (int)(((V + splits - 1) / splits + 7) / 8 * 8);
-  hipLaunchKernelGGL(pref_row_kernel<T>, dim3((unsigned)tokens, splits), dim3(kThreads), 0, s, logits, ld, V, cols,
-                     labels, w.part, w.done);
-  if (int rc = launch_status()) return rc;
+  for (long t0 = 0; t0 < tokens; t0 += kMaxGroups) {
+    const unsigned rows = (unsigned)std::min(tokens - t0, kMaxGroups);
+    hipLaunchKernelGGL(pref_row_kernel<T>, dim3(rows, splits), dim3(kThreads), 0, s, logits + t0 * ld, ld, V, cols,
+                       labels + t0, w.part + t0 * splits, w.done);
+    if (int rc = launch_status()) return rc;
+  }
   PairArgs a;
   a.pairs = b->num_seqs / 2;
   for (a.first = 0; a.first < a.pairs; a.first += a.count) {
@@ -419,8 +422,7 @@ int gradient(const fl_preference_desc* d, long tokens, const T* logits, long ld,
   // instead of 860, 166 MB 548 instead of 542, 26 MB 319 instead of 317).
   const bool stream = (size_t)tokens * width * sizeof(T) >= kStreamBytes;
   const auto kernel = stream ? pref_grad_kernel<T, true> : pref_grad_kernel<T, false>;
-  // (rows x blocks would pass a launch's 2^31 workgroups from 2^26 rows on)
-  const long most = std::max(1L, (1L << 30) / blocks);
+  const long most = kMaxGroups / blocks;  // (a row has 2^14 blocks at most)
   for (long t1 = tokens; t1 > 0;) {
     const long t0 = std::max(0L, t1 - most);
     hipLaunchKernelGGL(kernel, dim3((unsigned)((t1 - t0) * blocks)), dim3(kThreads), 0, s,

@@ -114,6 +114,27 @@ def test_more_elements_than_32_bits_count():
     assert all(abs(p - q * want) <= (2.0 ** -8 + 2.0 ** -22) * q * want for p, q in zip(got, (3.0, 4.0, 12.0)))
 
 
+def test_more_elements_than_one_launch_takes():
+    """34 GB in bf16, the second of three tensors: its rest is scaled too, and the
+    third behind it."""
+    n = (1 << 34) + 2051
+    grads = [torch.full((5,), 2.0, dtype=torch.bfloat16, device="cuda"),
+             torch.zeros(n, dtype=torch.bfloat16, device="cuda"),
+             torch.full((7,), 2.0, dtype=torch.bfloat16, device="cuda")]
+    at = [0, (1 << 34) - 1, 1 << 34, n - 1]
+    for i in at:
+        grads[1][i] = 8.0
+    op = GradNorm(grads)
+    assert abs(float(op.clip(1.0)) - 304 ** 0.5) <= 2.0 ** -23 * 18
+    coef = float(op.result[1])
+    for g, i in [(grads[0], 0), (grads[2], 6)]:
+        assert abs(float(g[i]) - 2 * coef) <= 2.0 ** -8 * 2 * coef
+    for i in at:
+        assert abs(float(grads[1][i]) - 8 * coef) <= 2.0 ** -8 * 8 * coef
+    del grads, op, g
+    torch.cuda.empty_cache()
+
+
 def test_arena_clips_before_the_update():
     shapes = [("a", (16, 256)), ("b", (768, 16)), ("c", (5,))]
     arena = ParamArena(shapes, bf16_copy=True)

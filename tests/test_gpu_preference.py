@@ -162,6 +162,26 @@ def test_more_pairs_than_one_launch_takes():
     _check(x, 64, labels, cu, ref, 0.2, 0.1, 0.5, "f32", *_run(x, labels, cu, ref, batch, 64, "f32", eps=0.1)[1:])
 
 
+def test_more_rows_than_one_launch_takes():
+    """2^23 + 1000 rows of 8 columns, few of them with a label: the rows behind the
+    first launch's count and get their gradient."""
+    T, V = (1 << 23) + 1000, 8
+    cu = [0, 100, T - 50, T - 20, T]
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.randn((T, V), generator=g, device="cuda")
+    labels = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    rows = [3, 50, 4000, T - 60, T - 45, T - 3, T - 1]
+    for i, t in enumerate(rows):
+        labels[t] = i
+    batch = BatchDesc(cu, [0, 4])
+    _, logp, loss, total, dl = _run(x, labels, cu, None, batch, V, "f32")
+    few = [0, 2, 4, 5, 7]  # the labelled rows alone
+    _check(x[rows], V, labels[rows], few, None, 0.2, 0.0, 0.5, "f32", logp, loss, total, dl[rows])
+    rest = torch.ones(T, dtype=torch.bool, device="cuda")
+    rest[rows] = False
+    assert not dl[rest].any()
+
+
 def test_full_vocabulary():
     x, labels, cu, ref, batch = _case([40, 25], 130528, "bf16")
     _check(x, 130528, labels, cu, ref, 0.2, 0.0, 0.5, "bf16", *_run(x, labels, cu, ref, batch, 130528, "bf16")[1:])
