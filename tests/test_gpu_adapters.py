@@ -378,6 +378,46 @@ def test_captured_and_replayed_on_another_stream():
         assert all(torch.equal(p, q) for p, q in zip(captured, eager)), i
 
 
+def test_two_streams_at_once():
+    """Calls of one handle with a workspace each, on two streams: the results of one
+    after the other."""
+    parts = []
+    op = ClientAdapters(2, 16, 1024, 2048, "bf16", 2.0)
+    for seed, lens, slots in ((1, [[300], [41]], [1, 0]), (2, [[17], [1], [250]], [0, -1, 0])):
+        batch, rows = _batch(lens)
+        d = _inputs(rows[-1], 2, 16, 1024, 2048, "bf16", seed)
+        parts.append((batch, slots, d, op.workspace(batch)))
+
+    def run(batch, slots, d, ws, stream=None):
+        T = batch.total_tokens
+        y, v = torch.empty((T, 2048), dtype=torch.bfloat16, device="cuda"), torch.empty((T, 16), device="cuda")
+        dx, da = torch.empty_like(d["x"]), torch.zeros((2, 16, 1024), device="cuda")
+        db = torch.zeros((2, 2048, 16), device="cuda")
+        torch.cuda.synchronize()
+        return (y, v, dx, da, db), lambda: (
+            op.forward(batch, slots, d["x"], d["a"], d["b"], d["base"], y, v, ws, stream),
+            op.backward(batch, slots, d["dy"], d["x"], d["a"], d["b"], v, d["dres"], dx, da, db, ws, stream))
+
+    want = []
+    for p in parts:
+        out, go = run(*p)
+        go()
+        torch.cuda.synchronize()
+        want.append(out)
+    streams = [torch.cuda.Stream() for _ in parts]
+    both = [run(*p, s) for p, s in zip(parts, streams)]
+    for _ in range(5):
+        for out, _ in both:
+            out[3].zero_()
+            out[4].zero_()
+        torch.cuda.synchronize()
+        for _, go in both:
+            go()
+        torch.cuda.synchronize()
+        for (out, _), w in zip(both, want):
+            assert all(torch.equal(p, q) for p, q in zip(out, w))
+
+
 def test_offsets_past_32_bits():
     """Rows 65536 elements apart: the last ones lie past 2^31 elements."""
     T, step = 40000, 65536

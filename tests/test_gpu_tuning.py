@@ -14,8 +14,8 @@ from tests.gpu_helpers import TOL, dev, rel_l2
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
-from paper_2406_14898_amd import (BatchDesc, ClientHead, FlglmError, ParamArena, PreferenceLoss, ServerStack,  # noqa: E402
-                                  StackAdapters)
+from paper_2406_14898_amd import (BatchDesc, ClientHead, FlglmError, GradNorm, ParamArena, PreferenceLoss,  # noqa: E402
+                                  ServerStack, StackAdapters)
 
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 
@@ -288,4 +288,94 @@ def test_adapters_keep_their_tensors():
         d["a"] = d["b"] = None
     assert [p for la in adapters.record.layers[:2] for p in (la.a, la.b)] == held[:4]
     assert [p for la in adapters.record.grads[:2] for p in (la.a, la.b)] == held[4:]
+    stack.close()
+
+
+def test_adapters_with_prefix_and_glm_blocks():
+    """P-tuning prefix, scaled residual, 2-D positions and a bidirectional context:
+    one client's adapters against the stack whose W_qkv holds them, both in bf16
+    (each within the stack's own tolerance of the exact result)."""
+    shape = synth.StackShape(num_layers=2, hidden=256, num_heads=2, ffn_hidden=512, rotary_dim=64)
+    stack = ServerStack(2, 256, 2, 512, 64, "bf16", residual_alpha=2.0, rotary_2d=True, num_prefix=16)
+    batch = BatchDesc([0, 30, 71], [0, 2], [10, 7])
+    raw = [dict(synth.layer_params(shape, l, seed=1, bf16=True), **synth.prefix_params(shape, l, 16, seed=1))
+           for l in range(2)]
+    params = [{k: dev(v, "bf16") for k, v in p.items()} for p in raw]
+    ad = _adapters(1, 16, 256, 2, "bf16", 4)
+    merged = []
+    for p, d in zip(params, ad):
+        w = p["w_qkv"].double() + 1.5 * d["b"][0].double() @ d["a"][0].double()
+        merged.append(dict(p, w_qkv=w.to(torch.bfloat16)))
+    x, dy = (torch.randn((71, 256), generator=torch.Generator().manual_seed(s)).bfloat16().cuda() for s in (1, 2))
+    outs, dw = [], None
+    for use in (True, False):
+        grads = [{k: torch.zeros(v.shape, device="cuda") for k, v in p.items()} for p in params]
+        ga = _zeros(ad)
+        adapters = StackAdapters(stack, batch, [0], ad, ga, 1.5) if use else None
+        saved, ws = stack.buffers(batch, False)
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        stack.forward(batch, params if use else merged, x, y, saved, ws, adapters=adapters)
+        stack.backward(batch, params if use else merged, grads, x, saved, dy, dx, ws, adapters=adapters)
+        torch.cuda.synchronize()
+        outs.append([y, dx] + [g[k] for g in grads for k in ("prefix_k", "prefix_v")])
+        if use:
+            got = ga
+        else:
+            dw = [g["w_qkv"].double() for g in grads]
+    tol = 2 * TOL["bf16"]
+    for p, q in zip(*outs):
+        assert rel_l2(p.double().cpu().numpy(), q.double().cpu().numpy()) < tol
+    for l in range(2):
+        a, b = (ad[l][k][0].double() for k in ("a", "b"))
+        for name, w in (("a", 1.5 * b.t() @ dw[l]), ("b", 1.5 * dw[l] @ a.t())):
+            assert rel_l2(got[l][name][0].double().cpu().numpy(), w.cpu().numpy()) < tol, (l, name)
+    stack.close()
+
+
+@pytest.mark.parametrize("recompute", [False, True])
+def test_stack_with_adapters_captured(recompute):
+    """Forward, backward and clipping in one graph: every replay equals the eager
+    calls on the same input, with eager work of its own workspaces between."""
+    shape = synth.StackShape(num_layers=2, hidden=256, num_heads=4, ffn_hidden=512, rotary_dim=32)
+    stack = ServerStack(2, 256, 4, 512, 32, "bf16")
+    params = [{k: dev(v, "bf16") for k, v in synth.layer_params(shape, l, seed=1, bf16=True).items()} for l in range(2)]
+    batch = BatchDesc([0, 40, 41, 90], [0, 1, 3])
+    ad = _adapters(2, 8, 256, 2, "bf16", 4)
+    x, dy = (torch.randn((90, 256), generator=torch.Generator().manual_seed(s)).bfloat16().cuda() for s in (1, 2))
+
+    def side_of_one():
+        ga = _zeros(ad)
+        adapters = StackAdapters(stack, batch, [1, 0], ad, ga, 2.0)
+        saved, ws = stack.buffers(batch, recompute)
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        norm = GradNorm([t for d in ga for t in d.values()])
+
+        def run():
+            for d in ga:
+                for t in d.values():
+                    t.zero_()
+            stack.forward(batch, params, x, y, saved, ws, recompute, adapters=adapters)
+            stack.backward(batch, params, [{}, {}], x, saved, dy, dx, ws, recompute, adapters=adapters)
+            norm.clip(0.5)
+        return run, [y, dx, norm.result] + [t for d in ga for t in d.values()]
+
+    captured, a = side_of_one()
+    eager, b = side_of_one()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        captured()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured()
+    for i in range(4):
+        x.copy_(torch.randn_like(x))
+        eager()
+        for t in a:
+            t.fill_(3)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(a, b)), i
     stack.close()
