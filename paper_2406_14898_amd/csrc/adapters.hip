@@ -21,7 +21,7 @@
 //     (down 70 us, 4.9 TB/s of reads; up 350 us, 5.8 TB/s)
 //   backward, the same and dres: 2.05 GB in 412 us (out 194, dv_sum 6, in 190,
 //     join 13, the gradients' clearing)
-//   64 clients of one token, 4096 -> 12288, rank 16: 34 MB in 15.7 us
+//   64 clients of one token, 4096 -> 12288, rank 16: 34 MB in 15.0 us
 //   one token, rank 8: 6.1 us
 //
 // v and dv are fp32.  In bf16 mode a matrix product with them runs on the bf16
@@ -970,6 +970,8 @@ int launch_status() {
 }
 long cdiv(long a, long b) { return (a + b - 1) / b; }
 
+constexpr long kCus = 256;
+
 struct Run {
   int row0, rows, slot;
 };
@@ -1010,13 +1012,19 @@ void fill(const std::vector<Run>& runs, size_t* i, int rows_a_step, Segs* t) {
 
 // Forward: workgroups along the reduction of v, for batches whose tiles alone
 // do not fill the chip; every wave has a step at least.  `up` adds the parts in
-// every block of columns, which is why they are few (4096 -> 4096, rank 64, one
-// client of 128 rows: 8 parts 16 us, 16 parts 18; 2048 rows: 7 parts 26 us, 16
-// 33, none 44; 64 clients of one row, rank 16: 3 parts 17.7 us, none 21; all
-// before `up` had the loads of four parts in flight).
+// every block of columns, four loads at a time, which is why they are few and 5
+// to 7 cost as much as 8.  (4096 -> 4096, rank 64, 512 rows: 4 parts 18.5 us, 8
+// parts 16.6, 16 parts 19.2; 41 tiles: 6 and 4 parts 28.3 and 27.1; 94 tiles: 2
+// and 4 parts 42.4 and 49.9; 128 tiles: none and 2 parts 61.8 and 50.3.  4096 ->
+// 12288, rank 16, 64 tiles: 3, 4 and 7 parts 44.0, 42.9 and 45.5, of one token
+// each 15.9, 15.0 and 16.7.)
 int splits_of(const fl_adapter_desc* d, const fl_batch_desc* b) {
-  const long tiles = b->total_tokens / kTile + b->num_clients;
-  return (int)std::max(1L, std::min<long>({256 / tiles, d->in_features / (64 * kWaves), 8}));
+  long tiles = 0;
+  for (int c = 0; c < b->num_clients; ++c)
+    tiles += cdiv(b->cu_seqlens[b->client_seq_ptr[c + 1]] - b->cu_seqlens[b->client_seq_ptr[c]], kTile);
+  long parts = kCus / tiles;
+  if (parts > 4 && parts < 8) parts = 4;
+  return (int)std::max(1L, std::min<long>({parts, d->in_features / (64 * kWaves), 8}));
 }
 // Whether operands of this width pass the last-level cache by: from a size on
 // that it would not hold for an output's reader, or for the backward.  (4096 <-> 12288, rank 16, with a scaling of
@@ -1036,7 +1044,6 @@ long in_cols(const fl_adapter_desc* d) { return cdiv(d->in_features, kInCols); }
 // Backward: workers that share the steps, for each block of columns; the chip
 // holds one workgroup of bwd_out a CU, two of bwd_in (one for ranks past 32 and
 // in fp32).
-constexpr long kCus = 256;
 long out_workers(const fl_adapter_desc* d) { return std::max(1L, kCus / (out_cols(d) * out_slices(d))); }
 long in_workers(const fl_adapter_desc* d) {
   return std::max(1L, kCus * (d->dtype == FL_BF16 && d->rank <= 32 ? 2 : 1) / in_cols(d));
