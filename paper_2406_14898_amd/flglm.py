@@ -544,8 +544,9 @@ def fl_adapter_backward(desc: fl_adapter_desc, batch: BatchDesc, client_adapter,
 def stack_adapters(num_adapters: int, rank: int, scale: float, batch: BatchDesc, client_adapter, layers,
                    grads=None) -> fl_stack_adapters:
     """layers / grads: one dict of device tensors "a", "b" a block.  The record
-    keeps the host arrays that it points at."""
-    arr, p = _client_adapter(client_adapter, batch)
+    keeps the host arrays that it points at, and they are its own: a caller may
+    refill client_adapter between a forward and its backward."""
+    arr, p = _client_adapter(np.array(client_adapter), batch)
     la = (fl_layer_adapters * len(layers))(*[fl_layer_adapters(_ptr(d["a"]), _ptr(d["b"])) for d in layers])
     ga = None
     if grads is not None:
