@@ -9,6 +9,7 @@ stream when torch has a GPU, else the default stream).
 
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -514,13 +515,32 @@ def fl_adapter_workspace_bytes(desc: fl_adapter_desc, batch: BatchDesc) -> int:
     return n.value
 
 
+def _exact_i32(name: str, a):
+    """Contiguous writable int32 array of the integers in a; refused where a value
+    is not one that int32 holds (a plain cast would wrap or cut it)."""
+    if type(a) in (list, tuple):
+        try:
+            return np.frombuffer(array.array("i", a), dtype=np.int32)
+        except (TypeError, ValueError, OverflowError):  # not plain integers, or none
+            pass
+    a = np.asarray(a)
+    if a.dtype == np.int32 and a.flags.c_contiguous and a.flags.writeable:
+        return a
+    try:
+        with np.errstate(invalid="ignore"):
+            arr = np.array(a, dtype=np.int32, order="C")
+        if np.array_equal(arr, a):
+            return arr
+    except (TypeError, ValueError, OverflowError):
+        pass
+    raise FlglmError(FL_ERR_ARG, f"{name} are not integers of 32 bits")
+
+
 def _client_adapter(client_adapter, batch: BatchDesc):
     n = batch.desc.num_clients
-    arr = np.ascontiguousarray(client_adapter, dtype=np.int32)
+    arr = _exact_i32("adapter slots", client_adapter)
     if arr.shape != (n,):
         raise FlglmError(FL_ERR_ARG, f"{arr.size} adapter slots for {n} clients")
-    if not arr.flags.writeable:
-        arr = arr.copy()
     return arr, (ctypes.c_int32 * n).from_buffer(arr)  # (a third of the time of arr.ctypes.data_as)
 
 
@@ -546,7 +566,7 @@ def stack_adapters(num_adapters: int, rank: int, scale: float, batch: BatchDesc,
     """layers / grads: one dict of device tensors "a", "b" a block.  The record
     keeps the host arrays that it points at, and they are its own: a caller may
     refill client_adapter between a forward and its backward."""
-    arr, p = _client_adapter(np.array(client_adapter), batch)
+    arr, p = _client_adapter(np.array(_exact_i32("adapter slots", client_adapter)), batch)
     la = (fl_layer_adapters * len(layers))(*[fl_layer_adapters(_ptr(d["a"]), _ptr(d["b"])) for d in layers])
     ga = None
     if grads is not None:
