@@ -425,6 +425,27 @@ def _host_i32(a):
     return arr, arr.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
 
 
+def _exact_i32(name: str, a):
+    """Contiguous writable int32 array of the integers in a; refused where a value
+    is not one that int32 holds (a plain cast would wrap or cut it)."""
+    if type(a) in (list, tuple):
+        try:
+            return np.frombuffer(array.array("i", a), dtype=np.int32)
+        except (TypeError, ValueError, OverflowError):  # not plain integers, or none
+            pass
+    a = np.asarray(a)
+    if a.dtype == np.int32 and a.flags.c_contiguous and a.flags.writeable:
+        return a
+    try:
+        with np.errstate(invalid="ignore"):
+            arr = np.array(a, dtype=np.int32, order="C")
+        if np.array_equal(arr, a):
+            return arr
+    except (TypeError, ValueError, OverflowError):
+        pass
+    raise FlglmError(FL_ERR_ARG, f"{name} are not integers of 32 bits")
+
+
 def fl_client_create(vocab: int, hidden: int, dtype: int = FL_BF16, ln_eps: float = 1e-5) -> int:
     h = ctypes.c_void_p()
     _check(load().fl_client_create(ctypes.byref(fl_client_desc(vocab, hidden, dtype, ln_eps)), ctypes.byref(h)))
@@ -490,11 +511,12 @@ def fl_preference_backward(desc: fl_preference_desc, batch: BatchDesc, logits, l
 
 def fl_lm_head_preference_forward(handle: int, desc: fl_preference_desc, batch: BatchDesc, h, w, labels, ref_logp, logp,
                                   loss, loss_sum, workspace, pref_workspace, stream=None, ln_g=None, ln_b=None) -> None:
-    arr, p = _host_i32(labels)
+    arr = _exact_i32("labels", labels)
     if arr.shape != (batch.total_tokens,):
         raise FlglmError(FL_ERR_ARG, f"{arr.size} labels for {batch.total_tokens} tokens")
     _check(load().fl_lm_head_preference_forward(
-        handle, ctypes.byref(desc), ctypes.byref(batch.desc), _ptr(h), _ptr(ln_g), _ptr(ln_b), _ptr(w), p,
+        handle, ctypes.byref(desc), ctypes.byref(batch.desc), _ptr(h), _ptr(ln_g), _ptr(ln_b), _ptr(w),
+        arr.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)),
         _ptr(ref_logp), _ptr(logp), _ptr(loss), _ptr(loss_sum), _ptr(workspace),
         workspace.numel() * workspace.element_size(), _ptr(pref_workspace),
         pref_workspace.numel() * pref_workspace.element_size(), _stream(stream)))
@@ -513,27 +535,6 @@ def fl_adapter_workspace_bytes(desc: fl_adapter_desc, batch: BatchDesc) -> int:
     n = ctypes.c_size_t()
     _check(load().fl_adapter_workspace_bytes(ctypes.byref(desc), ctypes.byref(batch.desc), ctypes.byref(n)))
     return n.value
-
-
-def _exact_i32(name: str, a):
-    """Contiguous writable int32 array of the integers in a; refused where a value
-    is not one that int32 holds (a plain cast would wrap or cut it)."""
-    if type(a) in (list, tuple):
-        try:
-            return np.frombuffer(array.array("i", a), dtype=np.int32)
-        except (TypeError, ValueError, OverflowError):  # not plain integers, or none
-            pass
-    a = np.asarray(a)
-    if a.dtype == np.int32 and a.flags.c_contiguous and a.flags.writeable:
-        return a
-    try:
-        with np.errstate(invalid="ignore"):
-            arr = np.array(a, dtype=np.int32, order="C")
-        if np.array_equal(arr, a):
-            return arr
-    except (TypeError, ValueError, OverflowError):
-        pass
-    raise FlglmError(FL_ERR_ARG, f"{name} are not integers of 32 bits")
 
 
 def _client_adapter(client_adapter, batch: BatchDesc):

@@ -1,6 +1,8 @@
 """Host side of the operators' binding, without a GPU: what a record keeps of
 the program's own arrays, and which integers it takes."""
 
+import os
+
 import numpy as np
 import pytest
 
@@ -52,3 +54,34 @@ def test_slots_of_every_type_that_holds_them(slots):
     assert _slots(F.stack_adapters(2, 8, 1.0, batch, slots, BLOCKS), 2) == [1, -1]
     arr, p = F._client_adapter(slots, batch)
     assert list(p) == [1, -1]
+
+
+@pytest.mark.parametrize("wrong", [2 ** 32 + 3, -2 ** 32 + 3, 3.5], ids=str)
+def test_preference_labels_that_int32_cannot_hold_are_refused(wrong):
+    """None of them is the label 3 that a cast makes of it (refused before the
+    library is called: the handle and addresses below are of nothing)."""
+    batch, desc = BatchDesc([0, 2, 4], [0, 2]), F.fl_preference_desc(1000, F.FL_BF16, 0.1, 0.0)
+    for labels in (np.array([1, wrong, 2, -100]), [1, wrong, 2, -100]):
+        with pytest.raises(F.FlglmError) as e:
+            F.fl_lm_head_preference_forward(0, desc, batch, G, G, labels, None, G, G, G, None, None)
+        assert e.value.code == F.FL_ERR_ARG and "labels" in str(e.value)
+
+
+def test_preference_labels_of_every_type_reach_the_library():
+    """Labels of other types, or read-only, pass the binding; the library refuses the
+    call for its NULL handle."""
+    batch, desc = BatchDesc([0, 2, 4], [0, 2]), F.fl_preference_desc(1000, F.FL_BF16, 0.1, 0.0)
+    if not os.path.exists(F.LIB_PATH):
+        from paper_2406_14898_amd import build
+        build.build()
+    fixed = np.array([1, 3, 2, -100], np.int32)
+    fixed.setflags(write=False)
+    for labels in ([1, 3, 2, -100], fixed, np.array([1, 3, 2, -100]), np.array([1.0, 3.0, 2.0, -100.0])):
+        room = np.zeros(8, np.uint8)
+
+        class Room:  # an address and its size
+            numel, element_size = (lambda self: 8), (lambda self: 1)
+            is_cuda, data_ptr = True, (lambda self: room.ctypes.data)
+        with pytest.raises(F.FlglmError) as e:
+            F.fl_lm_head_preference_forward(None, desc, batch, G, G, labels, None, G, G, G, Room(), Room())
+        assert e.value.code == F.FL_ERR_NULL
