@@ -416,6 +416,9 @@ typedef struct fl_stack_adapters {
   const fl_layer_adapters* layers;      /* host [N] */
   const fl_layer_adapter_grads* grads;  /* host [N]; backward only */
 } fl_stack_adapters;
+/* Adapters overlap nothing that the call writes; their gradients overlap no
+ * other buffer of the call, no adapter and no other gradient, except that
+ * blocks may share an array (their sums add up in it): else FL_ERR_ALIAS. */
 /* Device memory beside the stack's workspace: every block's v, kept from the
  * forward for the backward, and scratch. */
 int fl_stack_adapter_bytes(const fl_stack* stack, const fl_batch_desc* batch, const fl_stack_adapters* adapters,

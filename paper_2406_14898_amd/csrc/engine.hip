@@ -9,6 +9,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <new>
 #include <string>
@@ -895,9 +896,49 @@ struct StackAdapters {
   }
 };
 
-// Checks the adapters of a call and carves their workspace.
+struct Range {
+  const void* p;
+  size_t n;
+};
+
+// No gradient of the adapters may share memory with an adapter or with another
+// gradient, except that blocks may share one: their sums then add up in it.
+int check_adapter_gradients(const fl_stack* st, const fl_stack_adapters* ad, size_t na) {
+  struct Item {
+    uintptr_t a, b;
+    bool written;
+  };
+  std::vector<Item> r;
+  try {
+    r.reserve(4 * (size_t)st->d.num_layers);
+    for (int l = 0; l < st->d.num_layers; ++l) {
+      const uintptr_t a = (uintptr_t)ad->layers[l].a, b = (uintptr_t)ad->layers[l].b;
+      const uintptr_t da = (uintptr_t)ad->grads[l].a, db = (uintptr_t)ad->grads[l].b;
+      r.push_back({a, a + na * st->E, false});
+      r.push_back({b, b + 3 * na * st->E, false});
+      r.push_back({da, da + na * 4, true});
+      r.push_back({db, db + 3 * na * 4, true});
+    }
+  } catch (const std::bad_alloc&) {
+    return fail(FL_ERR_NOMEM, "out of host memory while checking the adapters' gradients");
+  }
+  std::sort(r.begin(), r.end(), [](const Item& x, const Item& y) { return x.a != y.a ? x.a < y.a : x.b < y.b; });
+  uintptr_t end_read = 0;
+  Item last{0, 0, true};  // the gradient that reaches furthest so far
+  for (const Item& x : r) {
+    const bool same = x.written && x.a == last.a && x.b == last.b;
+    if ((x.a < last.b && !same) || (x.written && x.a < end_read))
+      return fail(FL_ERR_ALIAS, "an adapter gradient overlaps an adapter or another gradient without being it");
+    if (!x.written) end_read = std::max(end_read, x.b);
+    else if (x.b > last.b) last = x;
+  }
+  return FL_OK;
+}
+
+// Checks the adapters of a call and carves their workspace.  mem: the call's
+// other buffers, those from mem[reads] on only read.
 int carve_adapters(const fl_stack* st, const fl_batch_desc* b, const fl_stack_adapters* ad, bool backward, void* ws,
-                   size_t ws_bytes, StackAdapters* out) {
+                   size_t ws_bytes, std::initializer_list<Range> mem, int reads, StackAdapters* out) {
   const int N = st->d.num_layers;
   out->ad = ad;
   out->batch = b;
@@ -914,22 +955,31 @@ int carve_adapters(const fl_stack* st, const fl_batch_desc* b, const fl_stack_ad
   out->scratch = out->v + N * out->v_bytes;
   if (int rc = adapter_check(&out->desc, b, ad->client_adapter, out->scratch, scratch)) return rc;
   if (!ad->layers || (backward && !ad->grads)) return fail(FL_ERR_NULL, "adapter layers / gradients are NULL");
+  for (const Range& m : mem)
+    if (overlap(ws, ws_bytes, m.p, m.n))
+      return fail(FL_ERR_ALIAS, "the adapters' workspace overlaps an activation, a gradient of one, saved or workspace");
   const size_t n = (size_t)ad->num_adapters * ad->rank * st->d.hidden;
+  auto meets = [&](const void* p, size_t bytes, size_t count) {
+    for (size_t i = 0; i < count; ++i)
+      if (overlap(p, bytes, mem.begin()[i].p, mem.begin()[i].n)) return true;
+    return overlap(ws, ws_bytes, p, bytes);
+  };
   for (int l = 0; l < N; ++l) {
     const fl_layer_adapters& p = ad->layers[l];
     if (!p.a || !p.b) return fail(FL_ERR_NULL, "layer %d: an adapter is NULL", l);
     if (!aligned16(p.a) || !aligned16(p.b)) return fail(FL_ERR_ALIGN, "layer %d: an adapter is not 16-byte aligned", l);
-    if (overlap(ws, ws_bytes, p.a, n * st->E) || overlap(ws, ws_bytes, p.b, 3 * n * st->E))
-      return fail(FL_ERR_ALIAS, "layer %d: an adapter overlaps the adapters' workspace", l);
+    if (meets(p.a, n * st->E, reads) || meets(p.b, 3 * n * st->E, reads))
+      return fail(FL_ERR_ALIAS, "layer %d: an adapter overlaps an output, saved or a workspace", l);
     if (!backward) continue;
     const fl_layer_adapter_grads& g = ad->grads[l];
     if (!g.a || !g.b) return fail(FL_ERR_NULL, "layer %d: an adapter gradient is NULL", l);
     if (!aligned16(g.a) || !aligned16(g.b))
       return fail(FL_ERR_ALIGN, "layer %d: an adapter gradient is not 16-byte aligned", l);
-    if (overlap(ws, ws_bytes, g.a, n * 4) || overlap(ws, ws_bytes, g.b, 3 * n * 4) || overlap(g.a, n * 4, g.b, 3 * n * 4))
-      return fail(FL_ERR_ALIAS, "layer %d: an adapter gradient overlaps the other or the adapters' workspace", l);
+    if (meets(g.a, n * 4, mem.size()) || meets(g.b, 3 * n * 4, mem.size()))
+      return fail(FL_ERR_ALIAS, "layer %d: an adapter gradient overlaps an activation, a gradient of one, saved or a "
+                                "workspace", l);
   }
-  return FL_OK;
+  return backward ? check_adapter_gradients(st, ad, n) : FL_OK;
 }
 
 }  // namespace
@@ -1070,10 +1120,9 @@ static int stack_forward(fl_stack* st, const fl_batch_desc* b, const fl_layer_pa
 
   StackAdapters sa;
   if (adapters) {
-    if ((rc = carve_adapters(st, b, adapters, false, adapter_ws, adapter_ws_bytes, &sa))) return rc;
-    if (overlap(adapter_ws, adapter_ws_bytes, ws, ws_bytes) || overlap(adapter_ws, adapter_ws_bytes, x, act) ||
-        overlap(adapter_ws, adapter_ws_bytes, y, act) || overlap(adapter_ws, adapter_ws_bytes, saved, nsaved))
-      return fail(FL_ERR_ALIAS, "the adapters' workspace overlaps x / y / saved / workspace");
+    if ((rc = carve_adapters(st, b, adapters, false, adapter_ws, adapter_ws_bytes,
+                             {{y, act}, {saved, nsaved}, {ws, ws_bytes}, {x, act}}, 3, &sa)))
+      return rc;
   }
   hipStream_t s = (hipStream_t)stream;
   Carver cw(ws);
@@ -1176,11 +1225,9 @@ static int stack_backward(fl_stack* st, const fl_batch_desc* b, const fl_layer_p
 
   StackAdapters sa;
   if (adapters) {
-    if ((rc = carve_adapters(st, b, adapters, true, adapter_ws, adapter_ws_bytes, &sa))) return rc;
-    if (overlap(adapter_ws, adapter_ws_bytes, ws, ws_bytes) || overlap(adapter_ws, adapter_ws_bytes, x, act) ||
-        overlap(adapter_ws, adapter_ws_bytes, dy, act) || overlap(adapter_ws, adapter_ws_bytes, dx, act) ||
-        overlap(adapter_ws, adapter_ws_bytes, saved, nsaved))
-      return fail(FL_ERR_ALIAS, "the adapters' workspace overlaps x / dy / dx / saved / workspace");
+    if ((rc = carve_adapters(st, b, adapters, true, adapter_ws, adapter_ws_bytes,
+                             {{dx, act}, {saved, nsaved}, {ws, ws_bytes}, {x, act}, {dy, act}}, 3, &sa)))
+      return rc;
   }
   hipStream_t s = (hipStream_t)stream;
   Carver cw(ws);
