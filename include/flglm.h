@@ -347,7 +347,8 @@ int fl_preference_backward(const fl_preference_desc* desc, const fl_batch_desc* 
  * cross-entropy's place: the logits stay in the client's workspace, where the
  * backward replaces them by their gradient.  desc's vocab and dtype are the
  * client's; labels host [T] (a negative one marks a row without label, one >=
- * vocab gives FL_ERR_ARG); the other arguments as in the four calls above. */
+ * vocab gives FL_ERR_ARG); the other arguments as in the four calls above.
+ * Outputs, gradients and workspaces overlap no other argument. */
 int fl_lm_head_preference_forward(fl_client* client, const fl_preference_desc* desc, const fl_batch_desc* batch,
                                   const void* h, const void* ln_g, const void* ln_b, const void* w,
                                   const int32_t* labels, const float* ref_logp, float* logp, float* loss,

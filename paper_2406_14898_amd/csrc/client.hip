@@ -23,6 +23,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -374,6 +375,23 @@ int head_gradients(const fl_client* c, const ClientWs& w, const void* h, const v
   return FL_OK;
 }
 
+struct Span {
+  const void* p;
+  size_t n;
+};
+// Whether one of `own` shares memory with another of them or with one of `read`
+// (NULL ones aside).
+bool any_overlap(std::initializer_list<Span> own, std::initializer_list<Span> read) {
+  const auto meet = [](const Span& a, const Span& b) { return a.p && b.p && overlap(a.p, a.n, b.p, b.n); };
+  for (const Span* a = own.begin(); a != own.end(); ++a) {
+    for (const Span* b = a + 1; b != own.end(); ++b)
+      if (meet(*a, *b)) return true;
+    for (const Span& b : read)
+      if (meet(*a, b)) return true;
+  }
+  return false;
+}
+
 // The loss's descriptor is of the client's own logits.
 int check_preference_head(const fl_client* c, const fl_preference_desc* pref, const fl_batch_desc* batch) {
   if (!c) return set_error(FL_ERR_NULL, "client handle is NULL");
@@ -547,11 +565,11 @@ int fl_lm_head_preference_forward(fl_client* c, const fl_preference_desc* pref, 
   if (!al16(h) || !al16(w_vocab)) return set_error(FL_ERR_ALIGN, "h / w not 16-byte aligned");
   if (int rc = preference_check(pref, batch, ref_logp, logp, loss, loss_sum, pref_workspace, pref_workspace_bytes))
     return rc;
-  const size_t S = batch->num_seqs;
-  if (overlap(logp, 4 * S, workspace, workspace_bytes) || overlap(loss, 2 * S, workspace, workspace_bytes) ||
-      overlap(loss_sum, 4, workspace, workspace_bytes) ||
-      overlap(pref_workspace, pref_workspace_bytes, workspace, workspace_bytes))
-    return set_error(FL_ERR_ALIAS, "outputs or the loss's workspace overlap the client's workspace");
+  const size_t S = batch->num_seqs, H = c->d.hidden, E = c->E;
+  if (any_overlap({{workspace, workspace_bytes}, {pref_workspace, pref_workspace_bytes}, {logp, 4 * S}, {loss, 2 * S},
+                   {loss_sum, 4}},
+                  {{h, T * H * E}, {w_vocab, c->d.vocab * H * E}, {ln_g, H * E}, {ln_b, H * E}, {ref_logp, 4 * S}}))
+    return set_error(FL_ERR_ALIAS, "an output or a workspace overlaps another argument");
   if (int rc = check_labels(c, labels, T)) return rc;
   const ClientWs w = carve(c, T, (char*)workspace);
   hipStream_t s = (hipStream_t)stream;
@@ -572,10 +590,11 @@ int fl_lm_head_preference_backward(fl_client* c, const fl_preference_desc* pref,
   if (int rc = check_head_backward(c, h, ln_g, w_vocab, T, grad_scale, dh, dln_g, dln_b, dw_vocab, workspace,
                                    workspace_bytes))
     return rc;
-  if (overlap(pref_workspace, pref_workspace_bytes, workspace, workspace_bytes) ||
-      overlap(pref_workspace, pref_workspace_bytes, dh, T * c->d.hidden * c->E) ||
-      (dw_vocab && overlap(pref_workspace, pref_workspace_bytes, dw_vocab, 4 * c->d.vocab * c->d.hidden)))
-    return set_error(FL_ERR_ALIAS, "the loss's workspace overlaps dh, dw or the client's workspace");
+  const size_t H = c->d.hidden, E = c->E;
+  if (any_overlap({{workspace, workspace_bytes}, {pref_workspace, pref_workspace_bytes}, {dh, T * H * E},
+                   {dw_vocab, 4 * c->d.vocab * H}, {dln_g, 4 * H}, {dln_b, 4 * H}},
+                  {{h, T * H * E}, {w_vocab, c->d.vocab * H * E}, {ln_g, H * E}}))
+    return set_error(FL_ERR_ALIAS, "a gradient or a workspace overlaps another argument");
   const ClientWs w = carve(c, T, (char*)workspace);
   hipStream_t s = (hipStream_t)stream;
   // in place: the logits become their own gradient (padded columns: 0)

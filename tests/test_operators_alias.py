@@ -97,3 +97,57 @@ def test_stack_backward_refuses_gradients_that_run_into_each_other(dtype):
                   [_grad(a=11 * G + 16), _grad(a=11 * G + 16)]):
         code, why = _stack_call(True, [_pair(), _pair()], grads, dtype)
         assert code == F.FL_ERR_ALIAS and "gradient" in why, grads
+
+
+# ---------------------------------------------------------------------------
+# The head with the preference loss
+# ---------------------------------------------------------------------------
+
+VOCAB, PAIRS = 1000, dict(cu_seqlens=[0, 5, 14, 21, 22], client_seq_ptr=[0, 2, 4])
+HEAD = dict(h=G, w=2 * G, ln_g=3 * G, ln_b=4 * G, ref=5 * G, logp=6 * G, loss=7 * G, total=8 * G, ws=9 * G, pws=10 * G,
+            dh=11 * G, dw=12 * G, dln_g=13 * G, dln_b=14 * G)
+T = 22
+HEAD_BYTES = dict(h=2 * T * H, w=2 * VOCAB * H, ln_g=2 * H, ln_b=2 * H, ref=16, dh=2 * T * H, dw=4 * VOCAB * H, dln_g=4 * H,
+                  dln_b=4 * H)
+
+
+def _head_call(backward, **at):
+    lib = _lib()
+    p = dict(HEAD, **at)
+    h = F.fl_client_create(VOCAB, H, F.FL_BF16)
+    b, d = BatchDesc(**PAIRS), F.fl_preference_desc(VOCAB, F.FL_BF16, 0.1, 0.0)
+    ws_n, pn = F.fl_client_workspace_bytes(h, T), F.fl_preference_workspace_bytes(d, b)
+    if backward:
+        code = lib.fl_lm_head_preference_backward(h, ctypes.byref(d), ctypes.byref(b.desc), p["h"], p["ln_g"], p["w"],
+                                                  ctypes.c_float(1.0), p["dh"], p["dln_g"], p["dln_b"], p["dw"], p["ws"], ws_n,
+                                                  p["pws"], pn, None)
+    else:
+        code = lib.fl_lm_head_preference_forward(h, ctypes.byref(d), ctypes.byref(b.desc), p["h"], p["ln_g"], p["ln_b"], p["w"],
+                                                 (ctypes.c_int32 * T)(*[5] * T), p["ref"], p["logp"], p["loss"], p["total"],
+                                                 p["ws"], ws_n, p["pws"], pn, None)
+    F.fl_client_destroy(h)
+    return code
+
+
+@pytest.mark.parametrize("own", ["logp", "loss", "total", "ws", "pws"])
+@pytest.mark.parametrize("other", ["h", "w", "ln_g", "ln_b", "ref"])
+def test_head_preference_forward_refuses_outputs_in_what_it_reads(own, other):
+    assert _head_call(False, **{own: HEAD[other]}) == F.FL_ERR_ALIAS
+    end = HEAD[other] + HEAD_BYTES[other] - 16  # the last bytes
+    assert _head_call(False, **{own: end}) == F.FL_ERR_ALIAS
+
+
+@pytest.mark.parametrize("own,other", [("logp", "loss"), ("logp", "total"), ("loss", "total"), ("ws", "pws"), ("logp", "ws"),
+                                       ("loss", "ws"), ("total", "ws"), ("logp", "pws"), ("total", "pws")])
+def test_head_preference_forward_refuses_outputs_in_each_other(own, other):
+    assert _head_call(False, **{own: HEAD[other]}) == F.FL_ERR_ALIAS
+
+
+@pytest.mark.parametrize("own", ["ws", "pws", "dh", "dw", "dln_g", "dln_b"])
+@pytest.mark.parametrize("other", ["h", "w", "ln_g", "ws", "pws", "dh", "dw", "dln_g", "dln_b"])
+def test_head_preference_backward_refuses_gradients_in_other_memory(own, other):
+    if own == other:
+        return
+    assert _head_call(True, **{own: HEAD[other]}) == F.FL_ERR_ALIAS
+    if other in HEAD_BYTES:
+        assert _head_call(True, **{own: HEAD[other] + HEAD_BYTES[other] - 16}) == F.FL_ERR_ALIAS
