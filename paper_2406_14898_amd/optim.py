@@ -40,6 +40,7 @@ class ParamArena:
         self.compute = torch.zeros(max(n, _ALIGN), dtype=torch.bfloat16, device=device) if bf16_copy else None
         self.step_count = 0
         self._norm: Optional[GradNorm] = None
+        self._clipped: List = []
 
     def _view(self, buf, name):
         off, shape = self.offsets[name]
@@ -71,12 +72,33 @@ class ParamArena:
         if self.compute is not None:
             self.compute.copy_(self.master)
 
+    def _runs(self) -> List[Tuple[int, int]]:
+        """(first element, elements) of the tensors' values, neighbours without
+        padding between them as one."""
+        runs: List[Tuple[int, int]] = []
+        for off, shape in self.offsets.values():
+            n = 1
+            for s in shape:
+                n *= int(s)
+            if n and runs and sum(runs[-1]) == off:
+                runs[-1] = (runs[-1][0], runs[-1][1] + n)
+            elif n:
+                runs.append((off, n))
+        return runs
+
     def clip_grad_norm(self, max_norm: float, stream=None):
         """Scales the gradients in place so that their global norm is at most
-        max_norm; returns the norm before (device fp32 [1])."""
+        max_norm; returns the norm before (device fp32 [1]).  The padding between
+        tensors, which nothing clears but a whole step, keeps its zeros: a NaN
+        coefficient would stay in it for every later norm."""
         if self._norm is None or self._norm.grads[0] is not self.grad:
             self._norm = GradNorm([self.grad])
-        return self._norm.clip(max_norm, stream=stream)
+            self._clipped = [self.grad[a:a + n] for a, n in self._runs()]
+        norm = self._norm.norm(max_norm, stream)
+        if self._clipped:
+            at = F.pointers(self._clipped)
+            F.fl_clip_grads(F.FL_F32, at, at, [t.numel() for t in self._clipped], self._norm.result, stream)
+        return norm
 
     def adam_step(self, lr: float = 2e-2, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                   zero_grad: bool = True, stream=None) -> None:

@@ -11,7 +11,7 @@ from tests.gpu_helpers import dev
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
-from paper_2406_14898_amd import BatchDesc, ServerStack, StackAdapters  # noqa: E402
+from paper_2406_14898_amd import BatchDesc, ParamArena, ServerStack, StackAdapters  # noqa: E402
 
 u = 2.0 ** -23
 
@@ -43,3 +43,29 @@ def test_blocks_that_share_a_gradient_add_up_in_it():
         assert ((shared[k].double() - (one + two)).abs() <= 64 * u * (one.abs() + two.abs()) + 64 * u *
                 float((one + two).abs().max())).all() and shared[k].any()
     stack.close()
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_bad_step_leaves_an_arena_usable(bad):
+    """NaN (or infinite) gradients, clipped, the update skipped and the gradients
+    cleared through their views, none of a size that fills its place: the next
+    norm is that of the next gradients, and the padding is still zero."""
+    arena = ParamArena([("a", (3, 7)), ("b", (16,)), ("c", (13,)), ("d", (1,))], bf16_copy=False)
+    views = arena.grad_views()
+    for t in views.values():
+        t.fill_(1.0)
+    inside = arena.grad != 0
+    views["c"][5] = bad
+    norm = float(arena.clip_grad_norm(1.0))
+    assert math.isnan(norm) if math.isnan(bad) else norm == math.inf
+    assert not arena.grad[~inside].any()
+    for t in views.values():
+        t.zero_()
+    assert float(arena.clip_grad_norm(1.0)) == 0.0
+    for t in views.values():
+        t.fill_(2.0)
+    want = 2 * math.sqrt(21 + 16 + 13 + 1)
+    assert abs(float(arena.clip_grad_norm(1.0)) - want) <= 2.0 ** -23 * want
+    # coefficient and product rounded once each
+    assert ((arena.grad[inside].double() - 2 / (want + 1e-6)).abs() <= 2.0 ** -22 * 2 / want).all()
+    assert not arena.grad[~inside].any()

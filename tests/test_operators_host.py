@@ -85,3 +85,18 @@ def test_preference_labels_of_every_type_reach_the_library():
         with pytest.raises(F.FlglmError) as e:
             F.fl_lm_head_preference_forward(None, desc, batch, G, G, labels, None, G, G, G, Room(), Room())
         assert e.value.code == F.FL_ERR_NULL
+
+
+@pytest.mark.parametrize("sizes,runs", [
+    ([(16, 16), (8,), (24,)], [(0, 288)]), ([(5,), (8,), (3, 3), (16,)], [(0, 5), (8, 17), (32, 16)]),
+    ([(0,), (7,), (0, 4), (1,)], [(0, 7), (8, 1)]), ([], []), ([(0,)], []),
+])
+def test_an_arena_knows_its_values_from_its_padding(sizes, runs):
+    """What clipping scales: every tensor's elements, none between them."""
+    from paper_2406_14898_amd import ParamArena
+    arena = ParamArena([(str(i), s) for i, s in enumerate(sizes)], bf16_copy=False, device="cpu")
+    assert arena._runs() == runs
+    for a, n in arena._runs():
+        arena.grad[a:a + n] = 1
+    assert all((t == 1).all() for t in arena.grad_views().values())
+    assert int(arena.grad.sum()) == sum(t.numel() for t in arena.grad_views().values())
