@@ -287,6 +287,41 @@ def _stream(s) -> Optional[int]:
     return s.cuda_stream
 
 
+class Memory:
+    """Device tensors that an object allocates for its own use.  torch's allocator
+    orders them with the stream they were allocated on alone, so the first use on
+    another one waits for what that stream did with the memory before, and makes
+    the allocator wait for it when the tensors are freed: an object may be dropped
+    while its kernels are still to run."""
+
+    def __init__(self, *tensors):
+        import torch
+        self.tensors = tensors
+        self.streams = {_stream(None)}
+        self.free = None
+        if not torch.cuda.is_current_stream_capturing():  # (a capture begins on an idle device)
+            self.free = torch.cuda.Event()
+            self.free.record()
+
+    def on(self, stream) -> Optional[int]:
+        """The stream's handle, for a call that uses the memory on it."""
+        s = _stream(stream)
+        if s not in self.streams:
+            self._meet(s)
+        return s
+
+    def _meet(self, s) -> None:
+        import torch
+        stream = torch.cuda.ExternalStream(s) if s else torch.cuda.default_stream()
+        with torch.cuda.stream(stream):
+            capturing = torch.cuda.is_current_stream_capturing()
+        if self.free is not None and not capturing:
+            stream.wait_event(self.free)
+        for t in self.tensors:
+            t.record_stream(stream)
+        self.streams.add(s)
+
+
 # ---------------------------------------------------------------------------
 # Descriptors
 # ---------------------------------------------------------------------------

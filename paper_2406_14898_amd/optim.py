@@ -111,7 +111,8 @@ class ParamArena:
 class GradNorm:
     """Global norm of a list of gradients (fp32 or bf16, all of one type) and
     their clipping.  Owns the workspace and the result: calls of one GradNorm
-    on different streams, or graphs captured from it, must not overlap."""
+    on different streams, or graphs captured from it, must not overlap, and it
+    lives as long as such a graph.  (Calls on any stream may outlive it.)"""
 
     def __init__(self, grads: Sequence):
         import torch
@@ -130,6 +131,7 @@ class GradNorm:
         self.array = ctypes.c_void_p * len(self.grads)
         self.workspace = torch.empty(F.fl_grad_norm_workspace_bytes(self.sizes), dtype=torch.uint8, device=dev)
         self.result = torch.empty(2, dtype=torch.float32, device=dev)  # norm, coefficient
+        self.memory = F.Memory(self.workspace, self.result)
         self.device = dev
 
     def norm(self, max_norm: float = float("inf"), stream=None):
@@ -151,18 +153,20 @@ class GradNorm:
                 raise F.FlglmError(F.FL_ERR_ARG, f"an output is not as many contiguous elements as its gradient, in "
                                                  f"{self.dtype} on device {self.device}")
             to = self._addresses(out)
-        self._norm(grads, max_norm, stream)
+        stream = self._norm(grads, max_norm, stream)
         F.fl_clip_grads(self.kind, grads, to, self.sizes, self.result, stream)
         return self.result[:1]
 
     def _addresses(self, tensors):
         return self.array(*map(type(self.result).data_ptr, tensors))
 
-    def _norm(self, grads, max_norm, stream) -> None:
+    def _norm(self, grads, max_norm, stream):
         if F.current_device() != self.device:
             raise F.FlglmError(F.FL_ERR_ARG, f"the gradients are on device {self.device}, not on the current one")
+        stream = self.memory.on(stream)
         F.fl_grad_norm(self.kind, grads, self.sizes, max_norm, self.result, self.workspace, self.workspace.numel(),
                        stream)
+        return stream
 
 
 def average(arenas: Sequence[ParamArena], stream=None) -> None:

@@ -11,7 +11,7 @@ from tests.gpu_helpers import dev
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
-from paper_2406_14898_amd import BatchDesc, ParamArena, ServerStack, StackAdapters  # noqa: E402
+from paper_2406_14898_amd import BatchDesc, GradNorm, ParamArena, ServerStack, StackAdapters  # noqa: E402
 
 u = 2.0 ** -23
 
@@ -69,3 +69,85 @@ def test_a_bad_step_leaves_an_arena_usable(bad):
     # coefficient and product rounded once each
     assert ((arena.grad[inside].double() - 2 / (want + 1e-6)).abs() <= 2.0 ** -22 * 2 / want).all()
     assert not arena.grad[~inside].any()
+
+
+class _Busy:
+    """About 10 ms of copies on a stream."""
+
+    def __init__(self):
+        self.a, self.b = (torch.empty(1 << 28, device="cuda") for _ in range(2))
+
+    def __call__(self, stream):
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                self.a.copy_(self.b)
+
+
+def _taken_and_spoilt(sizes, n=24):
+    """Tensors of these sizes in bytes, full of NaN."""
+    return [torch.full((s,), 255, dtype=torch.uint8, device="cuda") for s in sizes for _ in range(n)]
+
+
+@pytest.mark.parametrize("explicit", [True, False])
+def test_a_dropped_gradient_norm_keeps_its_memory_until_it_has_run(explicit):
+    """GradNorm(...).clip() on a stream that is busy: what the current stream
+    allocates and writes meanwhile is not the workspace."""
+    busy, side = _Busy(), torch.cuda.Stream()
+    grads = [_randn(3000000, seed=1), _randn(77, seed=2)]
+    want = math.sqrt(sum(float(g.double().square().sum()) for g in grads))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        out = [torch.empty_like(g) for g in grads]
+        torch.cuda.synchronize()
+        busy(side)
+        op = GradNorm(grads)
+        sizes = [op.workspace.numel(), 8]
+        if explicit:
+            norm = op.clip(0.5 * want, out=out, stream=side)
+        else:
+            with torch.cuda.stream(side):
+                norm = op.clip(0.5 * want, out=out)
+        del op
+        spoilt = _taken_and_spoilt(sizes)
+        torch.cuda.synchronize()
+        assert abs(float(norm) - want) <= 2.0 ** -23 * want
+        for g, o in zip(grads, out):  # norm, coefficient and product: one rounding each
+            assert ((o.double() - 0.5 * g.double()).abs() <= 4e-6 * g.double().abs()).all()
+        del spoilt, norm
+
+
+def test_a_gradient_norm_waits_for_its_memory():
+    """Its workspace was another tensor's until now, and the current stream has yet
+    to write that one: the stream of the call waits for it."""
+    busy, side = _Busy(), torch.cuda.Stream()
+    grads = [_randn(3000000, seed=1)]
+    want = float(grads[0].double().norm())
+    sizes = [GradNorm(grads).workspace.numel(), 8]
+    for _ in range(3):
+        torch.cuda.synchronize()
+        busy(torch.cuda.current_stream())
+        before = _taken_and_spoilt(sizes)
+        del before
+        norm = GradNorm(grads).norm(stream=side)
+        torch.cuda.synchronize()
+        assert abs(float(norm) - want) <= 2.0 ** -23 * want
+
+
+def test_an_arena_with_another_buffer_clips_on_another_stream():
+    """The old buffer's workspace goes while its norm is still to run."""
+    busy, side = _Busy(), torch.cuda.Stream()
+    arena = ParamArena([("a", (1000, 1000))], bf16_copy=False)
+    first, second = _randn(1000000, seed=1), _randn(1000000, seed=2, std=3.0)
+    arena.grad = first
+    want = [float(t.double().norm()) for t in (first, second)]
+    arena.clip_grad_norm(math.inf)
+    size = arena._norm.workspace.numel()
+    arena._norm = None
+    torch.cuda.synchronize()
+    busy(side)
+    norms = [arena.clip_grad_norm(math.inf, stream=side)]
+    arena.grad = second
+    norms.append(arena.clip_grad_norm(math.inf, stream=side))
+    spoilt = _taken_and_spoilt([size])
+    torch.cuda.synchronize()
+    assert all(abs(float(n) - w) <= 2.0 ** -23 * w for n, w in zip(norms, want))
