@@ -66,7 +66,8 @@ class StackAdapters:
     take as `adapters`.  layers / grads: one dict "a" [n, rank, H], "b" [n, 3H,
     rank] a block (gradients fp32, accumulated; None: forward only).  Owns the
     workspace, in which a forward leaves what its backward reads: calls on
-    different streams, or graphs captured with it, must not overlap."""
+    different streams, or graphs captured with it, must not overlap, and it lives
+    as long as such a graph.  (Calls on any stream may outlive it.)"""
 
     def __init__(self, stack, batch: F.BatchDesc, client_adapter, layers: Sequence[Dict],
                  grads: Optional[Sequence[Dict]] = None, scale: float = 1.0, device="cuda"):
@@ -87,6 +88,7 @@ class StackAdapters:
         self.record = F.stack_adapters(n, r, scale, batch, client_adapter, layers, grads)
         self.workspace = torch.empty(F.fl_stack_adapter_bytes(stack.handle, batch, self.record), dtype=torch.uint8,
                                      device=device)
+        self.memory = F.Memory(self.workspace, *self.tensors)
 
     def check(self, stack, batch: F.BatchDesc, backward: bool = False) -> None:
         """Refuses a call that the record and the workspace were not made for."""

@@ -54,6 +54,7 @@ class ServerStack:
         layers = [F.layer_params(p) for p in params]
         if adapters is not None:
             adapters.check(self, batch)
+            stream = adapters.memory.on(stream)
             F.fl_server_stack_forward_adapters(self.handle, batch, layers, adapters.record, x, y, saved, recompute,
                                                workspace, workspace.numel(), adapters.workspace,
                                                adapters.workspace.numel(), stream)
@@ -68,6 +69,7 @@ class ServerStack:
         gl = [F.layer_grads(g) for g in grads]
         if adapters is not None:
             adapters.check(self, batch, backward=True)
+            stream = adapters.memory.on(stream)
             F.fl_server_stack_backward_adapters(self.handle, batch, layers, gl, adapters.record, x, saved, dy, dx,
                                                 recompute, workspace, workspace.numel(), adapters.workspace,
                                                 adapters.workspace.numel(), stream)

@@ -151,3 +151,40 @@ def test_an_arena_with_another_buffer_clips_on_another_stream():
     spoilt = _taken_and_spoilt([size])
     torch.cuda.synchronize()
     assert all(abs(float(n) - w) <= 2.0 ** -23 * w for n, w in zip(norms, want))
+
+
+def test_dropped_stack_adapters_keep_their_memory_until_they_have_run():
+    """Forward and backward on a busy stream, the adapters dropped and their memory
+    asked for again by the current stream: the results of calls in order."""
+    H, r = 256, 8
+    shape = synth.StackShape(num_layers=2, hidden=H, num_heads=4, ffn_hidden=512, rotary_dim=32)
+    stack, batch = ServerStack(2, H, 4, 512, 32, "bf16"), BatchDesc([0, 64, 100], [0, 1, 2])
+    params = [{k: dev(v, "bf16") for k, v in synth.layer_params(shape, l, seed=1, bf16=True).items()} for l in range(2)]
+    x, dy = _randn(100, H, seed=3, dtype=torch.bfloat16), _randn(100, H, seed=4, dtype=torch.bfloat16)
+    busy, side = _Busy(), torch.cuda.Stream()
+    results = []
+    for drop in (False, True, True):
+        ad = [dict(a=_randn(2, r, H, seed=l, std=H ** -0.5, dtype=torch.bfloat16),
+                   b=_randn(2, 3 * H, r, seed=5 + l, std=0.05, dtype=torch.bfloat16)) for l in range(2)]
+        ga = [{k: torch.zeros(v.shape, device="cuda") for k, v in d.items()} for d in ad]
+        saved, ws = stack.buffers(batch, False)
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        torch.cuda.synchronize()
+        if drop:
+            busy(side)
+            held = _taken_and_spoilt([1 << 20], 2)  # the current stream's own work on what it frees
+            del held
+        adapters = StackAdapters(stack, batch, [1, 0], ad, ga, 2.0)
+        sizes = [adapters.workspace.numel()] + [d[k].numel() * 2 for d in ad for k in d]
+        ad = None
+        kw = dict(stream=side) if drop else {}
+        stack.forward(batch, params, x, y, saved, ws, adapters=adapters, **kw)
+        stack.backward(batch, params, [{}, {}], x, saved, dy, dx, ws, adapters=adapters, **kw)
+        if drop:
+            del adapters
+            spoilt = _taken_and_spoilt(sizes, 4)
+        torch.cuda.synchronize()
+        results.append([y, dx] + [g[k] for g in ga for k in ("a", "b")])
+    for got in results[1:]:
+        assert all(torch.equal(p, q) for p, q in zip(got, results[0]))
+    stack.close()
