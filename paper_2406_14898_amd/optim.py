@@ -88,9 +88,10 @@ class ParamArena:
 
     def clip_grad_norm(self, max_norm: float, stream=None):
         """Scales the gradients in place so that their global norm is at most
-        max_norm; returns the norm before (device fp32 [1]).  The padding between
-        tensors, which nothing clears but a whole step, keeps its zeros: a NaN
-        coefficient would stay in it for every later norm."""
+        max_norm; returns the norm before (device fp32 [1], which the next call
+        overwrites: clone it to keep it).  The padding between tensors, which
+        nothing clears but a whole step, keeps its zeros: a NaN coefficient would
+        stay in it for every later norm."""
         if self._norm is None or self._norm.grads[0] is not self.grad:
             self._norm = GradNorm([self.grad])
             self._clipped = [self.grad[a:a + n] for a, n in self._runs()]
@@ -112,7 +113,9 @@ class GradNorm:
     """Global norm of a list of gradients (fp32 or bf16, all of one type) and
     their clipping.  Owns the workspace and the result: calls of one GradNorm
     on different streams, or graphs captured from it, must not overlap, and it
-    lives as long as such a graph.  (Calls on any stream may outlive it.)"""
+    lives as long as such a graph.  (Calls on any stream may outlive it.)  The
+    norm that a call returns is a view of the result, which the next call
+    overwrites: clone it to keep it."""
 
     def __init__(self, grads: Sequence):
         import torch

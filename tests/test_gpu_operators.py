@@ -188,3 +188,15 @@ def test_dropped_stack_adapters_keep_their_memory_until_they_have_run():
     for got in results[1:]:
         assert all(torch.equal(p, q) for p, q in zip(got, results[0]))
     stack.close()
+
+
+def test_a_returned_norm_is_the_result_of_the_last_call():
+    """norm() and clip() return a view of `result`; a clone keeps its value."""
+    g = [torch.full((9,), 2.0, device="cuda")]
+    op = GradNorm(g)
+    first = op.norm()
+    kept = first.clone()
+    g[0].fill_(3.0)
+    second = op.clip(math.inf)
+    assert first.data_ptr() == second.data_ptr() == op.result.data_ptr() and first.shape == (1,)
+    assert float(first) == float(second) == 9.0 and float(kept) == 6.0
