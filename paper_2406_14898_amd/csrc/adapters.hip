@@ -25,9 +25,9 @@
 //   one token, rank 8: 6.1 us
 //
 // v and dv are fp32.  In bf16 mode a matrix product with them runs on the bf16
-// matrix cores in parts: v = v0 + v1 (+ v2), each part the bf16 nearest to
-// what the parts before it leave.  Two parts hold 16 digits, enough under an
-// output that is rounded to bf16; three hold all 24, for dA and dB.
+// matrix cores in parts: v = v0 + v1 (+ v2), all of v's sign.  Two parts hold 16
+// digits, enough under an output that is rounded to bf16; three hold all 24, for
+// dA and dB.
 //
 // Rows reach their adapters through a table of segments (runs of rows with
 // one slot) in kernel arguments: nothing is uploaded, and a call can be
@@ -165,17 +165,34 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 template <typename T> struct Parts;
 template <> struct Parts<bf16> { static constexpr int result = 2, exact = 3; };
 template <> struct Parts<float> { static constexpr int result = 1, exact = 1; };
-// The part of x that T holds; x becomes the rest (0 behind an infinity or NaN).
+// Part p of N of x, as T holds it; x becomes the rest.  In bf16 every part but
+// the last is cut off towards zero, and a part that would be all of x is half of
+// it: no part of a number other than zero is zero or of another sign, and all of
+// an infinity's are infinite, so a product with an infinity is the infinity that
+// it is in one piece, not a sum of infinities of both signs or of 0 times one.
+// The last part, to the nearest, leaves 2^-16 of x behind two, nothing behind three.
+template <int P, int N>
 __device__ __forceinline__ float split(float& x, float*) {
-  const float p = x;
-  x = 0.f;
-  return p;
+  return x;
 }
+template <int P, int N>
 __device__ __forceinline__ bf16 split(float& x, bf16*) {
-  const bf16 p = from_f32<bf16>(x);
-  const float f = to_f32(p);
-  x = fabsf(f) < INFINITY ? x - f : 0.f;
-  return p;
+  if constexpr (P == N - 1) {
+    return from_f32<bf16>(x);
+  } else {
+    constexpr uint32_t kHeld = 0xffff0000u;
+    uint32_t bits = __float_as_uint(x) & kHeld;
+    if (__uint_as_float(bits) == x) bits = __float_as_uint(0.5f * x) & kHeld;
+    x = fabsf(x) < INFINITY ? x - __uint_as_float(bits) : x;
+    return __builtin_bit_cast(bf16, (uint16_t)(bits >> 16));
+  }
+}
+// put(p, part p of x) for each of N parts.
+template <int N, typename T, int P = 0, typename F>
+__device__ __forceinline__ void split_each(float x, F&& put) {
+  const T part = split<P, N>(x, (T*)nullptr);
+  put(P, part);
+  if constexpr (P + 1 < N) split_each<N, T, P + 1>(x, put);
 }
 
 // A product over RP ranks with the fp32 factor in NP parts: its reduction runs
@@ -187,6 +204,7 @@ template <typename T, int RP> struct Up {
   static constexpr int weights = RP < 32 ? 1 : RP / 32;  // different weight fragments of one column
   static constexpr int stride = parts * RP + 8;          // LDS row of one token
   __device__ static __forceinline__ int chunk(int s, int g) { return 4 * s + g; }
+  // (of the others both factors are zero: a weight there might be an infinity)
   __device__ static __forceinline__ bool live(int s, int g) { return chunk(s, g) < parts * RP / 8; }
   __device__ static __forceinline__ int rank(int s, int g) { return chunk(s, g) % (RP / 8) * 8; }
 };
@@ -340,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RP <= 32 ? 5 : 1)
 #pragma unroll
     for (int s = 0; s < U::weights; ++s) {
       Vec8<T> f;
-      buf_ld8(f, wb, col_off<T>(up_col(q, m), r, U::rank(s, g), r));
+      buf_ld8(f, wb, col_off<T>(up_col(q, m), r, U::live(s, g) ? U::rank(s, g) : r, r));
       wf[q][s] = f.frag();
     }
   if (slot >= 0) {
@@ -371,8 +389,7 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RP <= 32 ? 5 : 1)
       for (int i = 0; i < n; ++i) {
         __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(f[i]), ob, col_off<float>(row + i * kRows, r, rank, r), 0,
                                               0);
-#pragma unroll
-        for (int q = 0; q < U::parts; ++q) sh[row + i * kRows][q * RP + rank] = split(f[i], (T*)nullptr);
+        split_each<U::parts, T>(f[i], [&](int q, T part) { sh[row + i * kRows][q * RP + rank] = part; });
       }
     };
     if (rows > 16) stage(std::integral_constant<int, kMany>());
@@ -613,9 +630,7 @@ __global__ void __launch_bounds__((64 * OutWaves<T>::n))
 #pragma unroll
       for (int i = 0; i < Factor<RP, NT>::n; ++i) {
         const int row = Factor<RP, NT>::row(tid, i), c = Factor<RP, NT>::rank(tid);
-        float f = vn.f[i];
-#pragma unroll
-        for (int p = 0; p < NP; ++p) dst[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
+        split_each<NP, T>(vn.f[i], [&](int p, T part) { dst[(p * RP + c) * kTokStride + row] = part; });
       }
     };
     f32x4 acc[8][RT];
@@ -761,11 +776,8 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
 #pragma unroll
       for (int i = 0; i < Factor<RP, kThreads>::n; ++i) {
         const int row = Factor<RP, kThreads>::row(tid, i), c = Factor<RP, kThreads>::rank(tid);
-        float f = vn.f[i], f2 = f;
-#pragma unroll
-        for (int p = 0; p < NP; ++p) turned[(p * RP + c) * kTokStride + row] = split(f, (T*)nullptr);
-#pragma unroll
-        for (int p = 0; p < U::parts; ++p) in_rows[row * U::stride + p * RP + c] = split(f2, (T*)nullptr);
+        split_each<NP, T>(vn.f[i], [&](int p, T part) { turned[(p * RP + c) * kTokStride + row] = part; });
+        split_each<U::parts, T>(vn.f[i], [&](int p, T part) { in_rows[row * U::stride + p * RP + c] = part; });
       }
     };
     if (live) {
@@ -785,7 +797,7 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
           const int col = c0 + 64 * h + up_col(q, m);
 #pragma unroll
           for (int s = 0; s < U::weights; ++s) {
-            const uint32_t off = col_off<T>(U::rank(s, g), in, col, in);
+            const uint32_t off = U::live(s, g) ? col_off<T>(U::rank(s, g), in, col, in) : kNowhere;
 #pragma unroll
             for (int e = 0; e < 8; ++e) wf[h][q][s][e] = buf_ld1(ab, off + e * (uint32_t)(in * sizeof(T)), (T*)nullptr);
           }

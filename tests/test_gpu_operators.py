@@ -11,9 +11,11 @@ from tests.gpu_helpers import dev
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
-from paper_2406_14898_amd import BatchDesc, GradNorm, ParamArena, ServerStack, StackAdapters  # noqa: E402
+from paper_2406_14898_amd import (BatchDesc, ClientAdapters, GradNorm, ParamArena, ServerStack,  # noqa: E402
+                                  StackAdapters)
 
 u = 2.0 ** -23
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 
 
 def _randn(*shape, seed, std=1.0, dtype=torch.float32):
@@ -200,3 +202,45 @@ def test_a_returned_norm_is_the_result_of_the_last_call():
     second = op.clip(math.inf)
     assert first.data_ptr() == second.data_ptr() == op.result.data_ptr() and first.shape == (1,)
     assert float(first) == float(second) == 9.0 and float(kept) == 6.0
+
+
+def _kind(t):
+    """0: a number, 1 / 2: infinity of either sign, 3: NaN."""
+    t = t.double().cpu()
+    return (t == math.inf) * 1 + (t == -math.inf) * 2 + torch.isnan(t) * 3
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("r", [8, 16, 24, 64])
+@pytest.mark.parametrize("where", ["x", "a", "b", "dy"])
+def test_infinities_are_those_of_the_formulas(where, r, dt):
+    """An infinite input gives infinities of the signs, and NaN in the places, that
+    the formulas in one piece give; small whole v and dv among them, which bf16
+    holds in one part."""
+    t_, inn, out = DT[dt], 72, 136
+    whole = lambda *s, seed: torch.randint(1, 5, s, generator=torch.Generator().manual_seed(seed)).to(t_).cuda()  # noqa: E731
+    for x, a, b, dy in (
+            (_randn(60, inn, seed=1, dtype=t_), _randn(2, r, inn, seed=2, std=0.1, dtype=t_),
+             _randn(2, out, r, seed=3, std=0.3, dtype=t_), _randn(60, out, seed=4, std=0.1, dtype=t_)),
+            (whole(60, inn, seed=1), whole(2, r, inn, seed=2), whole(2, out, r, seed=3), whole(60, out, seed=4))):
+        t = dict(x=x, a=a, b=b, dy=dy)[where]
+        last = tuple(n - 1 for n in t.shape)
+        spots = [(3, 5), (40, 0), last] if t.dim() == 2 else [(0, 1, 3), last]
+        for i, spot in enumerate(spots):
+            t[spot] = -math.inf if i % 2 else math.inf
+        batch, rows, slots = BatchDesc([0, 35, 60], [0, 1, 2]), [0, 35, 60], [1, 0]
+        op = ClientAdapters(2, r, inn, out, dt, 1.0)
+        ws, v = op.workspace(batch), torch.empty((60, r), device="cuda")
+        y, dx = torch.empty((60, out), dtype=t_, device="cuda"), torch.empty((60, inn), dtype=t_, device="cuda")
+        da, db = torch.zeros((2, r, inn), device="cuda"), torch.zeros((2, out, r), device="cuda")
+        print(f"[infinities] {where} r={r} {dt}", flush=True)
+        op.forward(batch, slots, x, a, b, None, y, v, ws)
+        op.backward(batch, slots, dy, x, a, b, v, None, dx, da, db, ws)
+        x, a, b, dy, v64 = (q.double().cpu() for q in (x, a, b, dy, v))
+        for c, k in enumerate(slots):
+            p = slice(rows[c], rows[c + 1])
+            want_v = x[p] @ a[k].t()
+            dv = dy[p] @ b[k]
+            for name, got, want in (("v", v[p], want_v), ("y", y[p], v64[p] @ b[k].t()), ("dx", dx[p], dv @ a[k]),
+                                    ("da", da[k], dv.t() @ x[p]), ("db", db[k], dy[p].t() @ v64[p])):
+                assert torch.equal(_kind(got), _kind(want)), name
