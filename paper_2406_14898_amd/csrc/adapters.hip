@@ -25,9 +25,8 @@
 //   one token, rank 8: 6.1 us
 //
 // v and dv are fp32.  In bf16 mode a matrix product with them runs on the bf16
-// matrix cores in parts: v = v0 + v1 (+ v2), all of v's sign.  Two parts hold 16
-// digits, enough under an output that is rounded to bf16; three hold all 24, for
-// dA and dB.
+// matrix cores in three parts: v = v0 + v1 + v2, all of v's sign, together its 24
+// digits.
 //
 // Rows reach their adapters through a table of segments (runs of rows with
 // one slot) in kernel arguments: nothing is uploaded, and a call can be
@@ -161,16 +160,14 @@ __device__ __forceinline__ float buf_ldf(Buf b, uint32_t off) {
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// How many parts of T an fp32 factor is held in, under a T and an fp32 result.
-template <typename T> struct Parts;
-template <> struct Parts<bf16> { static constexpr int result = 2, exact = 3; };
-template <> struct Parts<float> { static constexpr int result = 1, exact = 1; };
+// How many parts of T hold an fp32 factor.
+template <typename T> constexpr int kParts = sizeof(T) == 2 ? 3 : 1;
 // Part p of N of x, as T holds it; x becomes the rest.  In bf16 every part but
 // the last is cut off towards zero, and a part that would be all of x is half of
 // it: no part of a number other than zero is zero or of another sign, and all of
 // an infinity's are infinite, so a product with an infinity is the infinity that
 // it is in one piece, not a sum of infinities of both signs or of 0 times one.
-// The last part, to the nearest, leaves 2^-16 of x behind two, nothing behind three.
+// (x has 24 digits and a part 8: three parts hold all of it.)
 template <int P, int N>
 __device__ __forceinline__ float split(float& x, float*) {
   return x;
@@ -195,11 +192,14 @@ __device__ __forceinline__ void split_each(float x, F&& put) {
   if constexpr (P + 1 < N) split_each<N, T, P + 1>(x, put);
 }
 
-// A product over RP ranks with the fp32 factor in NP parts: its reduction runs
-// over NP * RP / 8 chunks of eight slots, part by part.  Step s of 32 slots,
-// lane group g: which part and which eight ranks.
+// A product over RP ranks with the fp32 factor in parts: its reduction runs over
+// parts * RP / 8 chunks of eight slots, part by part.  Step s of 32 slots, lane
+// group g: which part and which eight ranks.  Sixteen ranks have four parts, which
+// fill two steps.  (Two parts, 16 digits, would do under most results, which are
+// rounded to 8, but not where terms cancel; three cost nothing, 40583 rows forward
+// 421 us either way, but 0.5 % past rank 32.)
 template <typename T, int RP> struct Up {
-  static constexpr int parts = Parts<T>::result;
+  static constexpr int parts = sizeof(T) == 2 && RP < 32 ? 4 : kParts<T>;
   static constexpr int steps = (parts * RP + 31) / 32;
   static constexpr int weights = RP < 32 ? 1 : RP / 32;  // different weight fragments of one column
   static constexpr int stride = parts * RP + 8;          // LDS row of one token
@@ -520,7 +520,7 @@ __device__ __forceinline__ void load_tile(Vec8<T> (&xr)[8], const T* x, long ld,
 template <typename T, int RT, typename F>
 __device__ __forceinline__ void outer(f32x4 (&acc)[8][RT], const Vec8<T> (&xt)[8], const T* wt, int m, int g,
                                       F&& between) {
-  constexpr int NP = Parts<T>::exact;
+  constexpr int NP = kParts<T>;
 #pragma unroll
   for (int p = 0; p < NP; ++p)
 #pragma unroll
@@ -584,7 +584,7 @@ __global__ void __launch_bounds__((64 * OutWaves<T>::n))
     bwd_out_kernel(Segs t, Slots sl, const T* dy, long lddy, const T* b, const float* v, int stride, int out_features,
                    float scale, float* dv_part, long total_rows, float* db, float* db_part, int groups, int slices) {
   constexpr int NW = OutWaves<T>::n, NT = 64 * NW;
-  constexpr int RP = 16 * RT, NP = Parts<T>::exact;
+  constexpr int RP = 16 * RT, NP = kParts<T>;
   constexpr int kRow = 128 + 16 / (int)sizeof(T);
   constexpr int kDv = RP + 1;
   static_assert(kStep * kDv * 4 <= kStep * kRow * (int)sizeof(T), "dv fits its tile's place");
@@ -752,7 +752,7 @@ template <typename T, int RT, bool STREAM>
 __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
     bwd_in_kernel(Segs t, Slots sl, const T* x, long ldx, const T* a, const float* dv, int parts, long apart, int r,
                   int in, const T* dres, long lddr, T* dx, long lddx, float* da, float* da_part) {
-  constexpr int RP = 16 * RT, NP = Parts<T>::exact;
+  constexpr int RP = 16 * RT, NP = kParts<T>;
   using U = Up<T, RP>;
   __shared__ __align__(16) T wt[2][NP * RP * kTokStride];
   __shared__ __align__(16) T wr[2][kStep * U::stride];

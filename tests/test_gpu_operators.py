@@ -244,3 +244,41 @@ def test_infinities_are_those_of_the_formulas(where, r, dt):
             for name, got, want in (("v", v[p], want_v), ("y", y[p], v64[p] @ b[k].t()), ("dx", dx[p], dv @ a[k]),
                                     ("da", da[k], dv.t() @ x[p]), ("db", db[k], dy[p].t() @ v64[p])):
                 assert torch.equal(_kind(got), _kind(want)), name
+
+
+@pytest.mark.parametrize("r,other", [(8, 4), (24, 23), (40, 36)])
+def test_sums_that_cancel_keep_their_digits(r, other):
+    """bf16, two ranks whose contributions cancel to about 2^-11 of their size: v and
+    dv enter y and dx with all of their digits.  Bounds: two terms in four parts
+    at most are eight additions, each off by u = 2^-23 of the terms' size; dv, of
+    two products, by two more; a bf16 result by half a step, 2^-8."""
+    T, inn, out, t_ = 50, 64, 96, torch.bfloat16
+    batch, op = BatchDesc([0, T], [0, 1]), ClientAdapters(1, r, inn, out, "bf16", 1.0)
+    ws, v = op.workspace(batch), torch.empty((T, r), device="cuda")
+    x = _randn(T, inn, seed=1, dtype=t_)
+    a, b = torch.zeros((1, r, inn), dtype=t_, device="cuda"), torch.zeros((1, out, r), dtype=t_, device="cuda")
+    a[0, 0] = _randn(inn, seed=2, dtype=t_)
+    a[0, other] = a[0, 0]
+    x[:, 1] *= 2.0 ** -9
+    a[0, other, 1] *= 0.5
+    b[0, :, 0] = _randn(out, seed=3, dtype=t_)
+    b[0, :, other] = -b[0, :, 0]
+    y = torch.empty((T, out), dtype=t_, device="cuda")
+    op.forward(batch, [0], x, a, b, None, y, v, ws)
+    v64, b64 = v.double(), b[0].double()
+    want, size = v64 @ b64.t(), v64.abs() @ b64.abs().t()
+    assert (want.abs() < 2.0 ** -8 * size).double().mean() > 0.8
+    assert ((y.double() - want).abs() <= 8 * u * size + 2.0 ** -8 * want.abs()).all()
+    # the backward: dv of two columns, the second small
+    dy = torch.zeros((T, out), dtype=t_, device="cuda")
+    dy[:, 0], dy[:, 5] = _randn(T, seed=4, dtype=t_), _randn(T, seed=5, std=2.0 ** -9, dtype=t_)
+    b[0, :, other] = b[0, :, 0]
+    b[0, 5, other] *= 0.5
+    a[0, other] = -a[0, 0]
+    dx = torch.empty((T, inn), dtype=t_, device="cuda")
+    da, db = torch.zeros((1, r, inn), device="cuda"), torch.zeros((1, out, r), device="cuda")
+    op.backward(batch, [0], dy, x, a, b, v, None, dx, da, db, ws)
+    dv = dy.double() @ b[0].double()
+    dv_size = dy.double().abs() @ b[0].double().abs()
+    want, size = dv @ a[0].double(), dv_size @ a[0].double().abs()
+    assert ((dx.double() - want).abs() <= 10 * u * size + 2.0 ** -8 * want.abs()).all()
