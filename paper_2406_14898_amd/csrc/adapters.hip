@@ -940,7 +940,7 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RT <= 2 ? 2 : 1))
 }
 
 // out[slot] += the parts of its workers, in order; n elements a slot.
-// blockIdx.y: the slot's place in the table; .z: dA or dB.
+// blockIdx.y: the slot's place in the table; .z: which of two.
 struct Join {
   Slots sl;
   const float* part;
@@ -1230,41 +1230,59 @@ int adapter_backward(const fl_adapter_desc* d, const fl_batch_desc* batch, const
   // rows 54.8 -> 55.3, and 12 parts of 41447 rows 409 -> 433; past rank 32 the code
   // for it costs the long batches 2 %)
   const bool few = cols_out <= 4 && T <= 1024 && d->rank <= 32;
+  const bool one = runs.size() <= kSegs;  // one table holds the batch: dA's and dB's parts are joined in one launch
+  auto join = [&](const Join& j, const Join* other) {
+    const long n = std::max(j.n, other ? other->n : 0);
+    const dim3 grid((unsigned)cdiv(n, 4 * kThreads), std::max(j.sl.count, other ? other->sl.count : 0), other ? 2 : 1);
+    hipLaunchKernelGGL(join_kernel, grid, dim3(kThreads), 0, s, j, other ? *other : j);
+    return launch_status();
+  };
+  Slots so, si;
+  int parts_out = 0, parts_in = 0;
+  bool any = false;
   for (size_t i = 0; i < runs.size();) {
     Segs t;
     fill(runs, &i, kStep, &t);
-    Slots so, si;
-    int parts_out, parts_in;
-    const int workers_out = share_out(t, 0, out_workers(d), &so, &parts_out);
-    const int workers_in = share_out(t, -1, in_workers(d), &si, &parts_in);
+    const int workers = share_out(t, 0, out_workers(d), &so, &parts_out);
+    if (!workers) continue;
+    any = true;
     const int rc = dispatch(d, [&](auto* type, auto rt) {
       using E = std::remove_pointer_t<decltype(type)>;
       constexpr int RT = decltype(rt)::value;
-      if (workers_out) {
-        const int groups = (int)(workers_out * cols_out), slices = out_slices(d);
-        hipLaunchKernelGGL((bwd_out_kernel<E, (RT < 2 ? RT : 2)>),
-                           dim3((unsigned)(slices == 1 ? groups : cdiv(groups, 8) * 16)),
-                           dim3(64 * OutWaves<E>::n), 0, s, t, so, (const E*)dy, ld_dy, (const E*)b, v, d->rank,
-                           d->out_features, d->scale, w.dv_part, T, db, w.db_part, groups, slices);
-        if (int e = launch_status()) return e;
-        if (cols_out > 1 && !few) {
-          hipLaunchKernelGGL(dv_sum_kernel, dim3((unsigned)cdiv(T * d->rank, 4 * kThreads)), dim3(kThreads), 0, s,
-                             w.dv_part, (int)cols_out, T * d->rank);
-          if (int e = launch_status()) return e;
-        }
-      }
-      const auto in = past_cache ? bwd_in_kernel<E, RT, kLines<E>> : bwd_in_kernel<E, RT, false>;
-      hipLaunchKernelGGL(in, dim3((unsigned)(workers_in * cols_in)), dim3(kThreads), 0, s, t, si,
-                         (const E*)x, ldx, (const E*)a, w.dv_part, few ? (int)cols_out : 1, T * d->rank, d->rank,
-                         d->in_features, (const E*)dres, ld_dres, (E*)dx, ld_dx, da, w.da_part);
+      const int groups = (int)(workers * cols_out), slices = out_slices(d);
+      hipLaunchKernelGGL((bwd_out_kernel<E, (RT < 2 ? RT : 2)>),
+                         dim3((unsigned)(slices == 1 ? groups : cdiv(groups, 8) * 16)),
+                         dim3(64 * OutWaves<E>::n), 0, s, t, so, (const E*)dy, ld_dy, (const E*)b, v, d->rank,
+                         d->out_features, d->scale, w.dv_part, T, db, w.db_part, groups, slices);
       return launch_status();
     });
     if (rc) return rc;
-    if (parts_out || parts_in) {
-      const Join ja{si, w.da_part, da, na}, jb{so, w.db_part, db, nb};
-      const dim3 grid((unsigned)cdiv(std::max(na, nb), 4 * kThreads), std::max(si.count, so.count), 2);
-      hipLaunchKernelGGL(join_kernel, grid, dim3(kThreads), 0, s, ja, jb);
-      if (int e = launch_status()) return e;
+    if (!one && parts_out) {  // the next launch writes its own parts there
+      if (int e = join(Join{so, w.db_part, db, nb}, nullptr)) return e;
+    }
+  }
+  if (any && cols_out > 1 && !few) {  // (of all launches at once: each row's parts are added a single time)
+    hipLaunchKernelGGL(dv_sum_kernel, dim3((unsigned)cdiv(T * d->rank, 4 * kThreads)), dim3(kThreads), 0, s, w.dv_part,
+                       (int)cols_out, T * d->rank);
+    if (int e = launch_status()) return e;
+  }
+  for (size_t i = 0; i < runs.size();) {
+    Segs t;
+    fill(runs, &i, kStep, &t);
+    const int workers = share_out(t, -1, in_workers(d), &si, &parts_in);
+    const int rc = dispatch(d, [&](auto* type, auto rt) {
+      using E = std::remove_pointer_t<decltype(type)>;
+      constexpr int RT = decltype(rt)::value;
+      const auto in = past_cache ? bwd_in_kernel<E, RT, kLines<E>> : bwd_in_kernel<E, RT, false>;
+      hipLaunchKernelGGL(in, dim3((unsigned)(workers * cols_in)), dim3(kThreads), 0, s, t, si, (const E*)x, ldx,
+                         (const E*)a, w.dv_part, few ? (int)cols_out : 1, T * d->rank, d->rank, d->in_features,
+                         (const E*)dres, ld_dres, (E*)dx, ld_dx, da, w.da_part);
+      return launch_status();
+    });
+    if (rc) return rc;
+    if (parts_in || (one && parts_out)) {
+      const Join jb{so, w.db_part, db, nb};
+      if (int e = join(Join{si, w.da_part, da, na}, one ? &jb : nullptr)) return e;
     }
   }
   return FL_OK;

@@ -8,6 +8,7 @@ import pytest
 
 import synth
 from tests.gpu_helpers import dev
+from tests.test_gpu_adapters import _run as run_and_check
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -282,3 +283,17 @@ def test_sums_that_cancel_keep_their_digits(r, other):
     dv_size = dy.double().abs() @ b[0].double().abs()
     want, size = dv @ a[0].double(), dv_size @ a[0].double().abs()
     assert ((dx.double() - want).abs() <= 10 * u * size + 2.0 ** -8 * want.abs()).all()
+
+
+@pytest.mark.parametrize("dt,r", [("bf16", 16), ("bf16", 40), ("f32", 24)])
+@pytest.mark.parametrize("longest", [3, 9])
+def test_several_tables_of_clients_with_wide_outputs(longest, dt, r):
+    """300 clients, neighbours of different slots, so three tables of 128 runs, over
+    an output of several blocks of columns: dv's parts of up to 1024 rows are added
+    where they are read, of more rows in a pass of their own."""
+    rng = np.random.default_rng(longest)
+    lens = [[int(n)] for n in rng.integers(1, longest + 1, 300)]
+    assert (sum(n for n, in lens) > 1024) == (longest == 9)
+    slots = [(i * 5) % 7 - 1 for i in range(300)]
+    run_and_check(lens, slots, 6, r, 136, 1544, dt, seed=6)
+    run_and_check(lens, [-1] * 150 + slots[:150], 6, r, 136, 1544, dt, seed=7)  # two tables, one of nobody at first
