@@ -1029,14 +1029,12 @@ void fill(const std::vector<Run>& runs, size_t* i, int rows_a_step, Segs* t) {
 // parts 16.6, 16 parts 19.2; 41 tiles: 6 and 4 parts 28.3 and 27.1; 94 tiles: 2
 // and 4 parts 42.4 and 49.9; 128 tiles: none and 2 parts 61.8 and 50.3.  4096 ->
 // 12288, rank 16, 64 tiles: 3, 4 and 7 parts 44.0, 42.9 and 45.5, of one token
-// each 15.9, 15.0 and 16.7.)
-int splits_of(const fl_adapter_desc* d, const fl_batch_desc* b) {
-  long tiles = 0;
-  for (int c = 0; c < b->num_clients; ++c)
-    tiles += cdiv(b->cu_seqlens[b->client_seq_ptr[c + 1]] - b->cu_seqlens[b->client_seq_ptr[c]], kTile);
-  long parts = kCus / tiles;
-  if (parts > 4 && parts < 8) parts = 4;
-  return (int)std::max(1L, std::min<long>({parts, d->in_features / (64 * kWaves), 8}));
+// each 15.9, 15.0 and 16.7; 1280 -> 3840, 23 tiles: 4 and 5 parts 20.9 and 21.0.)
+// The tiles are those launched, of runs of clients with one slot: 256 clients of
+// one token and one slot, 4 tiles, 21.8 us a call, without parts 28.0.
+int splits_of(const fl_adapter_desc* d, long tiles) {
+  const long parts = std::min<long>({kCus / tiles, d->in_features / (64 * kWaves), 8});
+  return (int)std::max(1L, parts > 4 && parts < 8 ? 4 : parts);
 }
 // Whether operands of this width pass the last-level cache by: from a size on
 // that it would not hold for an output's reader, or for the backward.  (4096 <-> 12288, rank 16, with a scaling of
@@ -1098,7 +1096,9 @@ AdapterWs carve(const fl_adapter_desc* d, const fl_batch_desc* b, char* base) {
     return p;
   };
   const size_t v = (size_t)b->total_tokens * d->rank * 4;
-  const int splits = splits_of(d, b);
+  // (the slots are not known here: as many parts as any table of them gives, all
+  // clients' rows being one run of one slot)
+  const int splits = splits_of(d, cdiv(b->total_tokens, kTile));
   w.v_part = take(splits > 1 ? splits * v : 0);
   const size_t fwd = off;
   off = 0;
@@ -1189,7 +1189,9 @@ int adapter_forward(const fl_adapter_desc* d, const fl_batch_desc* batch, const 
   std::vector<Run> runs;
   if (int rc = runs_of(batch, client_adapter, false, &runs)) return rc;
   const AdapterWs w = carve(d, batch, (char*)ws);
-  const int splits = splits_of(d, batch);
+  long tiles = 0;
+  for (const Run& q : runs) tiles += cdiv(q.rows, kTile);
+  const int splits = splits_of(d, tiles);
   const long T = batch->total_tokens;
   const long cols = cdiv(d->out_features, kUpCols);
   const bool past_cache = streams(d, T, d->out_features);

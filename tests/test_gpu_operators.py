@@ -8,7 +8,7 @@ import pytest
 
 import synth
 from tests.gpu_helpers import dev
-from tests.test_gpu_adapters import _run as run_and_check
+from tests.test_gpu_adapters import _forward_check, _run as run_and_check
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -297,3 +297,28 @@ def test_several_tables_of_clients_with_wide_outputs(longest, dt, r):
     slots = [(i * 5) % 7 - 1 for i in range(300)]
     run_and_check(lens, slots, 6, r, 136, 1544, dt, seed=6)
     run_and_check(lens, [-1] * 150 + slots[:150], 6, r, 136, 1544, dt, seed=7)  # two tables, one of nobody at first
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("slots", ["one", "own", "some"])
+@pytest.mark.parametrize("lens", [[1] * 256, [64] * 4 + [65] * 3, [1, 300, 1, 7]], ids=["tokens", "tiles", "ragged"])
+def test_a_workspace_serves_every_table_of_slots(lens, slots, dt):
+    """The workspace is asked for without the slots: neighbours that share one are
+    reduced in more parts than clients of their own, all within it."""
+    n, r, inn, out = 3, 16, 2056, 264
+    rows = [0]
+    for k in lens:
+        rows.append(rows[-1] + k)
+    T, t_ = rows[-1], DT[dt]
+    table = {"one": [1] * len(lens), "own": [i % n for i in range(len(lens))],
+             "some": [(i // 5) % (n + 1) - 1 for i in range(len(lens))]}[slots]
+    batch, op = BatchDesc(rows, list(range(len(lens) + 1))), ClientAdapters(n, r, inn, out, dt, 0.5)
+    size = op.workspace(batch).numel()
+    room = torch.full((size + 4096,), 77, dtype=torch.uint8, device="cuda")
+    d = dict(x=_randn(T, inn, seed=1, dtype=t_), a=_randn(n, r, inn, seed=2, std=inn ** -0.5, dtype=t_),
+             b=_randn(n, out, r, seed=3, std=0.3, dtype=t_))
+    base = _randn(T, out, seed=4, dtype=t_)
+    y, v = torch.empty_like(base), torch.empty((T, r), device="cuda")
+    op.forward(batch, table, d["x"], d["a"], d["b"], base, y, v, room[:size])
+    _forward_check(d, rows, table, 0.5, dt, y, v, base)
+    assert (room[size:] == 77).all()
