@@ -25,9 +25,10 @@
 // (8 workgroups' latency of a few dependent loads), gradient 395 us (0.96 GB
 // read, 1.28 GB written, 5.7 TB/s).
 //
-// Sums of exponentials are fp32 (values in [0, 1], at most 2^24 of them, added
-// in parts); log-probabilities and their sums over a sequence are 64 bits,
-// because z is a difference of sums of hundreds of rows.
+// Sums of exponentials are fp32 (values in [0, 1] but for the rounding of the
+// maximum, at most 2^24 of them, added in parts); log-probabilities and their
+// sums over a sequence are 64 bits, because z is a difference of sums of hundreds
+// of rows.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -43,25 +44,33 @@ using namespace flglm;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr double kLn2 = 1.0 / (double)kLog2e;  // of the fp32 factor, so that M kLn2 gives a row's maximum back
+constexpr double kLog2e64 = 1.44269504088896340736, kLn2 = 1.0 / kLog2e64;
+constexpr float kLog2eLow = (float)(kLog2e64 - (double)kLog2e);  // what the fp32 factor leaves of log2 e
+constexpr double kLn2Far = 1.0 / (double)kLog2e;  // of that factor alone, see exp2_far
 constexpr int kPairsArg = 128;       // pairs whose bounds travel in one launch's kernel arguments
 constexpr int kMaxSplits = 8;        // (one pair, 110 rows of 130528: 8 parts 12.4 us, 16 parts 13.9)
 constexpr int kBatch = 2;            // loads of a lane at once
 constexpr long kWantGroups = 2048;   // workgroups that fill the chip, four a CU, twice
 
 // Exponentials are powers of two: with M the running maximum of x log2 e,
-// rounded to fp32 and then taken as it is, s = sum of 2^(x log2 e - M), the
-// difference in one rounding, and logsumexp = M ln 2 + ln s.  (A maximum m that
-// is rounded again in m log2 e would put an error of its own on every row.)
+// rounded to fp32 and then taken as it is, s = sum of 2^(x log2 e - M), log2 e in
+// two parts of fp32, and logsumexp = M ln 2 + ln s.  (A maximum m that is rounded
+// again in m log2 e would put an error of its own on every row.  The fp32 factor
+// alone is too small by 1.3e-8 of its size: every logsumexp would be too large by
+// that part of the mean distance from the maximum, and a sequence's sum by the sum
+// of them.  The second part costs a step of 8 pairs 2 us of 578.)
 __device__ __forceinline__ float exp2_less(float x, float M) {
-  return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -M));
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2eLow, __builtin_fmaf(x, kLog2e, -M)));
 }
 // The larger M, the more its rounding moves s: by 2^64 where |M| reaches 2^31,
 // and x log2 e overflows for the type's lowest values, with which logits are
 // masked.  So in a row whose maximum is past +-kFar, a logit past it counts as
-// +-kFar (a power of two: its M is exact), and a row of nothing but lowest
-// values is uniform.  Below an ordinary maximum such a logit gives 2^-infinity
-// = 0 as it is.
+// +-kFar and log2 e is the fp32 factor (a power of two times it: M is exact), and
+// a row of nothing but lowest values is uniform.  Below an ordinary maximum such a
+// logit gives 2^-infinity = 0 as it is.
+__device__ __forceinline__ float exp2_far(float x, float M) {
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -M));
+}
 constexpr float kFar = 0x1p30f;
 __device__ __forceinline__ bool far_row(float M) { return fabsf(M) >= kFar * kLog2e; }
 __device__ __forceinline__ float saturate(float x) {  // infinities and NaN stay
@@ -97,7 +106,7 @@ __device__ __forceinline__ void take(float& m, float& s, const Vec8<T> (&v)[N]) 
     for (int u = 0; u < N; ++u)
       for (int k = 0; k < 8; ++k) {
         const float x = saturate(v[u].get(k));
-        if (mx > -INFINITY) sum += exp2_less(x, mx);
+        if (mx > -INFINITY) sum += exp2_far(x, mx);
         else m = x != x ? x : m;
       }
     if (mx > -INFINITY) {
@@ -223,8 +232,9 @@ __global__ void __launch_bounds__(kThreads) pref_pair_kernel(PairArgs a, const T
         const float2 q = part[(long)t * splits + k];
         join(m, s, q.x, q.y);
       }
-      if (far_row(m)) x = saturate(x);
-      const double l = (double)x - ((double)m * kLn2 + log((double)s));
+      const bool far = far_row(m);
+      if (far) x = saturate(x);
+      const double l = (double)x - ((double)m * (far ? kLn2Far : kLn2) + log((double)s));
       lp[0] += t < r1 ? l : 0.0;
       lp[1] += t < r1 ? 0.0 : l;
       f[0] = m;
@@ -304,7 +314,7 @@ __global__ void __launch_bounds__(kThreads) pref_grad_kernel(const T* logits, lo
 #pragma unroll
     for (int k = 0; k < 8; ++k) g[k] = ks * exp2_less(v.get(k), f[0]);
     if (far_row(f[0])) {
-      for (int k = 0; k < 8; ++k) g[k] = ks * exp2_less(saturate(v.get(k)), f[0]);
+      for (int k = 0; k < 8; ++k) g[k] = ks * exp2_far(saturate(v.get(k)), f[0]);
     }
     if ((unsigned)(lab - j0) < 8u) {
 #pragma unroll

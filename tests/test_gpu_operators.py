@@ -12,8 +12,8 @@ from tests.test_gpu_adapters import _forward_check, _run as run_and_check
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
-from paper_2406_14898_amd import (BatchDesc, ClientAdapters, GradNorm, ParamArena, ServerStack,  # noqa: E402
-                                  StackAdapters)
+from paper_2406_14898_amd import (BatchDesc, ClientAdapters, GradNorm, ParamArena, PreferenceLoss,  # noqa: E402
+                                  ServerStack, StackAdapters)
 
 u = 2.0 ** -23
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
@@ -322,3 +322,30 @@ def test_a_workspace_serves_every_table_of_slots(lens, slots, dt):
     op.forward(batch, table, d["x"], d["a"], d["b"], base, y, v, room[:size])
     _forward_check(d, rows, table, 0.5, dt, y, v, base)
     assert (room[size:] == 77).all()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_log_probabilities_have_no_bias(dt):
+    """2048 sequences of one row each, most of its probability 9 below its maximum,
+    which is the label: single errors are roundings of either sign, of 2^-24 or a
+    few, so the mean of 2048 of them is far below one; half of one is allowed.
+    (log2 e as one fp32 number would put 1.1e-7 on every row.)"""
+    V, rows = 130528, 2048
+    cu = list(range(rows + 1))
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.empty((rows, V), dtype=DT[dt], device="cuda")
+    labels = torch.randint(0, V, (rows,), generator=g, dtype=torch.int32, device="cuda")
+    want = []
+    for t in range(0, rows, 256):
+        part = torch.randn((256, V), generator=g, device="cuda").mul_(0.5).sub_(9.0)
+        part.scatter_(1, labels[t:t + 256, None].long(), torch.rand((256, 1), generator=g, device="cuda"))
+        x[t:t + 256] = part.to(DT[dt])
+        y = x[t:t + 256].double()
+        want.append(y.gather(1, labels[t:t + 256, None].long())[:, 0] - torch.logsumexp(y, 1))
+    batch, op = BatchDesc(cu, [0, rows]), PreferenceLoss(V, dt, 0.1, 0.0)
+    ws, out = op.workspace(batch), op.outputs(batch)
+    op.forward(batch, x, labels, None, *out, ws)
+    off = out[0].double() - torch.cat(want)
+    print(f"[bias] {dt}: mean {float(off.mean()):.3g}, scatter {float(off.std()):.3g}", flush=True)
+    assert abs(float(off.mean())) <= 2.0 ** -25
+    assert float(off.abs().max()) <= 2.0 ** -20
