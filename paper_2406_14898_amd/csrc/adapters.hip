@@ -1037,13 +1037,17 @@ int splits_of(const fl_adapter_desc* d, long tiles) {
   return (int)std::max(1L, parts > 4 && parts < 8 ? 4 : parts);
 }
 // Whether operands of this width pass the last-level cache by: from a size on
-// that it would not hold for an output's reader, or for the backward.  (4096 <-> 12288, rank 16, with a scaling of
-// the output behind the call: y of 192 MB 234 us, past the cache 227, of 96 MB
-// 82 and 81, of 48 MB 43 and 48; dx of 128 MB 232 and 226, in place 260 and 265,
-// of 64 MB 121 and 124.  dx of 340 MB, alone, 438 and 412; x of 340 MB, the
-// forward alone, 424 and 418.)
-bool streams(const fl_adapter_desc* d, long rows, int width) {
-  return d->dtype == FL_BF16 && (size_t)rows * width * 2 >= kStreamBytes;
+// that it would not hold for an output's reader, or for the backward; dx in place,
+// whose old values may be in the cache, from twice that size on.  (4096 <-> 12288,
+// rank 16, the kernels with a scaling of the output behind them: y of 192 MB 234
+// us, past the cache 227, of 96 MB 82 and 81, of 48 MB 43 and 48; dx of 128 MB 232
+// and 226, of 64 MB 121 and 124; dx of 340 MB, alone, 438 and 412; x of 340 MB, the
+// forward alone, 424 and 418.  In place, with a write of the old values before them
+// too: y of 96 MB 113 and 112, of 192 MB 220 and 212, of 340 MB 386 and 373; dx of
+// 96 MB 204 and 210, of 128 MB 257 and 264, of 192 MB 371 and 373, of 256 MB 492 and
+// 491, of 340 MB 642 and 631.)
+bool streams(const fl_adapter_desc* d, long rows, int width, bool in_place_dx = false) {
+  return d->dtype == FL_BF16 && (size_t)rows * width * 2 >= (in_place_dx ? 2 * kStreamBytes : kStreamBytes);
 }
 // Backward: columns of a workgroup of bwd_out (OutWaves).
 long out_cols(const fl_adapter_desc* d) {
@@ -1226,7 +1230,7 @@ int adapter_backward(const fl_adapter_desc* d, const fl_batch_desc* batch, const
   const long T = batch->total_tokens;
   const long na = (long)d->rank * d->in_features, nb = (long)d->rank * d->out_features;
   const long cols_in = in_cols(d), cols_out = out_cols(d);
-  const bool past_cache = streams(d, T, d->in_features);
+  const bool past_cache = streams(d, T, d->in_features, dx && dx == dres);
   // dv's parts, when few and short, are added where they are read: a launch less
   // (4096 -> 4096, rank 16, 64 rows 20.4 -> 19.2 us, 1024 rows 36.6 -> 35.0; 4096
   // rows 54.8 -> 55.3, and 12 parts of 41447 rows 409 -> 433; past rank 32 the code
