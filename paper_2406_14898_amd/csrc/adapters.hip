@@ -17,7 +17,7 @@
 //
 // Measured on one MI355X, bf16, clients of one slot each (a plain copy of
 // 1 GiB moves 5.0 TB/s here, reads alone 6.2):
-//   forward, 41447 rows, 4096 -> 12288, rank 16, 32 clients: 2.35 GB in 418 us
+//   forward, 40583 rows, 4096 -> 12288, rank 16, 32 clients: 2.35 GB in 418 us
 //     (down 70 us, 4.9 TB/s of reads; up 350 us, 5.8 TB/s)
 //   backward, the same and dres: 2.05 GB in 412 us (out 194, dv_sum 6, in 190,
 //     join 13, the gradients' clearing)
@@ -126,7 +126,7 @@ __device__ __forceinline__ void buf_st8(const Vec8<float>& v, Buf b, uint32_t of
 // columns 8 g (x) and 32 + 8 g (y); an access of whole 128-byte lines is lane
 // (m, g) at row m % 8 (x) or 8 + m % 8 (y) and columns 8 (g + 4 (m / 8)).  From
 // either to the other: the upper half of each 16 lanes of x is exchanged with
-// the lower half of y.  (41447 rows forward, base and y: in halves of lines
+// the lower half of y.  (40583 rows forward, base and y: in halves of lines
 // 485 us, in whole ones 457, and past the cache 433.)
 __device__ __forceinline__ void turn(u32x4& x, u32x4& y, bool upper) {
 #pragma unroll
@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
 #pragma unroll
     for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   // 64-column steps, dealt to the splits and then to the waves in turn: two
-  // products over 32 columns each, x loaded in whole lines (41447 rows forward:
+  // products over 32 columns each, x loaded in whole lines (40583 rows forward:
   // 424 us instead of 433)
   const int nk = (in + 63) / 64, stride = gridDim.y * kWaves;
   const uint32_t xrow = (uint32_t)ldx * 16 * sizeof(T), arow = (uint32_t)in * 16 * sizeof(T);
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(kThreads) down_kernel(Segs t, const T* x, long
 // y = base + scale v B^T on one 64-row tile and 256 columns; v the sum of
 // `parts` partial reductions (parts > 1: also stored to v_out).
 // (Five waves a SIMD, of 96 registers, instead of the four of more: 64 clients
-// of one token 15.7 us instead of 16.5, 41447 rows 484 instead of 480.)
+// of one token 15.7 us instead of 16.5, 40583 rows 484 instead of 480.)
 template <typename T, int RP, bool STREAM>
 __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && RP <= 32 ? 5 : 1))
     up_kernel(Segs t, const float* v, int parts, long total_rows, float* v_out, const T* b, int r, int out_features,
@@ -504,8 +504,9 @@ constexpr int kTokStride = kStep + 8;
 
 // One 32-row x 128-column tile of X in a wave's registers: lane (m, g) holds
 // rows 8g .. 8g + 7 at columns 8m .. 8m + 7.
-// The tile is read once: non-temporal (dy: 484 -> 463 us a backward of 41447
-// rows; not for what is read in two halves of a line: 487 -> 559 in `up`).
+// The tile is read once and in whole lines: non-temporal (dy: 484 -> 463 us a
+// backward of 40583 rows; of accesses to halves of lines it costs, 487 -> 559 in
+// `up` when it had such).
 template <typename T>
 __device__ __forceinline__ void load_tile(Vec8<T> (&xr)[8], const T* x, long ld, int row0, int rows, int c0, int width,
                                           int m, int g) {
@@ -1233,7 +1234,7 @@ int adapter_backward(const fl_adapter_desc* d, const fl_batch_desc* batch, const
   const bool past_cache = streams(d, T, d->in_features, dx && dx == dres);
   // dv's parts, when few and short, are added where they are read: a launch less
   // (4096 -> 4096, rank 16, 64 rows 20.4 -> 19.2 us, 1024 rows 36.6 -> 35.0; 4096
-  // rows 54.8 -> 55.3, and 12 parts of 41447 rows 409 -> 433; past rank 32 the code
+  // rows 54.8 -> 55.3, and 12 parts of 40583 rows 409 -> 433; past rank 32 the code
   // for it costs the long batches 2 %)
   const bool few = cols_out <= 4 && T <= 1024 && d->rank <= 32;
   const bool one = runs.size() <= kSegs;  // one table holds the batch: dA's and dB's parts are joined in one launch
