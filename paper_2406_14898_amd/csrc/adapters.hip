@@ -196,8 +196,8 @@ __device__ __forceinline__ void split_each(float x, F&& put) {
 // parts * RP / 8 chunks of eight slots, part by part.  Step s of 32 slots, lane
 // group g: which part and which eight ranks.  Sixteen ranks have four parts, which
 // fill two steps.  (Two parts, 16 digits, would do under most results, which are
-// rounded to 8, but not where terms cancel; three cost nothing, 40583 rows forward
-// 421 us either way, but 0.5 % past rank 32.)
+// rounded to 8, but not where terms cancel.  The third costs short batches 0.2 us
+// of 15, rank 64 half a percent, long batches nothing.)
 template <typename T, int RP> struct Up {
   static constexpr int parts = sizeof(T) == 2 && RP < 32 ? 4 : kParts<T>;
   static constexpr int steps = (parts * RP + 31) / 32;
@@ -1030,12 +1030,14 @@ void fill(const std::vector<Run>& runs, size_t* i, int rows_a_step, Segs* t) {
 // parts 16.6, 16 parts 19.2; 41 tiles: 6 and 4 parts 28.3 and 27.1; 94 tiles: 2
 // and 4 parts 42.4 and 49.9; 128 tiles: none and 2 parts 61.8 and 50.3.  4096 ->
 // 12288, rank 16, 64 tiles: 3, 4 and 7 parts 44.0, 42.9 and 45.5, of one token
-// each 15.9, 15.0 and 16.7; 1280 -> 3840, 23 tiles: 4 and 5 parts 20.9 and 21.0.)
-// The tiles are those launched, of runs of clients with one slot: 256 clients of
-// one token and one slot, 4 tiles, 21.8 us a call, without parts 28.0.
+// each 15.9, 15.0 and 16.7.  Where the width allows no more than 5 to 7, they are
+// taken: 1280 -> 3840, 23 tiles, 5 and 4 parts 15.4 and 15.7.)  The tiles are those
+// launched, of runs of clients with one slot: 256 clients of one token and one
+// slot, 4 tiles, 21.8 us a call, without parts 28.0.
 int splits_of(const fl_adapter_desc* d, long tiles) {
-  const long parts = std::min<long>({kCus / tiles, d->in_features / (64 * kWaves), 8});
-  return (int)std::max(1L, parts > 4 && parts < 8 ? 4 : parts);
+  long parts = kCus / tiles;
+  if (parts > 4 && parts < 8) parts = 4;
+  return (int)std::max(1L, std::min<long>({parts, d->in_features / (64 * kWaves), 8}));
 }
 // Whether operands of this width pass the last-level cache by: from a size on
 // that it would not hold for an output's reader, or for the backward; dx in place,
