@@ -21,7 +21,7 @@
 //     (down 70 us, 4.9 TB/s of reads; up 350 us, 5.8 TB/s)
 //   backward, the same and dres: 2.05 GB in 412 us (out 194, dv_sum 6, in 190,
 //     join 13, the gradients' clearing)
-//   64 clients of one token, 4096 -> 12288, rank 16: 34 MB in 15.0 us
+//   64 clients of one token, 4096 -> 12288, rank 16: 34 MB in 15.3 us
 //   one token, rank 8: 6.1 us
 //
 // v and dv are fp32.  In bf16 mode a matrix product with them runs on the bf16
